@@ -333,6 +333,101 @@ int alexnet_softmax_xent(alexnet_t* net, const float* d_logits, const int32_t* d
 int alexnet_softmax_xent_static(const float* d_logits, const int32_t* d_labels, int32_t batch, int32_t classes,
                                 float* d_dz, float* d_loss, int32_t* d_bad_label, void* stream);
 
+/* --- group normalisation and 8-bit activation checkpoints -------------------
+ * Operators over channel-last activations [n][hw][c] of any map, without a
+ * handle: they keep no state between calls, so calls on different streams may
+ * overlap as long as their buffers differ.  The current device must be the one
+ * the pointers and the stream belong to.  All calls may be captured into HIP
+ * graphs; a captured call uses the buffers it was given at every replay.
+ *
+ * TYPE: elements of activations and their gradients; everything else
+ * (statistics, gamma, beta and their gradients, sums) is float32.  Pointers are
+ * aligned to their element; 16-byte aligned ones with pixel strides that are
+ * multiples of 16 bytes are read and written 16 bytes at a time. */
+#define ALEXNET_TYPE_FP32 0
+#define ALEXNET_TYPE_BF16 1
+#define ALEXNET_TYPE_FP16 2
+
+#define ALEXNET_ACT_NONE 0
+#define ALEXNET_ACT_RELU 1
+#define ALEXNET_ACT_SILU 2 /* z / (1 + exp(-z)) */
+
+/* An activation [rows][cols] in 8 bits: d_codes holds a byte per value, d_scales
+ * [rows][ceil(cols / 32)] a byte s per 32 consecutive columns of a row (the
+ * last block of a row may be shorter), both contiguous:
+ *   value = code * 2^(s - 127)
+ * where the code is a two's complement integer in [-127, 127] (INT8) or an
+ * 8-bit float with four exponent and three fraction bits and no infinities
+ * (E4M3).  Packing takes the smallest scale from 2^-126 up under which the
+ * block's largest magnitude is at most 127 (448) and rounds each value to the
+ * nearest code (ties to even): off by at most half a step, which is
+ * 2^(s - 128) for INT8.  A block with an infinity or a NaN is packed as s = 255
+ * and reads back as NaN throughout. */
+#define ALEXNET_CODE_INT8 0
+#define ALEXNET_CODE_E4M3 1
+typedef struct {
+  void* d_codes;
+  void* d_scales;
+  int32_t code; /* ALEXNET_CODE_* */
+} alexnet_checkpoint_t;
+
+int alexnet_checkpoint_pack(const void* d_x, int64_t ld_x, int32_t type, int64_t rows, int32_t cols,
+                            const alexnet_checkpoint_t* out, void* stream);
+/* Values are rounded once to `type` (past its range: infinity). */
+int alexnet_checkpoint_unpack(const alexnet_checkpoint_t* in, int64_t rows, int32_t cols, void* d_x, int64_t ld_x,
+                              int32_t type, void* stream);
+
+/* Weight and bias gradient of a dense layer (of a 1x1 convolution: rows are
+ * pixels) from the checkpoint of its input x [rows][in]:
+ *   dw [out][in] = dy^T x, db [out] = sum of dy over the rows (d_db may be null)
+ * with dy [rows][out] of `type` at row stride ld_dy, products of the unpacked
+ * values, float32 sums and results.  No operand is rounded: x is exact in
+ * bfloat16 and dy is multiplied as one (BF16), two (FP16) or three (FP32)
+ * bfloat16 terms.  rows may be 0 (the gradients are then zero). */
+int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes);
+int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const void* d_dy, int64_t ld_dy, int32_t type,
+                                          int64_t rows, int32_t in, int32_t out, float* d_dw, float* d_db,
+                                          void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Group normalisation with an activation, channel-last.  Channels are split
+ * into `groups` runs of c / groups; with m and v the mean and (biased) variance
+ * over the hw * c / groups values of one picture's group and r = 1/sqrt(v + eps):
+ *   z = (x - m) * r * gamma[c] + beta[c],  y = act(z)
+ * ld_* are pixel strides in elements (>= c): a call can work on a slice of the
+ * channels of a wider tensor; pictures follow each other (hw * ld_*).  y may be
+ * x and dx may be dy (same pointer and stride); other overlaps are not allowed.
+ * n and hw may be 0: nothing is read then, the statistics are m = 0 and
+ * r = 1/sqrt(eps), the parameter gradients 0. */
+typedef struct {
+  int32_t n, hw, c, groups; /* pictures, pixels of a map, channels; groups divides c */
+  int32_t type, act;        /* ALEXNET_TYPE_*, ALEXNET_ACT_* */
+  float eps;                /* > 0 */
+} alexnet_group_norm_t;
+
+/* Scratch of a call: d_workspace is 256-byte aligned and holds at least
+ * workspace_bytes (null is fine when that is 0).  It is free again once the
+ * call's work has run. */
+int alexnet_group_norm_query(const alexnet_group_norm_t* cfg, size_t* workspace_bytes);
+/* d_gamma / d_beta [c] may be null (1 / 0); d_mean / d_rstd [n][groups] (may be
+ * null) receive m and r.  keep (may be null): where to leave the 8-bit
+ * checkpoint of x as [n * hw][c], as alexnet_checkpoint_pack would. */
+int alexnet_group_norm_forward(const alexnet_group_norm_t* cfg, const void* d_x, int64_t ld_x, const float* d_gamma,
+                               const float* d_beta, void* d_y, int64_t ld_y, float* d_mean, float* d_rstd,
+                               const alexnet_checkpoint_t* keep, void* d_workspace, size_t workspace_bytes,
+                               void* stream);
+/* Gradients from dy and either x (kept null) or its checkpoint (d_x null), with
+ * the statistics of the forward call:
+ *   dz = dy * act'(z), dbeta = sum dz, dgamma = sum dz (x - m) r,
+ *   dx = r (gamma dz - mean(gamma dz) - (x - m) r mean(gamma dz (x - m) r))
+ * with means over the group.  From a checkpoint x is its unpacked values
+ * throughout.  The relu's gate is z > 0 by the exact value of z.
+ * d_dgamma / d_dbeta may be null. */
+int alexnet_group_norm_backward(const alexnet_group_norm_t* cfg, const void* d_x, int64_t ld_x,
+                                const alexnet_checkpoint_t* kept, const void* d_dy, int64_t ld_dy,
+                                const float* d_mean, const float* d_rstd, const float* d_gamma, const float* d_beta,
+                                void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, void* d_workspace,
+                                size_t workspace_bytes, void* stream);
+
 /* --- per-kernel timing (measurement aid; not part of the training path) ---
  * Between alexnet_profile_begin and alexnet_profile_end every kernel the
  * calling thread launches through this library is bracketed by two HIP events

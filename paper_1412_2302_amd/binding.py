@@ -8,6 +8,7 @@ this module fails loudly when the library has not been built
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, Optional, Tuple
 
@@ -96,6 +97,28 @@ _SIGS.update({
     "alexnet_fc_backward": [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
     "alexnet_softmax_xent": [_vp, _vp, _vp, _vp, _vp, _vp],
     "alexnet_softmax_xent_static": [_vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp],
+})
+
+
+class CheckpointArg(C.Structure):
+    _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("code", C.c_int32)]
+
+
+class GroupNormCfg(C.Structure):
+    _fields_ = [("n", C.c_int32), ("hw", C.c_int32), ("c", C.c_int32), ("groups", C.c_int32),
+                ("type", C.c_int32), ("act", C.c_int32), ("eps", C.c_float)]
+
+
+_i64, _kp, _gp = C.c_int64, C.POINTER(CheckpointArg), C.POINTER(GroupNormCfg)
+_SIGS.update({
+    "alexnet_group_norm_query": [_gp, C.POINTER(_sz)],
+    "alexnet_group_norm_forward": [_gp, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _kp, _vp, _sz, _vp],
+    "alexnet_group_norm_backward": [_gp, _vp, _i64, _kp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz,
+                                    _vp],
+    "alexnet_checkpoint_pack": [_vp, _i64, _i32, _i64, _i32, _kp, _vp],
+    "alexnet_checkpoint_unpack": [_kp, _i64, _i32, _vp, _i64, _i32, _vp],
+    "alexnet_checkpoint_fc_query": [_i64, _i32, _i32, _i32, C.POINTER(_sz)],
+    "alexnet_checkpoint_fc_backward_weight": [_kp, _vp, _i64, _i32, _i64, _i32, _i32, _vp, _vp, _vp, _sz, _vp],
 })
 _SIGS["alexnet_profile_begin"] = []
 _SIGS["alexnet_profile_end"] = [C.POINTER(ProfEntry), _i32, C.POINTER(_i32)]
@@ -569,3 +592,266 @@ def nhwc_to_nchw(x: torch.Tensor) -> torch.Tensor:
     y = torch.empty(n, c, h, w, dtype=torch.float32, device="cuda")
     _check(_lib.alexnet_nhwc_to_nchw(_ptr(x.contiguous()), _ptr(y), n, c, h, w, _stream(None)))
     return y
+
+
+# ---- group normalisation and 8-bit activation checkpoints ----
+# Channel-last tensors [n]...[c] of float32, bfloat16 or float16.  A channel slice of a wider tensor is taken as it is (pixels
+# at one stride).  Outputs and scratch are allocated on the stream that the call runs on, so calls share nothing.
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
+CODE_BLOCK = 32  # channels that share a scale
+
+
+class Checkpoint:
+    """An activation in 8 bits: codes (int8 or float8_e4m3fn) of its shape, scales (uint8) [...][ceil(c / 32)];
+    value = code * 2^(scale - 127)."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dtype not in _CODES or scales.dtype != torch.uint8:
+            raise ValueError(f"Checkpoint: codes are int8 or float8_e4m3fn and scales uint8, got {codes.dtype} and {scales.dtype}")
+        if codes.dim() < 2 or codes.shape[:-1] != scales.shape[:-1] or scales.shape[-1] != -(-codes.shape[-1] // CODE_BLOCK):
+            raise ValueError(f"Checkpoint: scales {list(scales.shape)} do not belong to codes {list(codes.shape)}")
+        if not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("Checkpoint: codes and scales must be contiguous")
+        self.codes, self.scales = codes, scales
+
+    @staticmethod
+    def empty(shape, dtype: torch.dtype, device) -> "Checkpoint":
+        if dtype not in _CODES:
+            raise ValueError(f"a checkpoint's codes are int8 or float8_e4m3fn, got {dtype}")
+        return Checkpoint(torch.empty(shape, dtype=dtype, device=device),
+                          torch.empty((*shape[:-1], -(-shape[-1] // CODE_BLOCK)), dtype=torch.uint8, device=device))
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def _arg(self) -> CheckpointArg:
+        return CheckpointArg(self.codes.data_ptr(), self.scales.data_ptr(), _CODES[self.codes.dtype])
+
+
+def _rows_stride(t, what: str) -> int:
+    """Elements from one pixel to the next of a channel-last tensor whose pixels lie at one stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor, got one on {t.device}")
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{what}: expected float32, bfloat16 or float16, got {t.dtype}")
+    if t.dim() < 2 or t.shape[-1] < 1:
+        raise ValueError(f"{what}: expected [rows]...[channels], got {list(t.shape)}")
+    c = t.shape[-1]
+    if t.is_contiguous():
+        return c
+    ld = reach = None
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if ld is None:
+            ld = reach = stride
+        elif stride != reach:
+            ld = -1
+            break
+        reach = stride * size
+    ld = c if ld is None else ld
+    if (c > 1 and t.stride(-1) != 1) or ld < c:
+        raise ValueError(f"{what}: pixels must lie at one stride with their channels side by side, got strides {t.stride()} "
+                         f"of {list(t.shape)}")
+    return ld
+
+
+class _On:
+    """The device and stream of a call.  With a stream of its own, what the call allocates belongs to that stream's pool, and
+    the allocator learns of the use of its tensors on the other one."""
+
+    def __init__(self, first: torch.Tensor, stream):
+        self.dev, self.given = first.device, stream
+        if stream is not None and stream.device != self.dev:
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors to {self.dev}")
+        self.ctx = (torch.cuda.stream(stream) if stream is not None else
+                    torch.cuda.device(self.dev) if self.dev.index != torch.cuda.current_device() else None)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            if self.given is not None:
+                self.caller = torch.cuda.current_stream(self.dev)
+            self.ctx.__enter__()
+        self.raw = torch.cuda.current_stream(self.dev).cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        return self.ctx.__exit__(*exc) if self.ctx is not None else None
+
+    def used(self, inputs, outputs):
+        if self.given is None or self.given == self.caller:
+            return
+        for t in inputs:
+            if t is not None:
+                t.record_stream(self.given)
+        for t in outputs:
+            if t is not None:
+                t.record_stream(self.caller)
+
+
+def _same_device(first: torch.Tensor, what: str, *tensors):
+    for t in tensors:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{what}: tensors on {first.device} and {t.device}")
+
+
+def _vector(t, n: int, first: torch.Tensor, what: str):
+    if t is not None:
+        _need(t, torch.float32, n, what)
+        if t.numel() != n or t.device != first.device:
+            raise ValueError(f"{what}: expected {n} elements on {first.device}, got {t.numel()} on {t.device}")
+
+
+def _result(out, shape, dtype, device, what: str):
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+        return out, shape[-1]
+    ld = _rows_stride(out, what)
+    if out.shape != shape or out.dtype != dtype or out.device != device:
+        raise ValueError(f"{what}: expected {dtype} {list(shape)} on {device}, got {out.dtype} {list(out.shape)} on {out.device}")
+    return out, ld
+
+
+@functools.lru_cache(maxsize=256)
+def _group_norm_cfg(n: int, hw: int, c: int, groups: int, kind: int, act: int, eps: float):
+    if max(n, hw, c, groups) >= 1 << 31:
+        raise ValueError("group_norm: sizes of 2^31 and more are not supported")
+    cfg, ws = GroupNormCfg(n, hw, c, groups, kind, act, eps), _sz()
+    _check(_lib.alexnet_group_norm_query(C.byref(cfg), C.byref(ws)))
+    return cfg, ws.value
+
+
+def _activation(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def group_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int,
+                       eps: float = 1e-5, act: str = "none", checkpoint: Optional[torch.dtype] = None,
+                       out: Optional[torch.Tensor] = None, stream=None):
+    """y = act(group_norm(x) * gamma + beta) of x [n]...[c]: (y, mean [n][groups], rstd [n][groups], kept).  checkpoint: the
+    type of the codes (torch.int8, torch.float8_e4m3fn) of an 8-bit copy of x to leave in `kept`, else that is None.  out: where y
+    goes (may be x)."""
+    what = "group_norm_forward"
+    ld_x = _rows_stride(x, what + ": x")
+    n, c = x.shape[0], x.shape[-1]
+    cfg, ws_bytes = _group_norm_cfg(n, x.shape[1:-1].numel(), c, groups, _TYPES[x.dtype], _activation(act), eps)
+    _vector(gamma, c, x, what + ": gamma")
+    _vector(beta, c, x, what + ": beta")
+    with _On(x, stream) as on:
+        y, ld_y = _result(out, x.shape, x.dtype, x.device, what + ": out")
+        stats = torch.empty((2, n, groups), dtype=torch.float32, device=x.device)
+        mean, rstd = stats[0], stats[1]
+        kept = None if checkpoint is None else Checkpoint.empty(x.shape, checkpoint, x.device)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device)
+        _check(_lib.alexnet_group_norm_forward(cfg, x.data_ptr(), ld_x, _ptr(gamma), _ptr(beta), y.data_ptr(), ld_y,
+                                               mean.data_ptr(), rstd.data_ptr(), None if kept is None else kept._arg(),
+                                               ws.data_ptr(), ws_bytes, on.raw))
+        on.used((x, gamma, beta, out), (y, stats) if kept is None else (y, stats, kept.codes, kept.scales))
+    return y, mean, rstd, kept
+
+
+def group_norm_backward(x, dy: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
+                        beta: Optional[torch.Tensor], act: str = "none", out: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dgamma, dbeta) of group_norm_forward from x, or its Checkpoint, and the forward call's mean and rstd.  out: where dx
+    goes (may be dy)."""
+    what = "group_norm_backward"
+    kept = x if isinstance(x, Checkpoint) else None
+    ld_x = 0 if kept is not None else _rows_stride(x, what + ": x")
+    ld_dy = _rows_stride(dy, what + ": dy")
+    if x.shape != dy.shape or (kept is None and x.dtype != dy.dtype):
+        raise ValueError(f"{what}: x {list(x.shape)} and dy {list(dy.shape)} differ in shape or type")
+    n, c = dy.shape[0], dy.shape[-1]
+    if mean.dim() != 2 or mean.shape[0] != n or mean.shape[1] < 1:
+        raise ValueError(f"{what}: mean: expected [{n}][groups], got {list(mean.shape)}")
+    groups = mean.shape[1]
+    _vector(mean, n * groups, dy, what + ": mean")
+    _vector(rstd, n * groups, dy, what + ": rstd")
+    _vector(gamma, c, dy, what + ": gamma")
+    _vector(beta, c, dy, what + ": beta")
+    source = (x,) if kept is None else (kept.codes, kept.scales)
+    _same_device(dy, what, *source)
+    cfg, ws_bytes = _group_norm_cfg(n, dy.shape[1:-1].numel(), c, groups, _TYPES[dy.dtype], _activation(act), 1e-5)
+    with _On(dy, stream) as on:
+        dx, ld_dx = _result(out, dy.shape, dy.dtype, dy.device, what + ": out")
+        grads = torch.empty((2, c), dtype=torch.float32, device=dy.device)
+        dgamma, dbeta = grads[0], grads[1]
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dy.device)
+        _check(_lib.alexnet_group_norm_backward(cfg, x.data_ptr() if kept is None else None, ld_x,
+                                                None if kept is None else kept._arg(), dy.data_ptr(), ld_dy, mean.data_ptr(),
+                                                rstd.data_ptr(), _ptr(gamma), _ptr(beta), dx.data_ptr(), ld_dx,
+                                                dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), ws_bytes, on.raw))
+        on.used((*source, dy, mean, rstd, gamma, beta, out), (dx, grads))
+    return dx, dgamma, dbeta
+
+
+def checkpoint_pack(x: torch.Tensor, dtype: torch.dtype = torch.int8, stream=None) -> Checkpoint:
+    """x [rows]...[c] in 8 bits: codes of `dtype` (torch.int8 or torch.float8_e4m3fn), a power-of-two scale per 32 channels."""
+    ld = _rows_stride(x, "checkpoint_pack: x")
+    with _On(x, stream) as on:
+        kept = Checkpoint.empty(x.shape, dtype, x.device)
+        _check(_lib.alexnet_checkpoint_pack(x.data_ptr(), ld, _TYPES[x.dtype], x.shape[:-1].numel(), x.shape[-1],
+                                            kept._arg(), on.raw))
+        on.used((x,), (kept.codes, kept.scales))
+    return kept
+
+
+def checkpoint_unpack(kept: Checkpoint, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """The values of a checkpoint as float32, bfloat16 or float16."""
+    codes = kept.codes
+    if dtype not in _TYPES:
+        raise ValueError(f"checkpoint_unpack: expected float32, bfloat16 or float16, got {dtype}")
+    _need(codes, codes.dtype, 0, "checkpoint_unpack: codes")
+    _need(kept.scales, torch.uint8, 0, "checkpoint_unpack: scales")
+    _same_device(codes, "checkpoint_unpack", kept.scales)
+    with _On(codes, stream) as on:
+        x, ld = _result(out, codes.shape, dtype, codes.device, "checkpoint_unpack: out")
+        _check(_lib.alexnet_checkpoint_unpack(kept._arg(), codes.shape[:-1].numel(), codes.shape[-1], x.data_ptr(), ld,
+                                              _TYPES[dtype], on.raw))
+        on.used((codes, kept.scales, out), (x,))
+    return x
+
+
+@functools.lru_cache(maxsize=256)
+def _checkpoint_fc_ws(rows: int, cols: int, out: int, kind: int) -> int:
+    ws = _sz()
+    _check(_lib.alexnet_checkpoint_fc_query(rows, cols, out, kind, C.byref(ws)))
+    return ws.value
+
+
+def checkpoint_fc_backward_weight(kept: Checkpoint, dy: torch.Tensor, dw: Optional[torch.Tensor] = None,
+                                  db: Optional[torch.Tensor] = None, stream=None):
+    """(dw [out][in], db [out]) in float32 of a dense layer, or of a 1 x 1 convolution over pixels, whose input [rows]...[in]
+    was kept as a Checkpoint, from dy [rows]...[out]."""
+    what = "checkpoint_fc_backward_weight"
+    codes = kept.codes
+    ld = _rows_stride(dy, what + ": dy")
+    _need(codes, codes.dtype, 0, what + ": codes")
+    _need(kept.scales, torch.uint8, 0, what + ": scales")
+    if codes.shape[:-1].numel() != dy.shape[:-1].numel():
+        raise ValueError(f"{what}: a checkpoint {list(codes.shape)} and dy {list(dy.shape)} differ in their rows")
+    rows, cols, wide = codes.shape[:-1].numel(), codes.shape[-1], dy.shape[-1]
+    _same_device(dy, what, codes, kept.scales)
+    ws_bytes = _checkpoint_fc_ws(rows, cols, wide, _TYPES[dy.dtype])
+    if dw is not None:
+        _vector(dw, wide * cols, dy, what + ": dw")
+    if db is not None:
+        _vector(db, wide, dy, what + ": db")
+    with _On(dy, stream) as on:
+        given = (dw, db)
+        dw = torch.empty((wide, cols), dtype=torch.float32, device=dy.device) if dw is None else dw
+        db = torch.empty(wide, dtype=torch.float32, device=dy.device) if db is None else db
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dy.device)
+        _check(_lib.alexnet_checkpoint_fc_backward_weight(kept._arg(), dy.data_ptr(), ld, _TYPES[dy.dtype], rows, cols, wide,
+                                                          dw.data_ptr(), db.data_ptr(), ws.data_ptr(), ws_bytes, on.raw))
+        on.used((codes, kept.scales, dy, *given), (dw, db))
+    return dw, db
