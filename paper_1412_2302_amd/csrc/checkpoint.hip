@@ -1,5 +1,4 @@
-// Activations into their 8-bit form and back (codes8.h), and the weight gradient of a dense layer that multiplies with the
-// 8-bit form itself.
+// Activations into their 8-bit form and back (codes8.h).
 #include <algorithm>
 
 #include "codes8.h"
@@ -129,61 +128,6 @@ static int checkpoint_call(const char* who, const alexnet_checkpoint_t* k, const
                                      : pack_or_unpack_type<_Float16>(a, k->code, x != nullptr, st);
 }
 
-// ---- weight gradient ----------------------------------------------------------------
-// dw[o][i] = sum over rows of dy[r][o] * x[r][i]: 16 x 16 tiles of dw, one value a thread, sixteen rows at a time through LDS.
-struct WeightArgs {
-  const uint8_t *codes, *scales;
-  int code;
-  const void* dy;
-  long ld_dy, rows;
-  int in, out, nb;
-  float *dw, *db;
-};
-template <typename T>
-__global__ void __launch_bounds__(256) weight_kernel(WeightArgs a) {
-  __shared__ float sx[16][17], sd[16][17];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, i0 = blockIdx.x * 16, o0 = blockIdx.y * 16;
-  float acc = 0.f, sum = 0.f, total = 0.f, total_b = 0.f;
-  for (long r0 = 0; r0 < a.rows; r0 += 16) {
-    if (r0 % 256 == 0) {  // sums of sums: the rounding of a long sum grows with the root of 256 rows, not of all
-      total += acc;
-      total_b += sum;
-      acc = sum = 0.f;
-    }
-    const long r = r0 + ty;
-    float x = 0.f, d = 0.f;
-    if (r < a.rows && i0 + tx < a.in) {
-      float f[4];
-      const uint32_t w = a.codes[r * a.in + i0 + tx];
-      const float s = code_scale(a.scales[r * a.nb + (i0 + tx) / kCodeBlock]);
-      if (a.code == ALEXNET_CODE_INT8)
-        codes_to_float4<ALEXNET_CODE_INT8>(w, s, f);
-      else
-        codes_to_float4<ALEXNET_CODE_E4M3>(w, s, f);
-      x = f[0];
-    }
-    if (r < a.rows && o0 + tx < a.out) d = (float)((const T*)a.dy)[r * a.ld_dy + o0 + tx];
-    __syncthreads();
-    sx[ty][tx] = x;
-    sd[ty][tx] = d;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      acc = __builtin_fmaf(sd[k][ty], sx[k][tx], acc);
-      sum += sd[k][ty];
-    }
-  }
-  if (o0 + ty < a.out && i0 + tx < a.in) a.dw[(long)(o0 + ty) * a.in + i0 + tx] = total + acc;
-  if (a.db && blockIdx.x == 0 && tx == 0 && o0 + ty < a.out) a.db[o0 + ty] = total_b + sum;
-}
-
-static int fc_check(const char* who, int64_t rows, int in, int out, int type) {
-  AX_REQUIRE(type_ok(type), ALEXNET_EINVAL, "%s: unknown type %d", who, type);
-  AX_REQUIRE(rows >= 0 && rows <= 1L << 31 && in >= 1 && in <= 1 << 20 && out >= 1 && out <= 1 << 20, ALEXNET_ESHAPE,
-             "%s: bad sizes, %ld rows of %d by %d", who, (long)rows, in, out);
-  return ALEXNET_OK;
-}
-
 }  // namespace ax
 
 using namespace ax;
@@ -198,54 +142,6 @@ int alexnet_checkpoint_pack(const void* d_x, int64_t ld_x, int32_t type, int64_t
 int alexnet_checkpoint_unpack(const alexnet_checkpoint_t* in, int64_t rows, int32_t cols, void* d_x, int64_t ld_x,
                               int32_t type, void* stream) {
   return checkpoint_call("alexnet_checkpoint_unpack", in, nullptr, d_x, ld_x, type, rows, cols, stream);
-}
-
-int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes) {
-  AX_TRY(fc_check("alexnet_checkpoint_fc_query", rows, in, out, type));
-  AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_checkpoint_fc_query: null argument");
-  *workspace_bytes = 0;
-  return ALEXNET_OK;
-}
-int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const void* d_dy, int64_t ld_dy, int32_t type,
-                                          int64_t rows, int32_t in, int32_t out, float* d_dw, float* d_db,
-                                          void* d_workspace, size_t workspace_bytes, void* stream) {
-  const char* who = "alexnet_checkpoint_fc_backward_weight";
-  AX_TRY(fc_check(who, rows, in, out, type));
-  AX_REQUIRE(d_dw, ALEXNET_EINVAL, "%s: null argument", who);
-  AX_REQUIRE(((uintptr_t)d_dw | (uintptr_t)d_db) % 4 == 0 && (uintptr_t)d_dy % type_size(type) == 0, ALEXNET_EALIGN,
-             "%s: a pointer is not aligned to its elements", who);
-  if (rows > 0) {
-    AX_REQUIRE(d_dy, ALEXNET_EINVAL, "%s: null argument", who);
-    AX_TRY(check_checkpoint(x, who));
-    AX_REQUIRE(ld_dy >= out, ALEXNET_ESHAPE, "%s: row stride %ld is under %d columns", who, (long)ld_dy, out);
-  }
-  (void)d_workspace;
-  (void)workspace_bytes;
-  hipStream_t st = (hipStream_t)stream;
-  WeightArgs a = {};
-  if (rows > 0) {
-    a.codes = (const uint8_t*)x->d_codes;
-    a.scales = (const uint8_t*)x->d_scales;
-    a.code = x->code;
-  }
-  a.dy = d_dy;
-  a.ld_dy = ld_dy;
-  a.rows = rows;
-  a.in = in;
-  a.out = out;
-  a.nb = ceil_div(in, kCodeBlock);
-  a.dw = d_dw;
-  a.db = d_db;
-  KernelScope ks("checkpoint_weight", 2.0 * rows * in * out, 4.0 * in * out, st);
-  const dim3 grid((unsigned)ceil_div(in, 16), (unsigned)ceil_div(out, 16)), block(256);
-  if (type == ALEXNET_TYPE_FP32)
-    hipLaunchKernelGGL((weight_kernel<float>), grid, block, 0, st, a);
-  else if (type == ALEXNET_TYPE_BF16)
-    hipLaunchKernelGGL((weight_kernel<__bf16>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((weight_kernel<_Float16>), grid, block, 0, st, a);
-  AX_LAUNCH_CHECK();
-  return ALEXNET_OK;
 }
 
 }  // extern "C"

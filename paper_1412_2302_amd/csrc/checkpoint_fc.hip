@@ -1,0 +1,380 @@
+// Weight gradient of a dense layer (of a 1 x 1 convolution, whose rows are pixels) from the 8-bit checkpoint of its input:
+//   dw[o][i] = sum over rows r of dy[r][o] * x[r][i],   db[o] = sum over r of dy[r][o]
+//
+// Multiplied on the bf16 matrix instructions without rounding an operand: x is a code of at most eight significant bits times a
+// power of two, which bf16 holds, and dy goes in as its leading eight bits, the next eight and the last eight (fp32; two terms
+// hold fp16, one bf16).  Sums stay fp32.
+//
+// Both operands have the summed index outermost, and the matrix instruction wants eight consecutive rows of one column in a
+// lane.  A thread therefore loads a patch of eight rows by NA (NB) columns, and while it widens and splits the values in
+// registers it turns the patch: eight rows of a column are one 16-byte unit in LDS.  Units of the columns j, j + NA, j + 2 NA,
+// ... lie side by side ("position" j * 64 + g is column g * NA + j), so that the lanes of a store write consecutive units and
+// those of a fragment read read consecutive ones; and a lane's NB accumulators are NB consecutive columns of dw.
+//
+// A workgroup of four waves owns 64 NA x 64 NB of dw and a slice of the rows, 32 rows at a time through two stages of LDS: the
+// next rows are on their way while these are multiplied.  Rows are split over workgroups where dw alone has too few tiles; the
+// slices are added up in a second launch.
+#include <algorithm>
+
+#include "codes8.h"
+#include "kernels.h"
+
+namespace ax {
+
+constexpr int kStep = 32;         // rows of a stage
+constexpr int kSliceRows = 4096;  // of a workgroup at most: a longer running sum loses more to rounding than one split up
+constexpr int kMaxSlices = 1024;
+
+struct FcArgs {
+  const uint8_t *codes, *scales;
+  const void* dy;
+  long ld_dy;
+  long rows;
+  int in, out, nb;
+  int gm, gn, slices, steps;  // tiles of dw down and across; steps of a slice
+  float *dw, *db;             // one slab of each per slice
+  long dw_slab;
+};
+
+template <typename T>
+constexpr int terms() {
+  return sizeof(T) == 4 ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;
+}
+// the upper halves of two numbers as one word: bf16 by leaving off what follows
+__device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+}
+__device__ __forceinline__ float upper(float v) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xffff0000u); }
+
+typedef uint32_t Unit __attribute__((ext_vector_type(4)));
+typedef __bf16 Frag __attribute__((ext_vector_type(8)));
+typedef float Acc __attribute__((ext_vector_type(16)));
+
+// a type that may be read or written at any address (the hardware takes vector accesses at any)
+template <typename R>
+struct __attribute__((packed)) Loose {
+  R v;
+};
+
+template <typename T, int CODE, int NA, int NB>
+__global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
+  constexpr int TERMS = terms<T>();
+  typedef T RowA __attribute__((ext_vector_type(NA)));
+  __shared__ Unit sa[2][TERMS][4][64 * NA];
+  __shared__ Unit sb[2][4][64 * NB];
+  const int t = threadIdx.x, oct = t >> 6, g = t & 63, lane = t & 63, wave = t >> 6;
+  // Workgroups go to the eight XCDs in turn: those of one XCD, which share an L2, walk the tiles of one slice of the rows
+  const int tiles = a.gm * a.gn, total = tiles * a.slices, q8 = total >> 3, r8 = total & 7, xcd = blockIdx.x & 7;
+  const int id = xcd * q8 + min(xcd, r8) + ((int)blockIdx.x >> 3);
+  const int slice = id / tiles, tile = id - slice * tiles, tm = tile / a.gn, tn = tile - tm * a.gn;
+  const int m0 = tm * 64 * NA, n0 = tn * 64 * NB;
+  const long first = (long)slice * a.steps * kStep;
+  const int rows = (int)min((long)a.steps * kStep, a.rows - first), steps = (rows + kStep - 1) / kStep;
+  const T* const dy = (const T*)a.dy + first * a.ld_dy;
+  const uint8_t* const codes = a.codes + first * a.in;
+  const uint8_t* const scales = a.scales + first * a.nb;
+  const int ca = m0 + NA * g, cb = n0 + NB * g;
+  const bool inner_a = m0 + 64 * NA <= a.out, inner_b = n0 + 64 * NB <= a.in;
+
+  T va[8][NA];
+  uint32_t vb[8];
+  uint32_t sc[8];
+  // Rows past the end and columns past the edge repeat the last ones: read in bounds, rows zeroed below, columns never stored.
+  auto load = [&](int step) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const long r = min(step * kStep + oct * 8 + i, rows - 1);
+      const T* const pa = dy + r * a.ld_dy;
+      if (inner_a) {
+        if constexpr (NA == 1) {
+          va[i][0] = pa[ca];
+        } else {
+          const RowA w = reinterpret_cast<const Loose<RowA>*>(pa + ca)->v;
+#pragma unroll
+          for (int e = 0; e < NA; ++e) va[i][e] = w[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < NA; ++e) va[i][e] = pa[min(ca + e, a.out - 1)];
+      }
+      const uint8_t* const pb = codes + r * a.in;
+      if (inner_b) {
+        if constexpr (NB == 4)
+          vb[i] = reinterpret_cast<const Loose<uint32_t>*>(pb + cb)->v;
+        else
+          vb[i] = reinterpret_cast<const Loose<uint16_t>*>(pb + cb)->v;
+      } else {
+        vb[i] = 0;
+#pragma unroll
+        for (int e = 0; e < NB; ++e) vb[i] |= (uint32_t)pb[min(cb + e, a.in - 1)] << 8 * e;
+      }
+      sc[i] = scales[r * a.nb + min(cb, a.in - 1) / kCodeBlock];
+    }
+  };
+  float sum[NA];
+#pragma unroll
+  for (int e = 0; e < NA; ++e) sum[e] = 0.f;
+  auto put = [&](int step, int stage) {
+    const int left = rows - step * kStep - oct * 8;  // rows of the patch that there are
+    float f[8][NA];
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < NA; ++e) {
+        f[i][e] = (float)va[i][e];
+        if (left < 8) f[i][e] = i < left ? f[i][e] : 0.f;
+        sum[e] += f[i][e];
+        if (TERMS > 1) most = fmaxf(most, fabsf(f[i][e]));
+      }
+    const bool endless = TERMS > 1 && most == __builtin_inff();  // infinities leave no rest: inf - inf is not a number
+#pragma unroll
+    for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+      for (int e = 0; e < NA; ++e) {
+        Unit u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = upper_halves(f[2 * i][e], f[2 * i + 1][e]);
+        sa[stage][term][oct][e * 64 + g] = u;
+        if (term + 1 < TERMS) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i][e] = endless && fabsf(f[i][e]) == __builtin_inff() ? 0.f : f[i][e] - upper(f[i][e]);
+        }
+      }
+    float x[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      codes_to_float4<CODE>(vb[i], code_scale(sc[i]), x[i]);
+      if (left < 8)
+#pragma unroll
+        for (int e = 0; e < NB; ++e) x[i][e] = i < left ? x[i][e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < NB; ++e) {
+      Unit u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = upper_halves(x[2 * i][e], x[2 * i + 1][e]);
+      sb[stage][oct][e * 64 + g] = u;
+    }
+  };
+
+  Acc acc[NA][NB];
+#pragma unroll
+  for (int j = 0; j < NA; ++j)
+#pragma unroll
+    for (int k = 0; k < NB; ++k)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[j][k][r] = 0.f;
+  const int wm = (wave >> 1) * 32 + (lane & 31), wn = (wave & 1) * 32 + (lane & 31), half = lane >> 5;
+  load(0);
+  put(0, 0);
+  for (int step = 0; step < steps; ++step) {
+    const int stage = step & 1;
+    __syncthreads();
+    if (step + 1 < steps) load(step + 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      Frag b[NB];
+#pragma unroll
+      for (int k = 0; k < NB; ++k) b[k] = __builtin_bit_cast(Frag, sb[stage][2 * h + half][k * 64 + wn]);
+#pragma unroll
+      for (int term = TERMS - 1; term >= 0; --term)
+#pragma unroll
+        for (int j = 0; j < NA; ++j) {
+          const Frag f = __builtin_bit_cast(Frag, sa[stage][term][2 * h + half][j * 64 + wm]);
+#pragma unroll
+          for (int k = 0; k < NB; ++k) acc[j][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, b[k], acc[j][k], 0, 0, 0);
+        }
+    }
+    if (step + 1 < steps) put(step + 1, stage ^ 1);
+  }
+
+  float* const dw = a.dw + slice * a.dw_slab;
+  const int ci = n0 + NB * wn;
+#pragma unroll
+  for (int j = 0; j < NA; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int o = m0 + NA * ((wave >> 1) * 32 + 8 * (r / 4) + 4 * half + r % 4) + j;
+      if (o >= a.out) continue;
+      float* const p = dw + (long)o * a.in + ci;
+      if (inner_b) {
+        typedef float RowB __attribute__((ext_vector_type(NB)));
+        RowB w;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) w[k] = acc[j][k][r];
+        reinterpret_cast<Loose<RowB>*>(p)->v = w;
+      } else {
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+          if (ci + k < a.in) p[k] = acc[j][k][r];
+      }
+    }
+  if (a.db && tn == 0) {
+    __syncthreads();
+    float* const part = reinterpret_cast<float*>(sa);
+#pragma unroll
+    for (int e = 0; e < NA; ++e) part[oct * 64 * NA + g * NA + e] = sum[e];
+    __syncthreads();
+    if (t < 64 * NA && m0 + t < a.out)
+      a.db[(long)slice * a.out + m0 + t] = (part[t] + part[64 * NA + t]) + (part[2 * 64 * NA + t] + part[3 * 64 * NA + t]);
+  }
+}
+
+// dst[i] = the sum of src[slice][i]; the gradients of the weights, then of the biases (may be null)
+__global__ void __launch_bounds__(256) fc_slices_kernel(const float* __restrict__ dw, const float* __restrict__ db, int slices, long n,
+                                                        long slab, int out, float* __restrict__ dw_out, float* __restrict__ db_out,
+                                                        int dw_blocks) {
+  typedef float V4 __attribute__((ext_vector_type(4)));
+  const bool bias = (int)blockIdx.x >= dw_blocks;
+  const long i = ((long)(bias ? blockIdx.x - dw_blocks : blockIdx.x) * 256 + threadIdx.x) * 4;
+  const long end = bias ? out : n, step = bias ? out : slab;
+  const float* const s = (bias ? db : dw) + i;
+  float* const d = (bias ? db_out : dw_out) + i;
+  if (i + 4 <= end) {
+    V4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < slices; ++k) v += reinterpret_cast<const Loose<V4>*>(s + k * step)->v;
+    reinterpret_cast<Loose<V4>*>(d)->v = v;
+  } else {
+    for (int e = 0; i + e < end; ++e) {
+      float v = 0.f;
+      for (int k = 0; k < slices; ++k) v += s[k * step + e];
+      d[e] = v;
+    }
+  }
+}
+
+// zero rows: nothing is summed
+static int fc_zero(float* dw, size_t n, float* db, int out, hipStream_t st) {
+  AX_TRY(launch_fill(dw, n, 0.f, st));
+  return db ? launch_fill(db, out, 0.f, st) : ALEXNET_OK;
+}
+
+struct FcPlan {
+  int na, nb;  // the tile is 64 na x 64 nb
+  int gm, gn, slices, steps;
+  size_t slab, ws;  // floats of a slice's dw; bytes of scratch
+};
+// Workgroups run two to a compute unit.  A workgroup costs its steps and a start; more slices shorten that and lengthen the
+// adding up, which writes and reads dw once per slice.
+static FcPlan fc_plan(long rows, int in, int out, int type) {
+  FcPlan best = {};
+  double least = 1e30;
+  const int terms = type == ALEXNET_TYPE_FP32 ? 3 : type == ALEXNET_TYPE_FP16 ? 2 : 1;
+  for (int wide = 0; wide < 2; ++wide) {
+    FcPlan p = {};
+    p.na = wide ? 2 : 1;
+    p.nb = wide ? 4 : 2;
+    p.gm = ceil_div(out, 64 * p.na);
+    p.gn = ceil_div(in, 64 * p.nb);
+    const long tiles = (long)p.gm * p.gn, steps = std::max<long>(1, (rows + kStep - 1) / kStep);
+    const int least_slices = (int)((rows + kSliceRows - 1) / kSliceRows);
+    for (int s = std::max(1, least_slices); s <= std::min<long>(steps, kMaxSlices); s += s < 16 ? 1 : s / 8) {
+      p.steps = (int)((steps + s - 1) / s);
+      p.slices = (int)((steps + p.steps - 1) / p.steps);
+      const double step = wide ? 0.35 + 0.25 * terms : 0.2 + 0.07 * terms;  // microseconds
+      const double rounds = std::max(1.0, (double)tiles * p.slices / 512);
+      const double bytes = (double)in * out * 4;
+      const double cost = std::ceil(rounds) * (p.steps * step + 2.0) + (p.slices > 1 ? 4.0 + p.slices * bytes * 2 / 4e6 : bytes / 4e6);
+      if (cost < least) {
+        least = cost;
+        best = p;
+      }
+    }
+  }
+  best.slab = ((size_t)in * out + 63) & ~(size_t)63;
+  best.ws = best.slices > 1 ? align256(best.slices * (best.slab + out) * sizeof(float)) : 0;
+  return best;
+}
+
+template <typename T, int CODE>
+static int fc_launch(const FcArgs& a, const FcPlan& p, hipStream_t st) {
+  const dim3 grid((unsigned)(p.gm * p.gn * p.slices)), block(256);
+  if (p.na == 2)
+    hipLaunchKernelGGL((fc_weight_kernel<T, CODE, 2, 4>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((fc_weight_kernel<T, CODE, 1, 2>), grid, block, 0, st, a);
+  AX_LAUNCH_CHECK();
+  return ALEXNET_OK;
+}
+template <typename T>
+static int fc_launch_code(const FcArgs& a, int code, const FcPlan& p, hipStream_t st) {
+  return code == ALEXNET_CODE_INT8 ? fc_launch<T, ALEXNET_CODE_INT8>(a, p, st) : fc_launch<T, ALEXNET_CODE_E4M3>(a, p, st);
+}
+
+static int fc_check(const char* who, int64_t rows, int in, int out, int type) {
+  AX_REQUIRE(type_ok(type), ALEXNET_EINVAL, "%s: unknown type %d", who, type);
+  AX_REQUIRE(rows >= 0 && rows <= (long)kSliceRows * kMaxSlices && in >= 1 && in <= 1 << 20 && out >= 1 && out <= 1 << 20 &&
+                 (long)in * out <= 1L << 33,
+             ALEXNET_ESHAPE, "%s: bad sizes, %ld rows of %d by %d (at most 2^22 rows, 2^20 columns and 2^33 weights)", who, (long)rows, in, out);
+  return ALEXNET_OK;
+}
+
+}  // namespace ax
+
+using namespace ax;
+
+extern "C" {
+
+int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes) {
+  AX_TRY(fc_check("alexnet_checkpoint_fc_query", rows, in, out, type));
+  AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_checkpoint_fc_query: null argument");
+  *workspace_bytes = fc_plan(rows, in, out, type).ws;
+  return ALEXNET_OK;
+}
+int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const void* d_dy, int64_t ld_dy, int32_t type,
+                                          int64_t rows, int32_t in, int32_t out, float* d_dw, float* d_db,
+                                          void* d_workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "alexnet_checkpoint_fc_backward_weight";
+  AX_TRY(fc_check(who, rows, in, out, type));
+  AX_REQUIRE(d_dw, ALEXNET_EINVAL, "%s: null argument", who);
+  AX_REQUIRE(((uintptr_t)d_dw | (uintptr_t)d_db) % 4 == 0 && (uintptr_t)d_dy % type_size(type) == 0, ALEXNET_EALIGN,
+             "%s: a pointer is not aligned to its elements", who);
+  hipStream_t st = (hipStream_t)stream;
+  if (rows == 0) return fc_zero(d_dw, (size_t)in * out, d_db, out, st);
+  AX_REQUIRE(d_dy, ALEXNET_EINVAL, "%s: null argument", who);
+  AX_TRY(check_checkpoint(x, who));
+  AX_REQUIRE(ld_dy >= out, ALEXNET_ESHAPE, "%s: row stride %ld is under %d columns", who, (long)ld_dy, out);
+  const FcPlan p = fc_plan(rows, in, out, type);
+  if (p.ws) {
+    AX_REQUIRE(workspace_bytes >= p.ws && d_workspace, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who,
+               d_workspace ? workspace_bytes : (size_t)0, p.ws);
+    AX_REQUIRE((uintptr_t)d_workspace % 256 == 0, ALEXNET_EALIGN, "%s: workspace is not 256-byte aligned", who);
+  }
+  FcArgs a = {};
+  a.codes = (const uint8_t*)x->d_codes;
+  a.scales = (const uint8_t*)x->d_scales;
+  a.dy = d_dy;
+  a.ld_dy = ld_dy;
+  a.rows = rows;
+  a.in = in;
+  a.out = out;
+  a.nb = ceil_div(in, kCodeBlock);
+  a.gm = p.gm;
+  a.gn = p.gn;
+  a.slices = p.slices;
+  a.steps = p.steps;
+  const bool split = p.slices > 1;
+  float* const slices_db = split ? (float*)d_workspace + (size_t)p.slices * p.slab : nullptr;
+  a.dw = split ? (float*)d_workspace : d_dw;
+  a.dw_slab = split ? (long)p.slab : 0;
+  a.db = !d_db ? nullptr : split ? slices_db : d_db;
+  {
+    KernelScope ks("checkpoint_weight", 2.0 * rows * in * out,
+                   (double)rows * (in + out * type_size(type)) + 4.0 * in * out, st);
+    AX_TRY(type == ALEXNET_TYPE_FP32   ? fc_launch_code<float>(a, x->code, p, st)
+           : type == ALEXNET_TYPE_BF16 ? fc_launch_code<__bf16>(a, x->code, p, st)
+                                       : fc_launch_code<_Float16>(a, x->code, p, st));
+  }
+  if (!split) return ALEXNET_OK;
+  const long n = (long)in * out;
+  const int dw_blocks = ceil_div(n, 1024), blocks = dw_blocks + (d_db ? ceil_div(out, 1024) : 0);
+  KernelScope ks("checkpoint_weight_sum", 0, 4.0 * n * (p.slices + 1), st);
+  hipLaunchKernelGGL(fc_slices_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a.dw, a.db, p.slices, n, (long)p.slab, out, d_dw,
+                     d_db, dw_blocks);
+  AX_LAUNCH_CHECK();
+  return ALEXNET_OK;
+}
+
+}  // extern "C"
