@@ -15,6 +15,7 @@
 // next rows are on their way while these are multiplied.  Rows are split over workgroups where dw alone has too few tiles; the
 // slices are added up in a second launch.
 #include <algorithm>
+#include <utility>
 
 #include "codes8.h"
 #include "kernels.h"
@@ -56,13 +57,32 @@ struct __attribute__((packed)) Loose {
   R v;
 };
 
+// The scales of a wave's eight rows come one to a lane, where a row of sixteen lanes holds the scales of the blocks that its
+// own columns lie in: lane 2 i + b (NB = 4, two blocks to sixteen lanes) or i (one) that of row i.  Row I's for every lane:
+template <int I, int NB>
+__device__ __forceinline__ float row_scale(float s) {
+  int v = __builtin_bit_cast(int, s);
+  if constexpr (NB == 4) {
+    const int lo = __builtin_amdgcn_update_dpp(v, v, 0x150 + 2 * I, 0xf, 0x3, false);     // lane 2 I to lanes 0..7
+    v = __builtin_amdgcn_update_dpp(lo, v, 0x150 + 2 * I + 1, 0xf, 0xc, false);  // lane 2 I + 1 to lanes 8..15
+  } else {
+    v = __builtin_amdgcn_update_dpp(v, v, 0x150 + I, 0xf, 0xf, false);
+  }
+  return __builtin_bit_cast(float, v);
+}
+template <int CODE, int NB, int... I>
+__device__ __forceinline__ void widen_rows(const uint32_t* codes, float s, float (*x)[4], std::integer_sequence<int, I...>) {
+  (codes_to_float4<CODE>(codes[I], row_scale<I, NB>(s), x[I]), ...);
+}
+
 template <typename T, int CODE, int NA, int NB>
 __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
   constexpr int TERMS = terms<T>();
   typedef T RowA __attribute__((ext_vector_type(NA)));
   __shared__ Unit sa[2][TERMS][4][64 * NA];
   __shared__ Unit sb[2][4][64 * NB];
-  const int t = threadIdx.x, oct = t >> 6, g = t & 63, lane = t & 63, wave = t >> 6;
+  // a wave's rows are the same for its lanes: row addresses are scalars, lanes add their column
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), oct = wave, lane = t & 63, g = lane;
   // Workgroups go to the eight XCDs in turn: those of one XCD, which share an L2, walk the tiles of one slice of the rows
   const int tiles = a.gm * a.gn, total = tiles * a.slices, q8 = total >> 3, r8 = total & 7, xcd = blockIdx.x & 7;
   const int id = xcd * q8 + min(xcd, r8) + ((int)blockIdx.x >> 3);
@@ -73,79 +93,112 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
   const T* const dy = (const T*)a.dy + first * a.ld_dy;
   const uint8_t* const codes = a.codes + first * a.in;
   const uint8_t* const scales = a.scales + first * a.nb;
-  const int ca = m0 + NA * g, cb = n0 + NB * g;
-  const bool inner_a = m0 + 64 * NA <= a.out, inner_b = n0 + 64 * NB <= a.in;
+  // First of this thread's columns.  At the edge the last whole NA (NB) columns, read in bounds: the loops know no edge.
+  const int ca = min(m0 + NA * g, a.out - NA), cb = min(n0 + NB * g, a.in - NB);
+  const int block = (n0 + NB * (lane & ~15)) / kCodeBlock + (NB == 4 ? lane & 1 : 0), scale_row = NB == 4 ? (lane & 15) / 2 : lane & 7;
 
-  T va[8][NA];
-  uint32_t vb[8];
-  uint32_t sc[8];
-  // Rows past the end and columns past the edge repeat the last ones: read in bounds, rows zeroed below, columns never stored.
-  auto load = [&](int step) {
+  struct Rows {
+    T a[8][NA];
+    uint32_t b[8], s;
+  };
+  const uint32_t off_a = (uint32_t)ca * sizeof(T), off_b = (uint32_t)cb;
+  const uint32_t off_s = (uint32_t)(scale_row * a.nb + min(block, a.nb - 1));
+  // The first step takes the rows that are no whole step, those after it 32 each.
+  const int odd = rows - (steps - 1) * kStep;
+  const char* pa = (const char*)dy + (long)oct * 8 * a.ld_dy * (long)sizeof(T);
+  const uint8_t *pb = codes + (long)oct * 8 * a.in, *ps = scales + (long)oct * 8 * a.nb;
+  const long row_a = a.ld_dy * (long)sizeof(T);
+  // WHOLE: a step that is; else rows past its end repeat the last one, read in bounds and zeroed below
+  auto load = [&](Rows& v, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    // (opaque here, so that a load is one instruction with a scalar base and this offset)
+    uint32_t oa = off_a, ob = off_b, os = off_s;
+    asm volatile("" : "+v"(oa), "+v"(ob), "+v"(os));
+    const int last = WHOLE ? 7 : odd - 1 - oct * 8;  // of the patch; below zero: none of it
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const long r = min(step * kStep + oct * 8 + i, rows - 1);
-      const T* const pa = dy + r * a.ld_dy;
-      if (inner_a) {
-        if constexpr (NA == 1) {
-          va[i][0] = pa[ca];
-        } else {
-          const RowA w = reinterpret_cast<const Loose<RowA>*>(pa + ca)->v;
-#pragma unroll
-          for (int e = 0; e < NA; ++e) va[i][e] = w[e];
-        }
+      const int r = WHOLE ? i : min(i, last);
+      const char* const qa = pa + r * row_a;
+      if constexpr (NA == 1) {
+        v.a[i][0] = *(const T*)(qa + oa);
       } else {
+        const RowA w = reinterpret_cast<const Loose<RowA>*>(qa + oa)->v;
 #pragma unroll
-        for (int e = 0; e < NA; ++e) va[i][e] = pa[min(ca + e, a.out - 1)];
+        for (int e = 0; e < NA; ++e) v.a[i][e] = w[e];
       }
-      const uint8_t* const pb = codes + r * a.in;
-      if (inner_b) {
-        if constexpr (NB == 4)
-          vb[i] = reinterpret_cast<const Loose<uint32_t>*>(pb + cb)->v;
-        else
-          vb[i] = reinterpret_cast<const Loose<uint16_t>*>(pb + cb)->v;
-      } else {
-        vb[i] = 0;
-#pragma unroll
-        for (int e = 0; e < NB; ++e) vb[i] |= (uint32_t)pb[min(cb + e, a.in - 1)] << 8 * e;
-      }
-      sc[i] = scales[r * a.nb + min(cb, a.in - 1) / kCodeBlock];
+      const uint8_t* const qb = pb + (long)r * a.in;
+      if constexpr (NB == 4)
+        v.b[i] = reinterpret_cast<const Loose<uint32_t>*>(qb + ob)->v;
+      else if constexpr (NB == 2)
+        v.b[i] = reinterpret_cast<const Loose<uint16_t>*>(qb + ob)->v;
+      else
+        v.b[i] = qb[ob];
     }
+    if constexpr (WHOLE)
+      v.s = ps[os];
+    else
+      v.s = ps[(long)min(scale_row, last) * a.nb + min(block, a.nb - 1)];
+    const int next = WHOLE ? kStep : odd;
+    pa += next * row_a;
+    pb += (long)next * a.in;
+    ps += (long)next * a.nb;
+    // the compiler would put the loads off to behind the products, whose time they need
+    __builtin_amdgcn_sched_barrier(0);
   };
   float sum[NA];
 #pragma unroll
   for (int e = 0; e < NA; ++e) sum[e] = 0.f;
-  auto put = [&](int step, int stage) {
-    const int left = rows - step * kStep - oct * 8;  // rows of the patch that there are
+  auto put = [&](const Rows& v, int stage, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    const int left = odd - oct * 8;  // rows of the first step's patch
     float f[8][NA];
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
+      for (int e = 0; e < NA; ++e) f[i][e] = (float)v.a[i][e];
+    if (!WHOLE) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < NA; ++e) f[i][e] = i < left ? f[i][e] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
       for (int e = 0; e < NA; ++e) {
-        f[i][e] = (float)va[i][e];
-        if (left < 8) f[i][e] = i < left ? f[i][e] : 0.f;
         sum[e] += f[i][e];
         if (TERMS > 1) most = fmaxf(most, fabsf(f[i][e]));
       }
-    const bool endless = TERMS > 1 && most == __builtin_inff();  // infinities leave no rest: inf - inf is not a number
+    const bool endless = TERMS > 1 && __any(most == __builtin_inff());  // infinities leave no rest: inf - inf is not a number
 #pragma unroll
-    for (int term = 0; term < TERMS; ++term)
+    for (int term = 0; term < TERMS; ++term) {
 #pragma unroll
       for (int e = 0; e < NA; ++e) {
         Unit u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = upper_halves(f[2 * i][e], f[2 * i + 1][e]);
         sa[stage][term][oct][e * 64 + g] = u;
-        if (term + 1 < TERMS) {
+      }
+      if (term + 1 < TERMS) {
+        if (endless) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[i][e] = endless && fabsf(f[i][e]) == __builtin_inff() ? 0.f : f[i][e] - upper(f[i][e]);
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < NA; ++e) f[i][e] = fabsf(f[i][e]) == __builtin_inff() ? 0.f : f[i][e] - upper(f[i][e]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < NA; ++e) f[i][e] -= upper(f[i][e]);
         }
       }
+    }
     float x[8][4];
+    widen_rows<CODE, NB>(v.b, code_scale(v.s), x, std::make_integer_sequence<int, 8>());
+    if (!WHOLE) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      codes_to_float4<CODE>(vb[i], code_scale(sc[i]), x[i]);
-      if (left < 8)
+      for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int e = 0; e < NB; ++e) x[i][e] = i < left ? x[i][e] : 0.f;
     }
@@ -166,12 +219,7 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[j][k][r] = 0.f;
   const int wm = (wave >> 1) * 32 + (lane & 31), wn = (wave & 1) * 32 + (lane & 31), half = lane >> 5;
-  load(0);
-  put(0, 0);
-  for (int step = 0; step < steps; ++step) {
-    const int stage = step & 1;
-    __syncthreads();
-    if (step + 1 < steps) load(step + 1);
+  auto multiply = [&](int stage) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       Frag b[NB];
@@ -186,38 +234,71 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
           for (int k = 0; k < NB; ++k) acc[j][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, b[k], acc[j][k], 0, 0, 0);
         }
     }
-    if (step + 1 < steps) put(step + 1, stage ^ 1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr std::true_type whole{};
+  constexpr std::false_type part{};
+  Rows u;
+  load(u, part);
+  if constexpr (NB == 4) {  // the products of a step cover the next one's loads
+    put(u, 0, part);
+    for (int step = 0;; ++step) {
+      __syncthreads();
+      if (step + 1 < steps) load(u, whole);
+      multiply(step & 1);
+      if (step + 1 >= steps) break;
+      put(u, ~step & 1, whole);
+    }
+  } else {  // two steps of loads in flight
+    Rows v;
+    if (steps > 1) load(v, whole);
+    put(u, 0, part);
+    for (int step = 0;; step += 2) {
+      __syncthreads();
+      if (step + 2 < steps) load(u, whole);
+      multiply(0);
+      if (step + 1 >= steps) break;
+      put(v, 1, whole);
+      __syncthreads();
+      if (step + 3 < steps) load(v, whole);
+      multiply(1);
+      if (step + 2 >= steps) break;
+      put(u, 0, whole);
+    }
   }
 
   float* const dw = a.dw + slice * a.dw_slab;
+  // Lanes past the edge store nothing; the one across it the columns that its neighbour has not.
   const int ci = n0 + NB * wn;
 #pragma unroll
-  for (int j = 0; j < NA; ++j)
+  for (int r = 0; r < 16; ++r) {
+    const int o = m0 + NA * ((wave >> 1) * 32 + 8 * (r / 4) + 4 * half + r % 4);
+    if (o >= a.out) continue;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int o = m0 + NA * ((wave >> 1) * 32 + 8 * (r / 4) + 4 * half + r % 4) + j;
-      if (o >= a.out) continue;
-      float* const p = dw + (long)o * a.in + ci;
-      if (inner_b) {
+    for (int j = 0; j < NA; ++j) {
+      float* const p = dw + (long)(min(o, a.out - NA) + j) * a.in;
+      if (ci + NB <= a.in) {
         typedef float RowB __attribute__((ext_vector_type(NB)));
         RowB w;
 #pragma unroll
         for (int k = 0; k < NB; ++k) w[k] = acc[j][k][r];
-        reinterpret_cast<Loose<RowB>*>(p)->v = w;
-      } else {
+        reinterpret_cast<Loose<RowB>*>(p + ci)->v = w;
+      } else if (ci < a.in) {
 #pragma unroll
-        for (int k = 0; k < NB; ++k)
-          if (ci + k < a.in) p[k] = acc[j][k][r];
+        for (int k = 1; k < NB; ++k)
+          if (a.in - NB + k >= ci) p[a.in - NB + k] = acc[j][k][r];
       }
     }
+  }
   if (a.db && tn == 0) {
     __syncthreads();
-    float* const part = reinterpret_cast<float*>(sa);
+    float* const sums = reinterpret_cast<float*>(sa);
 #pragma unroll
-    for (int e = 0; e < NA; ++e) part[oct * 64 * NA + g * NA + e] = sum[e];
+    for (int e = 0; e < NA; ++e) sums[oct * 64 * NA + g * NA + e] = sum[e];
     __syncthreads();
-    if (t < 64 * NA && m0 + t < a.out)
-      a.db[(long)slice * a.out + m0 + t] = (part[t] + part[64 * NA + t]) + (part[2 * 64 * NA + t] + part[3 * 64 * NA + t]);
+    if (t < 64 * NA && m0 + t / NA * NA < a.out)
+      a.db[(long)slice * a.out + min(m0 + t / NA * NA, a.out - NA) + t % NA] =
+          (sums[t] + sums[64 * NA + t]) + (sums[2 * 64 * NA + t] + sums[3 * 64 * NA + t]);
   }
 }
 
@@ -262,10 +343,12 @@ static FcPlan fc_plan(long rows, int in, int out, int type) {
   FcPlan best = {};
   double least = 1e30;
   const int terms = type == ALEXNET_TYPE_FP32 ? 3 : type == ALEXNET_TYPE_FP16 ? 2 : 1;
-  for (int wide = 0; wide < 2; ++wide) {
+  for (int shape = 0; shape < 3; ++shape) {
     FcPlan p = {};
-    p.na = wide ? 2 : 1;
-    p.nb = wide ? 4 : 2;
+    p.na = shape == 2 ? 2 : 1;
+    p.nb = 1 << shape;
+    if (out < p.na || in < p.nb) continue;
+    const bool wide = shape == 2;
     p.gm = ceil_div(out, 64 * p.na);
     p.gn = ceil_div(in, 64 * p.nb);
     const long tiles = (long)p.gm * p.gn, steps = std::max<long>(1, (rows + kStep - 1) / kStep);
@@ -293,8 +376,10 @@ static int fc_launch(const FcArgs& a, const FcPlan& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.gm * p.gn * p.slices)), block(256);
   if (p.na == 2)
     hipLaunchKernelGGL((fc_weight_kernel<T, CODE, 2, 4>), grid, block, 0, st, a);
-  else
+  else if (p.nb == 2)
     hipLaunchKernelGGL((fc_weight_kernel<T, CODE, 1, 2>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((fc_weight_kernel<T, CODE, 1, 1>), grid, block, 0, st, a);
   AX_LAUNCH_CHECK();
   return ALEXNET_OK;
 }
