@@ -47,32 +47,57 @@ __device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
 }
 __device__ __forceinline__ float upper(float v) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xffff0000u); }
 
-typedef uint32_t Unit __attribute__((ext_vector_type(4)));
-typedef __bf16 Frag __attribute__((ext_vector_type(8)));
-typedef float Acc __attribute__((ext_vector_type(16)));
-
 // a type that may be read or written at any address (the hardware takes vector accesses at any)
 template <typename R>
 struct __attribute__((packed)) Loose {
   R v;
 };
 
+typedef uint32_t Unit __attribute__((ext_vector_type(4)));
+typedef __bf16 Frag __attribute__((ext_vector_type(8)));
+typedef float Acc __attribute__((ext_vector_type(16)));
+
 // The scales of a wave's eight rows come one to a lane, where a row of sixteen lanes holds the scales of the blocks that its
 // own columns lie in: lane 2 i + b (NB = 4, two blocks to sixteen lanes) or i (one) that of row i.  Row I's for every lane:
 template <int I, int NB>
 __device__ __forceinline__ float row_scale(float s) {
-  int v = __builtin_bit_cast(int, s);
+  const int v = __builtin_bit_cast(int, s);
   if constexpr (NB == 4) {
-    const int lo = __builtin_amdgcn_update_dpp(v, v, 0x150 + 2 * I, 0xf, 0x3, false);     // lane 2 I to lanes 0..7
-    v = __builtin_amdgcn_update_dpp(lo, v, 0x150 + 2 * I + 1, 0xf, 0xc, false);  // lane 2 I + 1 to lanes 8..15
+    const int lo = __builtin_amdgcn_mov_dpp(v, 0x150 + 2 * I, 0xf, 0x3, false);                              // lanes 0..7
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(lo, v, 0x150 + 2 * I + 1, 0xf, 0xc, false));  // lanes 8..15
   } else {
-    v = __builtin_amdgcn_update_dpp(v, v, 0x150 + I, 0xf, 0xf, false);
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(v, 0x150 + I, 0xf, 0xf, false));
   }
-  return __builtin_bit_cast(float, v);
 }
-template <int CODE, int NB, int... I>
-__device__ __forceinline__ void widen_rows(const uint32_t* codes, float s, float (*x)[4], std::integer_sequence<int, I...>) {
-  (codes_to_float4<CODE>(codes[I], row_scale<I, NB>(s), x[I]), ...);
+template <int NB, int... I>
+__device__ __forceinline__ void row_scales(float s, float* out, std::integer_sequence<int, I...>) {
+  ((out[I] = row_scale<I, NB>(s)), ...);
+}
+// eight rows of NB codes to one unit per column
+template <int CODE, int NB>
+__device__ __forceinline__ void codes_to_units(const uint32_t* w, const float* s, Unit* u) {
+  if constexpr (CODE == ALEXNET_CODE_INT8) {
+#pragma unroll
+    for (int e = 0; e < NB; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        u[e][i] = upper_halves((float)(int8_t)(w[2 * i] >> 8 * e) * s[2 * i], (float)(int8_t)(w[2 * i + 1] >> 8 * e) * s[2 * i + 1]);
+  } else {
+    // two columns to an instruction, already bf16
+    typedef __bf16 Two __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < NB; e += 2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Two lo = e ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], s[2 * i], true)
+                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], s[2 * i], false);
+        const Two hi = e ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], s[2 * i + 1], true)
+                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], s[2 * i + 1], false);
+        const uint32_t l = __builtin_bit_cast(uint32_t, lo), h = __builtin_bit_cast(uint32_t, hi);
+        u[e][i] = __builtin_amdgcn_perm(h, l, 0x05040100u);
+        if (e + 1 < NB) u[e + 1][i] = __builtin_amdgcn_perm(h, l, 0x07060302u);
+      }
+  }
 }
 
 template <typename T, int CODE, int NA, int NB>
@@ -105,8 +130,8 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
   const uint32_t off_s = (uint32_t)(scale_row * a.nb + min(block, a.nb - 1));
   // The first step takes the rows that are no whole step, those after it 32 each.
   const int odd = rows - (steps - 1) * kStep;
-  const char* pa = (const char*)dy + (long)oct * 8 * a.ld_dy * (long)sizeof(T);
-  const uint8_t *pb = codes + (long)oct * 8 * a.in, *ps = scales + (long)oct * 8 * a.nb;
+  const char* pa;
+  const uint8_t *pb, *ps;
   const long row_a = a.ld_dy * (long)sizeof(T);
   // WHOLE: a step that is; else rows past its end repeat the last one, read in bounds and zeroed below
   auto load = [&](Rows& v, auto whole) {
@@ -146,78 +171,49 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
     __builtin_amdgcn_sched_barrier(0);
   };
   float sum[NA];
-#pragma unroll
-  for (int e = 0; e < NA; ++e) sum[e] = 0.f;
-  auto put = [&](const Rows& v, int stage, auto whole) {
-    constexpr bool WHOLE = decltype(whole)::value;
+  // FIX: infinities leave no rest (inf - inf is not a number)
+  auto put = [&](const Rows& v, int stage, auto whole, auto fix) {
+    constexpr bool WHOLE = decltype(whole)::value, FIX = decltype(fix)::value;
     const int left = odd - oct * 8;  // rows of the first step's patch
-    float f[8][NA];
-    float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int e = 0; e < NA; ++e) {
+      float f[8];
 #pragma unroll
-      for (int e = 0; e < NA; ++e) f[i][e] = (float)v.a[i][e];
-    if (!WHOLE) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < NA; ++e) f[i][e] = i < left ? f[i][e] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < NA; ++e) {
-        sum[e] += f[i][e];
-        if (TERMS > 1) most = fmaxf(most, fabsf(f[i][e]));
+      for (int i = 0; i < 8; ++i) {
+        f[i] = (float)v.a[i][e];
+        if (!WHOLE) f[i] = i < left ? f[i] : 0.f;
+        sum[e] += f[i];
       }
-    const bool endless = TERMS > 1 && __any(most == __builtin_inff());  // infinities leave no rest: inf - inf is not a number
 #pragma unroll
-    for (int term = 0; term < TERMS; ++term) {
-#pragma unroll
-      for (int e = 0; e < NA; ++e) {
+      for (int term = 0; term < TERMS; ++term) {
         Unit u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = upper_halves(f[2 * i][e], f[2 * i + 1][e]);
+        for (int i = 0; i < 4; ++i) u[i] = upper_halves(f[2 * i], f[2 * i + 1]);
         sa[stage][term][oct][e * 64 + g] = u;
-      }
-      if (term + 1 < TERMS) {
-        if (endless) {
+        if (term + 1 < TERMS) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int e = 0; e < NA; ++e) f[i][e] = fabsf(f[i][e]) == __builtin_inff() ? 0.f : f[i][e] - upper(f[i][e]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int e = 0; e < NA; ++e) f[i][e] -= upper(f[i][e]);
+          for (int i = 0; i < 8; ++i) f[i] = FIX && fabsf(f[i]) == __builtin_inff() ? 0.f : f[i] - upper(f[i]);
         }
       }
     }
-    float x[8][4];
-    widen_rows<CODE, NB>(v.b, code_scale(v.s), x, std::make_integer_sequence<int, 8>());
-    if (!WHOLE) {
+    float s[8];
+    row_scales<NB>(code_scale(v.s), s, std::make_integer_sequence<int, 8>());
+    uint32_t w[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < NB; ++e) x[i][e] = i < left ? x[i][e] : 0.f;
+    for (int i = 0; i < 8; ++i) {
+      w[i] = v.b[i];
+      if (!WHOLE) {
+        w[i] = i < left ? w[i] : 0u;
+        s[i] = i < left ? s[i] : 1.f;
+      }
     }
+    Unit u[NB];
+    codes_to_units<CODE, NB>(w, s, u);
 #pragma unroll
-    for (int e = 0; e < NB; ++e) {
-      Unit u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) u[i] = upper_halves(x[2 * i][e], x[2 * i + 1][e]);
-      sb[stage][oct][e * 64 + g] = u;
-    }
+    for (int e = 0; e < NB; ++e) sb[stage][oct][e * 64 + g] = u[e];
   };
 
   Acc acc[NA][NB];
-#pragma unroll
-  for (int j = 0; j < NA; ++j)
-#pragma unroll
-    for (int k = 0; k < NB; ++k)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[j][k][r] = 0.f;
   const int wm = (wave >> 1) * 32 + (lane & 31), wn = (wave & 1) * 32 + (lane & 31), half = lane >> 5;
   auto multiply = [&](int stage) {
 #pragma unroll
@@ -234,37 +230,80 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
           for (int k = 0; k < NB; ++k) acc[j][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, b[k], acc[j][k], 0, 0, 0);
         }
     }
-    __builtin_amdgcn_sched_barrier(0);
   };
-  constexpr std::true_type whole{};
-  constexpr std::false_type part{};
-  Rows u;
-  load(u, part);
-  if constexpr (NB == 4) {  // the products of a step cover the next one's loads
-    put(u, 0, part);
-    for (int step = 0;; ++step) {
-      __syncthreads();
-      if (step + 1 < steps) load(u, whole);
-      multiply(step & 1);
-      if (step + 1 >= steps) break;
-      put(u, ~step & 1, whole);
+  auto mix = [&]() {
+#pragma unroll
+    for (int i = 0; i < 2 * TERMS * NA * NB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+      __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // vector instructions
+      __builtin_amdgcn_sched_group_barrier(0x300, 1, 0);  // an access to LDS
     }
-  } else {  // two steps of loads in flight
-    Rows v;
-    if (steps > 1) load(v, whole);
-    put(u, 0, part);
-    for (int step = 0;; step += 2) {
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  // Two steps of loads in flight; a step's values go to LDS between the products of the step before, which leave the vector
+  // unit idle most of the time.
+  auto run = [&](auto fix) {
+#pragma unroll
+    for (int j = 0; j < NA; ++j)
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[j][k][r] = 0.f;
+#pragma unroll
+    for (int e = 0; e < NA; ++e) sum[e] = 0.f;
+    pa = (const char*)dy + (long)oct * 8 * row_a;
+    pb = codes + (long)oct * 8 * a.in;
+    ps = scales + (long)oct * 8 * a.nb;
+    Rows u, v;
+    load(u, no);
+    if (steps > 1) load(v, yes);
+    put(u, 0, no, fix);
+    int step = 0;
+    for (; step + 3 < steps; step += 2) {
       __syncthreads();
-      if (step + 2 < steps) load(u, whole);
+      load(u, yes);
       multiply(0);
-      if (step + 1 >= steps) break;
-      put(v, 1, whole);
+      put(v, 1, yes, fix);
+      mix();
       __syncthreads();
-      if (step + 3 < steps) load(v, whole);
+      load(v, yes);
       multiply(1);
-      if (step + 2 >= steps) break;
-      put(u, 0, whole);
+      put(u, 0, yes, fix);
+      mix();
     }
+    __syncthreads();  // one to three steps are left, the first in LDS, the second in v
+    if (step + 2 < steps) load(u, yes);
+    multiply(0);
+    if (step + 1 < steps) {
+      put(v, 1, yes, fix);
+      __syncthreads();
+      multiply(1);
+    }
+    if (step + 2 < steps) {
+      put(u, 0, yes, fix);
+      __syncthreads();
+      multiply(0);
+    }
+  };
+  run(no);
+  if constexpr (TERMS > 1) {
+    // a rest of an infinity has made a NaN: again, with a look at every value
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < NA; ++j)
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bad |= acc[j][k][r] != acc[j][k][r];
+    int* const any = reinterpret_cast<int*>(sa);  // not __syncthreads_or: its LDS would leave room for one workgroup only
+    __syncthreads();
+    const int mine = __any(bad);
+    if (lane == 0) any[wave] = mine;
+    __syncthreads();
+    const bool again = any[0] | any[1] | any[2] | any[3];
+    __syncthreads();
+    if (again) run(yes);
   }
 
   float* const dw = a.dw + slice * a.dw_slab;
@@ -337,29 +376,35 @@ struct FcPlan {
   int gm, gn, slices, steps;
   size_t slab, ws;  // floats of a slice's dw; bytes of scratch
 };
-// Workgroups run two to a compute unit.  A workgroup costs its steps and a start; more slices shorten that and lengthen the
-// adding up, which writes and reads dw once per slice.
+// The tile and the number of slices that a model of the measured times makes cheapest.  A step of a workgroup that has a
+// compute unit to itself takes kAloneUs microseconds, one among as many as fit kStepUs of the unit's time; slices are written
+// and read once more each.  256 x 9216 x 4096 fp32 (few rows, large dw): 128 x 256 tiles 75 us, 64 x 128 ones 76, 64 x 64 about
+// 110, two slices 179; 43264 x 384 x 384 bf16: 64 x 128 tiles in 56 slices 38 us, in 24 slices 45, in 12 slices 78, 128 x 256
+// tiles in 86 slices 39, 64 x 64 ones in 64 slices 56.
 static FcPlan fc_plan(long rows, int in, int out, int type) {
+  static const double kStepUs[3][3] = {{0.17, 0.26, 0.34}, {0.22, 0.39, 0.57}, {0.61, 0.95, 1.3}};  // [tile][terms - 1]
+  static const double kAloneUs[3][3] = {{0.44, 0.52, 0.6}, {0.57, 0.73, 0.89}, {1.03, 1.48, 1.92}};
+  static const int kFit[3] = {4, 4, 2};  // workgroups on a compute unit
   FcPlan best = {};
-  double least = 1e30;
+  double least = 1e300;
   const int terms = type == ALEXNET_TYPE_FP32 ? 3 : type == ALEXNET_TYPE_FP16 ? 2 : 1;
+  const long steps = (rows + kStep - 1) / kStep;
+  const double bytes = 4.0 * in * out;
   for (int shape = 0; shape < 3; ++shape) {
     FcPlan p = {};
     p.na = shape == 2 ? 2 : 1;
     p.nb = 1 << shape;
     if (out < p.na || in < p.nb) continue;
-    const bool wide = shape == 2;
     p.gm = ceil_div(out, 64 * p.na);
     p.gn = ceil_div(in, 64 * p.nb);
-    const long tiles = (long)p.gm * p.gn, steps = std::max<long>(1, (rows + kStep - 1) / kStep);
-    const int least_slices = (int)((rows + kSliceRows - 1) / kSliceRows);
-    for (int s = std::max(1, least_slices); s <= std::min<long>(steps, kMaxSlices); s += s < 16 ? 1 : s / 8) {
+    const double tiles = (double)p.gm * p.gn, us = kStepUs[shape][terms - 1], alone = kAloneUs[shape][terms - 1];
+    const int fit = kFit[shape];
+    for (long s = std::max<long>(1, (rows + kSliceRows - 1) / kSliceRows); s <= std::min<long>(steps, kMaxSlices); s += 1 + s / 8) {
       p.steps = (int)((steps + s - 1) / s);
       p.slices = (int)((steps + p.steps - 1) / p.steps);
-      const double step = wide ? 0.35 + 0.25 * terms : 0.2 + 0.07 * terms;  // microseconds
-      const double rounds = std::max(1.0, (double)tiles * p.slices / 512);
-      const double bytes = (double)in * out * 4;
-      const double cost = std::ceil(rounds) * (p.steps * step + 2.0) + (p.slices > 1 ? 4.0 + p.slices * bytes * 2 / 4e6 : bytes / 4e6);
+      const double units = tiles * p.slices / 256, full = std::floor(units / fit), rest = std::ceil(units - full * fit);
+      const double each = full * std::max(alone, us * fit) + (rest > 0 ? std::max(alone, us * rest) : 0.0);
+      const double cost = p.steps * each + p.slices * bytes / 10.8e6 + (p.slices > 1 ? 5.6 + p.slices * bytes / 8.9e6 : 0.0);
       if (cost < least) {
         least = cost;
         best = p;
