@@ -342,8 +342,7 @@ int alexnet_softmax_xent_static(const float* d_logits, const int32_t* d_labels, 
  *
  * TYPE: elements of activations and their gradients; everything else
  * (statistics, gamma, beta and their gradients, sums) is float32.  Pointers are
- * aligned to their element; 16-byte aligned ones with pixel strides that are
- * multiples of 16 bytes are read and written 16 bytes at a time. */
+ * aligned to their element and no more. */
 #define ALEXNET_TYPE_FP32 0
 #define ALEXNET_TYPE_BF16 1
 #define ALEXNET_TYPE_FP16 2

@@ -26,25 +26,28 @@ __global__ void __launch_bounds__(256) pack_kernel(CodeArgs a) {
   if (r0 >= a.rpi) return;
   const long row0 = rb * a.rpi * kRows + r0;
   const bool has = v < a.colvecs;
+  const int col = min(v * V, a.cols - V), dup = v * V - col;  // the last vector repeats columns of the one before
   typename Pack<T, V>::Raw raw[kRows];
 #pragma unroll
   for (int u = 0; u < kRows; ++u) {
     const long row = row0 + (long)u * a.rpi;
-    if (has && row < a.rows) raw[u] = Pack<T, V>::load((const T*)a.x + row * a.ld + v * V);
+    if (has && row < a.rows) raw[u] = Pack<T, V>::load((const T*)a.x + row * a.ld + col);
   }
 #pragma unroll
   for (int u = 0; u < kRows; ++u) {
     const long row = row0 + (long)u * a.rpi;
     if (row >= a.rows) break;  // all lanes of a block alike
-    float f[V];
+    float f[V], own[V];
     if (has)
       Pack<T, V>::widen(raw[u], f);
     else
 #pragma unroll
       for (int i = 0; i < V; ++i) f[i] = 0.f;
-    const uint32_t s = scale_code<CODE>(block_max_bits<V>(f));
+#pragma unroll
+    for (int i = 0; i < V; ++i) own[i] = V > 1 && i < dup ? 0.f : f[i];
+    const uint32_t s = scale_code<CODE>(block_max_bits<V>(own));
     if (has) {
-      *reinterpret_cast<typename Codes<V>::Raw*>(a.codes + row * a.cols + v * V) = floats_to_codes<CODE, V>(f, s);
+      store_codes<CODE, V>(a.codes + row * a.cols + col, f, s, dup);
       if (v * V % kCodeBlock == 0) a.scales[row * a.nb + v * V / kCodeBlock] = (uint8_t)s;
     }
   }
@@ -56,14 +59,16 @@ __global__ void __launch_bounds__(256) unpack_kernel(CodeArgs a) {
   const int cb = blockIdx.x - rb * a.col_blocks, t = threadIdx.x, r0 = t / a.width, v = cb * a.width + t - r0 * a.width;
   if (r0 >= a.rpi || v >= a.colvecs) return;
   const long row0 = rb * a.rpi * kRows + r0;
+  const int col = min(v * V, a.cols - V), dup = v * V - col;  // the last vector repeats columns of the one before
   typename Codes<V>::Raw raw[kRows];
-  uint32_t s[kRows];
+  uint32_t s[kRows], s0[kRows];
 #pragma unroll
   for (int u = 0; u < kRows; ++u) {
     const long row = row0 + (long)u * a.rpi;
     if (row < a.rows) {
-      raw[u] = *reinterpret_cast<const typename Codes<V>::Raw*>(a.codes + row * a.cols + v * V);
+      raw[u] = Codes<V>::load(a.codes + row * a.cols + col);
       s[u] = a.scales[row * a.nb + v * V / kCodeBlock];
+      if (V > 1 && dup) s0[u] = a.scales[row * a.nb + col / kCodeBlock];
     }
   }
 #pragma unroll
@@ -72,14 +77,21 @@ __global__ void __launch_bounds__(256) unpack_kernel(CodeArgs a) {
     if (row >= a.rows) break;
     float f[V];
     codes_to_float<CODE, V>(raw[u], code_scale(s[u]), f);
-    Pack<T, V>::store((T*)a.out + row * a.ld + v * V, f);
+    if (V > 1 && dup) {
+      float g[V];
+      codes_to_float<CODE, V>(raw[u], code_scale(s0[u]), g);
+      const int first = kCodeBlock - col % kCodeBlock;  // columns of the block that col lies in
+#pragma unroll
+      for (int i = 0; i < V; ++i) f[i] = i < first ? g[i] : f[i];
+    }
+    Pack<T, V>::store((T*)a.out + row * a.ld + col, f);
   }
 }
 
 template <typename T, int V>
 static int pack_or_unpack(CodeArgs a, int code, bool pack, hipStream_t st) {
   constexpr int lanes = kCodeBlock / V;
-  a.colvecs = a.cols / V;
+  a.colvecs = ceil_div(a.cols, V);
   a.width = std::min(256, ceil_div(a.colvecs, lanes) * lanes);
   a.rpi = 256 / a.width;
   a.col_blocks = ceil_div(a.colvecs, a.width);
@@ -101,8 +113,7 @@ static int pack_or_unpack(CodeArgs a, int code, bool pack, hipStream_t st) {
 template <typename T>
 static int pack_or_unpack_type(const CodeArgs& a, int code, bool pack, hipStream_t st) {
   constexpr int V = 16 / sizeof(T);
-  const bool vec = a.cols % V == 0 && rows_vec_ok(pack ? a.x : a.out, a.ld, sizeof(T)) && (uintptr_t)a.codes % V == 0;
-  return vec ? pack_or_unpack<T, V>(a, code, pack, st) : pack_or_unpack<T, 1>(a, code, pack, st);
+  return a.cols >= V ? pack_or_unpack<T, V>(a, code, pack, st) : pack_or_unpack<T, 1>(a, code, pack, st);
 }
 static int checkpoint_call(const char* who, const alexnet_checkpoint_t* k, const void* x, void* out, int64_t ld, int type,
                            int64_t rows, int cols, void* stream) {

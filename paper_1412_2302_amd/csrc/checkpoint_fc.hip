@@ -47,12 +47,6 @@ __device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
 }
 __device__ __forceinline__ float upper(float v) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xffff0000u); }
 
-// a type that may be read or written at any address (the hardware takes vector accesses at any)
-template <typename R>
-struct __attribute__((packed)) Loose {
-  R v;
-};
-
 typedef uint32_t Unit __attribute__((ext_vector_type(4)));
 typedef __bf16 Frag __attribute__((ext_vector_type(8)));
 typedef float Acc __attribute__((ext_vector_type(16)));

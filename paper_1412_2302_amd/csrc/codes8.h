@@ -27,21 +27,26 @@ inline int check_checkpoint(const alexnet_checkpoint_t* k, const char* who) {
   return ALEXNET_OK;
 }
 inline bool type_ok(int type) { return type >= ALEXNET_TYPE_FP32 && type <= ALEXNET_TYPE_FP16; }
-// 16-byte accesses to rows at this stride
-inline bool rows_vec_ok(const void* p, long ld, size_t size) { return (uintptr_t)p % 16 == 0 && ld * (long)size % 16 == 0; }
+
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 inline size_t type_size(int type) { return type == ALEXNET_TYPE_FP32 ? 4 : 2; }
+
+// A type that may be read or written at any address: the hardware takes vector accesses at any
+template <typename R>
+struct __attribute__((packed)) Loose {
+  R v;
+};
 
 // V values of type T: one access of V * sizeof(T) bytes
 template <typename T, int V>
 struct Pack {
   typedef T Raw __attribute__((ext_vector_type(V)));
-  static __device__ __forceinline__ Raw load(const T* p) { return *reinterpret_cast<const Raw*>(p); }
+  static __device__ __forceinline__ Raw load(const T* p) { return reinterpret_cast<const Loose<Raw>*>(p)->v; }
   static __device__ __forceinline__ void store(T* p, const float* v) {
     Raw r;
 #pragma unroll
     for (int i = 0; i < V; ++i) r[i] = (T)v[i];  // nearest even
-    *reinterpret_cast<Raw*>(p) = r;
+    reinterpret_cast<Loose<Raw>*>(p)->v = r;
   }
   static __device__ __forceinline__ void widen(const Raw& r, float* v) {
 #pragma unroll
@@ -61,14 +66,17 @@ template <int V>
 struct Codes {
   static_assert(V == 4 || V == 8, "words of four codes");
   typedef uint32_t Raw __attribute__((ext_vector_type(V / 4)));
+  static __device__ __forceinline__ Raw load(const uint8_t* p) { return reinterpret_cast<const Loose<Raw>*>(p)->v; }
 };
 template <>
 struct Codes<4> {
   typedef uint32_t Raw;
+  static __device__ __forceinline__ Raw load(const uint8_t* p) { return reinterpret_cast<const Loose<Raw>*>(p)->v; }
 };
 template <>
 struct Codes<1> {
   typedef uint8_t Raw;
+  static __device__ __forceinline__ Raw load(const uint8_t* p) { return *p; }
 };
 
 __device__ __forceinline__ float code_scale(uint32_t s) {
@@ -165,6 +173,25 @@ __device__ __forceinline__ typename Codes<V>::Raw floats_to_codes(const float* v
     r = (uint8_t)(bad ? 0u : floats_to_codes4<CODE>(t, inv));
   }
   return r;
+}
+
+// stores them, but for the first `dup`
+template <int CODE, int V>
+__device__ __forceinline__ void store_codes(uint8_t* p, const float* v, uint32_t s, int dup) {
+  const typename Codes<V>::Raw r = floats_to_codes<CODE, V>(v, s);
+  if (V == 1 || dup == 0) {
+    reinterpret_cast<Loose<typename Codes<V>::Raw>*>(p)->v = r;
+  } else if constexpr (V > 1) {
+#pragma unroll
+    for (int i = 1; i < V; ++i) {
+      uint32_t w;
+      if constexpr (V == 4)
+        w = r;
+      else
+        w = r[i / 4];
+      if (i >= dup) p[i] = (uint8_t)(w >> 8 * (i % 4));
+    }
+  }
 }
 
 }  // namespace ax

@@ -1,107 +1,16 @@
-// Group normalisation with an activation over channel-last activations, forward and backward, with the input of the backward
-// pass either as it was or from its 8-bit checkpoint (codes8.h).
-//
-// A thread owns V consecutive channels (16 bytes where strides and alignment allow, else one value) and walks down pixels, so
-// that loads are coalesced and everything per channel -- gamma, beta, the group's statistics, running sums -- stays in
-// registers.  Groups need not match vectors: all sums are kept per channel and meet only where a group is added up.
+// Group normalisation with an activation over channel-last activations, forward and backward: the kernels for maps of any
+// size, and the entry points.  Maps whose groups fit a workgroup's registers go to group_norm_resident.hip, which reads its
+// inputs once; here a first launch sums over chunks of pixels, a second joins the chunks and a third reads the inputs again and
+// writes the result.
 #include <math.h>
 
 #include <algorithm>
 
-#include "codes8.h"
+#include "group_norm.h"
+#include "group_norm_resident.h"
 #include "kernels.h"
 
 namespace ax {
-
-// Where the values of a map come from: a tensor of the activation's type, or a checkpoint of one code
-enum { SRC_TENSOR = 0, SRC_INT8 = 1, SRC_E4M3 = 2 };
-constexpr int kKeepNone = -1;
-
-struct GnArgs {
-  const void* x;
-  long ld_x;
-  const uint8_t *codes, *scales;  // the checkpoint that is read (backward)
-  uint8_t *keep, *keep_scales;    // the one that is written (forward)
-  const void* dy;
-  long ld_dy;
-  void* out;  // y or dx
-  long ld_out;
-  const float *gamma, *beta, *mean, *rstd;  // mean, rstd [n][groups]
-  float *mean_out, *rstd_out, *dgamma, *dbeta;
-  int n, hw, c, groups, cpg, act, nb;  // nb: scales of a pixel
-  float eps;
-  // a launch over (column blocks, chunks of pixels, pictures) in one dimension
-  int colvecs, cols, rpi, col_blocks, chunk, chunks;  // cols: threads of a row (whole blocks of 32 where a checkpoint is written)
-  float *part, *stat;  // [n][chunks][2][c]; [n][groups][2]
-};
-
-struct Spot {  // a thread's place in such a launch
-  int n, p0, p1, row, v, chunk;
-  bool on, has;  // takes part; has channels of its own (a padded row has threads without)
-};
-__device__ __forceinline__ Spot spot(const GnArgs& a, int V) {
-  Spot s;
-  int b = blockIdx.x;
-  const int cb = b % a.col_blocks;
-  b /= a.col_blocks;
-  s.chunk = b % a.chunks;
-  s.n = b / a.chunks;
-  s.row = (int)threadIdx.x / a.cols;
-  s.v = cb * a.cols + (int)threadIdx.x - s.row * a.cols;
-  s.on = s.row < a.rpi;
-  s.has = s.on && s.v < a.colvecs;
-  s.p0 = s.chunk * a.chunk;
-  s.p1 = min(a.hw, s.p0 + a.chunk);
-  (void)V;
-  return s;
-}
-
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == ALEXNET_ACT_RELU) return z < 0.f ? 0.f : z;  // a NaN stays one
-  if (act == ALEXNET_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));  // one ulp each
-  return z;
-}
-
-// dy * act'(z) of one value.  A relu's gate within rounding of its border is decided in 64 bits: a gate that falls the other way
-// is an error as large as the gradient itself, and one value in some ten million is that near.
-__device__ __forceinline__ float gated(float dy, float x, float mean, float rstd, float gamma, float beta, int act) {
-  if (act == ALEXNET_ACT_NONE) return dy;
-  const float t = (x - mean) * (rstd * gamma), z = t + beta;
-  if (act == ALEXNET_ACT_RELU) {
-    bool open = z > 0.f;
-    if (fabsf(z) <= 5e-7f * fabsf(t)) open = ((double)x - mean) * rstd * gamma + beta > 0.0;
-    return open ? dy : 0.f;
-  }
-  const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z));
-  return dy * (s * __builtin_fmaf(z, 1.f - s, 1.f));
-}
-
-// V values of row `row` (picture * hw + pixel) of what a kernel reads as x
-template <typename T, int V, int SRC>
-struct Source {
-  static constexpr int code = SRC == SRC_E4M3 ? ALEXNET_CODE_E4M3 : ALEXNET_CODE_INT8;
-  struct Raw {
-    typename std::conditional<SRC == SRC_TENSOR, typename Pack<T, V>::Raw, typename Codes<V>::Raw>::type r;
-    uint8_t s;
-  };
-  static __device__ __forceinline__ Raw load(const GnArgs& a, long row, int v) {
-    Raw w;
-    if constexpr (SRC == SRC_TENSOR) {
-      w.r = Pack<T, V>::load((const T*)a.x + row * a.ld_x + v * V);
-      w.s = 0;
-    } else {
-      w.r = *reinterpret_cast<const typename Codes<V>::Raw*>(a.codes + row * a.c + v * V);
-      w.s = a.scales[row * a.nb + v * V / kCodeBlock];
-    }
-    return w;
-  }
-  static __device__ __forceinline__ void widen(const Raw& w, float* f) {
-    if constexpr (SRC == SRC_TENSOR)
-      Pack<T, V>::widen(w.r, f);
-    else
-      codes_to_float<code, V>(w.r, code_scale(w.s), f);
-  }
-};
 
 // ---- statistics -----------------------------------------------------------------
 constexpr int kUnroll = 4;  // pixels of a thread's loads in flight
@@ -111,7 +20,8 @@ constexpr int kUnroll = 4;  // pixels of a thread's loads in flight
 template <typename T, int V, int KEEP>
 __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
   __shared__ float sm[256 * V], sq[256 * V];
-  const Spot s = spot(a, V);
+  const Spot s = spot(a, blockIdx.x);
+  const Vec v = vec_of<V>(s.v, 0, a.c);
   float m[V], q[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) m[i] = q[i] = 0.f;
@@ -122,7 +32,7 @@ __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int pu = p + u * a.rpi;
-        if (s.has && pu < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + pu) * a.ld_x + s.v * V);
+        if (s.has && pu < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + pu) * a.ld_x + v.c);
       }
       const int nu = min(kUnroll, (s.p1 - p + a.rpi - 1) / a.rpi);
       float f[kUnroll][V];
@@ -138,12 +48,7 @@ __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
           if (u >= nu) break;  // the same for all lanes of a block: they share the row
-          const uint32_t sc = scale_code<KEEP>(block_max_bits<V>(f[u]));
-          const long row = (long)s.n * a.hw + p + u * a.rpi;
-          if (s.has) {
-            *reinterpret_cast<typename Codes<V>::Raw*>(a.keep + row * a.c + s.v * V) = floats_to_codes<KEEP, V>(f[u], sc);
-            if (s.v * V % kCodeBlock == 0) a.keep_scales[row * a.nb + s.v * V / kCodeBlock] = (uint8_t)sc;
-          }
+          keep_codes<V, KEEP>(a, (long)s.n * a.hw + p + u * a.rpi, v, s.has, f[u]);
         }
       }
       const float inv = 1.f / (float)nu, w = (float)nu / (float)(cnt + nu), wq = (float)cnt * w;
@@ -174,8 +79,10 @@ __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
   // one thread per channel joins the rows' pairs
   const int pixels = s.p1 - s.p0, width = a.cols * V;
   for (int j = threadIdx.x; j < width; j += 256) {
-    const int ch = ((int)blockIdx.x % a.col_blocks) * width + j;
-    if (ch >= a.c) continue;
+    const int at = ((int)blockIdx.x % a.col_blocks) * a.cols + j / V;
+    const Vec vj = vec_of<V>(at, 0, a.c);
+    if (at >= a.colvecs || j % V < vj.dup) continue;
+    const int ch = vj.c + j % V;
     float sum = 0.f;
     for (int r = 0; r < a.rpi; ++r) {
       const int k = r < pixels ? (pixels - r + a.rpi - 1) / a.rpi : 0;
@@ -200,43 +107,75 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// one wave per group joins its channels' and chunks' pairs
-__global__ void __launch_bounds__(64) gn_statistics_kernel(GnArgs a) {
-  const int n = blockIdx.x / a.groups, g = blockIdx.x - n * a.groups, lane = threadIdx.x;
+// the sum over a workgroup of 256; everyone gets it
+__device__ __forceinline__ float group_sum(float v, float* lds) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// A team of threads (a wave where a group has few terms, else the workgroup) joins the pairs of a group's channels and chunks,
+// four to a thread and trip so that their loads are in flight together.
+template <int TEAM>
+__global__ void __launch_bounds__(256) gn_statistics_kernel(GnArgs a) {
+  __shared__ float lds[4];
+  const int id = blockIdx.x * (256 / TEAM) + (int)threadIdx.x / TEAM, t = threadIdx.x % TEAM;
+  if (TEAM == 64 && id >= a.n * a.groups) return;
+  const auto total_of = [&](float v) { return TEAM == 64 ? wave_sum(v) : group_sum(v, lds); };
+  const int n = id / a.groups, g = id - n * a.groups;
   const float* const part = a.part + (long)n * a.chunks * 2 * a.c + (long)g * a.cpg;
   const float total = (float)a.hw * (float)a.cpg;
   const int terms = a.chunks * a.cpg;
   float sum = 0.f;
-  for (int i = lane; i < terms; i += 64) {
-    const int k = i / a.cpg, j = i - k * a.cpg;
-    const float cnt = (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk);
-    sum = __builtin_fmaf(cnt, part[(long)k * 2 * a.c + j], sum);
+  for (int i0 = t; i0 < terms; i0 += 4 * TEAM) {
+    float m[4], w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = min(i0 + TEAM * u, terms - 1), k = i / a.cpg, j = i - k * a.cpg;
+      m[u] = part[(long)k * 2 * a.c + j];
+      w[u] = i0 + TEAM * u < terms ? (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (w[u] != 0.f) sum = __builtin_fmaf(w[u], m[u], sum);
   }
-  const float mean = wave_sum(sum) / total;
+  const float mean = total_of(sum) / total;
   float sq = 0.f;
-  for (int i = lane; i < terms; i += 64) {
-    const int k = i / a.cpg, j = i - k * a.cpg;
-    const float cnt = (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk);
-    const float d = part[(long)k * 2 * a.c + j] - mean;
-    sq += __builtin_fmaf(d * d, cnt, part[(long)k * 2 * a.c + a.c + j]);
+  for (int i0 = t; i0 < terms; i0 += 4 * TEAM) {
+    float m[4], w[4], q[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = min(i0 + TEAM * u, terms - 1), k = i / a.cpg, j = i - k * a.cpg;
+      m[u] = part[(long)k * 2 * a.c + j];
+      q[u] = part[(long)k * 2 * a.c + a.c + j];
+      w[u] = i0 + TEAM * u < terms ? (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float d = m[u] - mean;
+      if (w[u] != 0.f) sq += __builtin_fmaf(d * d, w[u], q[u]);
+    }
   }
-  const float rstd = 1.f / sqrtf(wave_sum(sq) / total + a.eps);
-  if (lane == 0) {
-    a.stat[2 * blockIdx.x] = mean;
-    a.stat[2 * blockIdx.x + 1] = rstd;
-    if (a.mean_out) a.mean_out[blockIdx.x] = mean;
-    if (a.rstd_out) a.rstd_out[blockIdx.x] = rstd;
+  const float rstd = 1.f / sqrtf(total_of(sq) / total + a.eps);
+  if (t == 0) {
+    a.stat[2 * (long)id] = mean;
+    a.stat[2 * (long)id + 1] = rstd;
+    if (a.mean_out) a.mean_out[id] = mean;
+    if (a.rstd_out) a.rstd_out[id] = rstd;
   }
 }
 
 template <typename T, int V>
 __global__ void __launch_bounds__(256) gn_apply_kernel(GnArgs a) {
-  const Spot s = spot(a, V);
+  const Spot s = spot(a, gridDim.x - 1 - blockIdx.x);  // backwards: what the sums' launch read last is still cached
   if (!s.has) return;
+  const Vec v = vec_of<V>(s.v, 0, a.c);
   float mean[V], scale[V], beta[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int ch = s.v * V + i, g = s.n * a.groups + ch / a.cpg;
+    const int ch = v.c + i, g = s.n * a.groups + ch / a.cpg;
     mean[i] = a.stat[2 * g];
     scale[i] = a.stat[2 * g + 1] * (a.gamma ? a.gamma[ch] : 1.f);
     beta[i] = a.beta ? a.beta[ch] : 0.f;
@@ -245,7 +184,7 @@ __global__ void __launch_bounds__(256) gn_apply_kernel(GnArgs a) {
     typename Pack<T, V>::Raw r[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-      if (p + u * a.rpi < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_x + s.v * V);
+      if (p + u * a.rpi < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_x + v.c);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
       if (p + u * a.rpi < s.p1) {
@@ -253,7 +192,7 @@ __global__ void __launch_bounds__(256) gn_apply_kernel(GnArgs a) {
         Pack<T, V>::widen(r[u], f);
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] = activate(__builtin_fmaf(f[i] - mean[i], scale[i], beta[i]), a.act);
-        Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + s.v * V, f);
+        Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, f);
       }
   }
 }
@@ -263,7 +202,8 @@ __global__ void __launch_bounds__(256) gn_apply_kernel(GnArgs a) {
 template <typename T, int V, int SRC>
 __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
   __shared__ float sm[256 * V], sq[256 * V];
-  const Spot s = spot(a, V);
+  const Spot s = spot(a, blockIdx.x);
+  const Vec v = vec_of<V>(s.v, 0, a.c);
   float db[V], dg[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) db[i] = dg[i] = 0.f;
@@ -271,7 +211,7 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
     float mean[V], rstd[V], gamma[V], beta[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int ch = s.v * V + i, g = s.n * a.groups + ch / a.cpg;
+      const int ch = v.c + i, g = s.n * a.groups + ch / a.cpg;
       mean[i] = a.mean[g];
       rstd[i] = a.rstd[g];
       gamma[i] = a.gamma ? a.gamma[ch] : 1.f;
@@ -284,21 +224,23 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
       for (int u = 0; u < kUnroll; ++u)
         if (p + u * a.rpi < s.p1) {
           const long row = (long)s.n * a.hw + p + u * a.rpi;
-          x[u] = Source<T, V, SRC>::load(a, row, s.v);
-          d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + s.v * V);
+          Source<T, V, SRC>::load(a, row, v, x[u]);
+          d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
         }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
         if (p + u * a.rpi < s.p1) {
           float xf[V], df[V];
-          Source<T, V, SRC>::widen(x[u], xf);
+          Source<T, V, SRC>::widen(x[u], v, xf);
           Pack<T, V>::widen(d[u], df);
+          float hat[V];
+          gate<V>(df, xf, hat, mean, rstd, gamma, beta, a.act);
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float dz = gated(df[i], xf[i], mean[i], rstd[i], gamma[i], beta[i], a.act);
-            db[i] += dz;
-            dg[i] = __builtin_fmaf(dz, (xf[i] - mean[i]) * rstd[i], dg[i]);
+            db[i] += df[i];
+            dg[i] = __builtin_fmaf(df[i], hat[i], dg[i]);
           }
+          __builtin_amdgcn_sched_barrier(0);  // pixel by pixel: side by side they take twice the registers
         }
     }
   }
@@ -312,8 +254,10 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
   __syncthreads();
   const int width = a.cols * V;
   for (int j = threadIdx.x; j < width; j += 256) {
-    const int ch = ((int)blockIdx.x % a.col_blocks) * width + j;
-    if (ch >= a.c) continue;
+    const int at = ((int)blockIdx.x % a.col_blocks) * a.cols + j / V;
+    const Vec vj = vec_of<V>(at, 0, a.c);
+    if (at >= a.colvecs || j % V < vj.dup) continue;
+    const int ch = vj.c + j % V;
     float b = 0.f, g = 0.f;
     for (int r = 0; r < a.rpi; ++r) {
       b += sm[r * width + j];
@@ -325,17 +269,26 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
   }
 }
 
-// Workgroups [0, n * groups): the means that dx subtracts, mean(gamma dz) and mean(gamma dz xhat); then, sixteen channels a
-// workgroup, the sums over pictures and chunks that are dbeta and dgamma.
-__global__ void __launch_bounds__(256) gn_grad_totals_kernel(GnArgs a) {
-  __shared__ float sb[256], sg[256];
+// A group whose terms (chunks times channels) are few is a wave's work, not a workgroup's: 4096 groups of 48 terms took 21 us
+// with a workgroup of 1024 each.
+static bool few_terms(const GnArgs& a) { return (long)a.chunks * a.cpg <= 512; }
+
+// Workgroups [0, group_blocks): the means that dx subtracts, mean(gamma dz) and mean(gamma dz xhat), sixteen groups each where
+// SHORT (a wave to a group), else one; then, sixteen channels a workgroup, the sums over pictures and chunks that are dbeta and
+// dgamma.
+template <bool SHORT>
+__global__ void __launch_bounds__(1024) gn_grad_totals_kernel(GnArgs a, int group_blocks) {
+  __shared__ float sb[1024], sg[1024];
   const int t = threadIdx.x;
   float b = 0.f, g = 0.f;
-  if ((int)blockIdx.x < a.n * a.groups) {
-    const int n = blockIdx.x / a.groups, group = blockIdx.x - n * a.groups;
+  if ((int)blockIdx.x < group_blocks) {
+    const int id = SHORT ? blockIdx.x * 16 + (t >> 6) : blockIdx.x, team = SHORT ? 64 : 1024, lane = SHORT ? t & 63 : t;
+    if (SHORT && id >= a.n * a.groups) return;
+    const int n = id / a.groups, group = id - n * a.groups;
     const float* const part = a.part + (long)n * a.chunks * 2 * a.c + (long)group * a.cpg;
     const int terms = a.chunks * a.cpg;
-    for (int i = t; i < terms; i += 256) {
+#pragma unroll 4
+    for (int i = lane; i < terms; i += team) {
       const int k = i / a.cpg, j = i - k * a.cpg;
       const float w = a.gamma ? a.gamma[group * a.cpg + j] : 1.f;
       b = __builtin_fmaf(w, part[(long)k * 2 * a.c + j], b);
@@ -343,20 +296,27 @@ __global__ void __launch_bounds__(256) gn_grad_totals_kernel(GnArgs a) {
     }
     b = wave_sum(b);
     g = wave_sum(g);
-    if ((t & 63) == 0) sb[t >> 6] = b, sg[t >> 6] = g;
-    __syncthreads();
-    if (t == 0) {
+    if (!SHORT) {
+      if ((t & 63) == 0) sb[t >> 6] = b, sg[t >> 6] = g;
+      __syncthreads();
+      if (t == 0)
+        for (int k = 1; k < 16; ++k) {
+          b += sb[k];
+          g += sg[k];
+        }
+    }
+    if (lane == 0) {
       const float inv = 1.f / ((float)a.hw * (float)a.cpg);
-      a.stat[2 * blockIdx.x] = (sb[0] + sb[1] + sb[2] + sb[3]) * inv;
-      a.stat[2 * blockIdx.x + 1] = (sg[0] + sg[1] + sg[2] + sg[3]) * inv;
+      a.stat[2 * (long)id] = b * inv;
+      a.stat[2 * (long)id + 1] = g * inv;
     }
     return;
   }
-  const int ch = ((int)blockIdx.x - a.n * a.groups) * 16 + (t & 15);
+  const int ch = ((int)blockIdx.x - group_blocks) * 16 + (t & 15);
   const long rows = (long)a.n * a.chunks;
   if (ch < a.c) {
-#pragma unroll 4
-    for (long r = t >> 4; r < rows; r += 16) {
+#pragma unroll 8
+    for (long r = t >> 4; r < rows; r += 64) {
       b += a.part[r * 2 * a.c + ch];
       g += a.part[r * 2 * a.c + a.c + ch];
     }
@@ -364,24 +324,42 @@ __global__ void __launch_bounds__(256) gn_grad_totals_kernel(GnArgs a) {
   sb[t] = b;
   sg[t] = g;
   __syncthreads();
-  if (t < 16 && ch < a.c) {
-    for (int r = 1; r < 16; ++r) {
-      b += sb[r * 16 + t];
-      g += sg[r * 16 + t];
+#pragma unroll
+  for (int d = 512; d >= 16; d >>= 1) {
+    if (t < d) {
+      sb[t] += sb[t + d];
+      sg[t] += sg[t + d];
     }
-    if (a.dbeta) a.dbeta[ch] = b;
-    if (a.dgamma) a.dgamma[ch] = g;
+    __syncthreads();
   }
+  if (t < 16 && ch < a.c) {
+    if (a.dbeta) a.dbeta[ch] = sb[t];
+    if (a.dgamma) a.dgamma[ch] = sg[t];
+  }
+}
+static int launch_totals(const GnArgs& a, bool groups, hipStream_t st) {
+  const bool few = few_terms(a);
+  const int group_blocks = !groups ? 0 : few ? ceil_div((long)a.n * a.groups, 16) : a.n * a.groups;
+  const int channel_blocks = a.dbeta || a.dgamma ? ceil_div(a.c, 16) : 0;
+  if (group_blocks + channel_blocks == 0) return ALEXNET_OK;
+  KernelScope ks("gn_grad_totals", 0, 0, st);
+  if (few)
+    hipLaunchKernelGGL(gn_grad_totals_kernel<true>, dim3((unsigned)(group_blocks + channel_blocks)), dim3(1024), 0, st, a, group_blocks);
+  else
+    hipLaunchKernelGGL(gn_grad_totals_kernel<false>, dim3((unsigned)(group_blocks + channel_blocks)), dim3(1024), 0, st, a, group_blocks);
+  AX_LAUNCH_CHECK();
+  return ALEXNET_OK;
 }
 
 template <typename T, int V, int SRC>
 __global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a) {
-  const Spot s = spot(a, V);
+  const Spot s = spot(a, gridDim.x - 1 - blockIdx.x);  // backwards, as in gn_apply_kernel
   if (!s.has) return;
+  const Vec v = vec_of<V>(s.v, 0, a.c);
   float mean[V], rstd[V], gamma[V], beta[V], ma[V], mb[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int ch = s.v * V + i, g = s.n * a.groups + ch / a.cpg;
+    const int ch = v.c + i, g = s.n * a.groups + ch / a.cpg;
     mean[i] = a.mean[g];
     rstd[i] = a.rstd[g];
     gamma[i] = a.gamma ? a.gamma[ch] : 1.f;
@@ -396,22 +374,21 @@ __global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a) {
     for (int u = 0; u < kUnroll; ++u)
       if (p + u * a.rpi < s.p1) {
         const long row = (long)s.n * a.hw + p + u * a.rpi;
-        x[u] = Source<T, V, SRC>::load(a, row, s.v);
-        d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + s.v * V);
+        Source<T, V, SRC>::load(a, row, v, x[u]);
+        d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
       }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
       if (p + u * a.rpi < s.p1) {
         float xf[V], df[V];
-        Source<T, V, SRC>::widen(x[u], xf);
+        Source<T, V, SRC>::widen(x[u], v, xf);
         Pack<T, V>::widen(d[u], df);
+        float hat[V];
+        gate<V>(df, xf, hat, mean, rstd, gamma, beta, a.act);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float dz = gated(df[i], xf[i], mean[i], rstd[i], gamma[i], beta[i], a.act);
-          const float hat = (xf[i] - mean[i]) * rstd[i];
-          df[i] = rstd[i] * (__builtin_fmaf(gamma[i], dz, -ma[i]) - hat * mb[i]);
-        }
-        Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + s.v * V, df);
+        for (int i = 0; i < V; ++i) df[i] = rstd[i] * (__builtin_fmaf(gamma[i], df[i], -ma[i]) - hat[i] * mb[i]);
+        Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, df);
+        __builtin_amdgcn_sched_barrier(0);
       }
   }
 }
@@ -434,7 +411,7 @@ __global__ void __launch_bounds__(256) gn_empty_kernel(float* mean, float* rstd,
 // pixels of a chunk: some eight workgroups per compute unit, each with a few rounds of loads
 static void split(GnArgs& a, int V, bool blocks32) {
   const int lanes = blocks32 ? kCodeBlock / V : 1;
-  a.colvecs = a.c / V;
+  a.colvecs = ceil_div(a.c, V);
   a.cols = std::min(256, ceil_div(a.colvecs, lanes) * lanes);
   a.rpi = 256 / a.cols;
   a.col_blocks = ceil_div(a.colvecs, a.cols);
@@ -451,8 +428,8 @@ static int gn_check(const alexnet_group_norm_t* cfg, const char* who) {
              who, cfg->n, cfg->hw, cfg->c, cfg->groups);
   AX_REQUIRE(cfg->c % cfg->groups == 0, ALEXNET_ESHAPE, "%s: %d channels are no whole number of %d groups", who, cfg->c, cfg->groups);
   // what a grid of 2^32 threads reaches
-  AX_REQUIRE(cfg->c <= 1 << 20 && cfg->hw <= 1 << 28 && (long)cfg->n * cfg->groups <= 1 << 23 && (long)cfg->n * ceil_div(cfg->c, 256) < 1 << 24,
-             ALEXNET_ESHAPE, "%s: at most 2^20 channels, 2^28 pixels of a map, 2^23 groups and 2^32 channels in all pictures", who);
+  AX_REQUIRE(cfg->c <= 1 << 20 && cfg->hw <= 1 << 28 && (long)cfg->n * cfg->groups <= 1 << 21 && (long)cfg->n * ceil_div(cfg->c, 256) < 1 << 24,
+             ALEXNET_ESHAPE, "%s: at most 2^20 channels, 2^28 pixels of a map, 2^21 groups and 2^32 channels in all pictures", who);
   AX_REQUIRE(cfg->eps > 0.f && cfg->eps < INFINITY, ALEXNET_EINVAL, "%s: eps must be positive and finite", who);
   return ALEXNET_OK;
 }
@@ -469,13 +446,12 @@ static GnArgs gn_args(const alexnet_group_norm_t* cfg) {
   return a;
 }
 static bool empty(const alexnet_group_norm_t* cfg) { return cfg->n == 0 || cfg->hw == 0; }
-// the largest scratch that any alignment of the tensors leads to
+// The largest scratch of the ways to cut rows into threads: with one value a thread (tiny or in-place odd rows) or vectors
 static size_t gn_ws(const alexnet_group_norm_t* cfg) {
   if (empty(cfg)) return 0;
   size_t most = 0;
-  for (int V : {1, 16 / (int)type_size(cfg->type)})
+  for (int V : {1, kBackwardVec, 16 / (int)type_size(cfg->type)})
     for (int b = 0; b < 2; ++b) {
-      if (cfg->c % V) continue;
       GnArgs a = gn_args(cfg);
       split(a, V, b);
       most = std::max(most, (size_t)a.n * a.chunks * 2 * a.c * sizeof(float));
@@ -494,8 +470,7 @@ static void gn_scratch(GnArgs& a, void* ws, size_t bytes) {
   } while (0)
 
 template <typename T, int V>
-static int gn_forward(GnArgs a, int keep, size_t ws, hipStream_t st) {
-  (void)ws;
+static int gn_forward(GnArgs a, int keep, hipStream_t st) {
   split(a, V, keep != kKeepNone);
   const long blocks = (long)a.n * a.chunks * a.col_blocks;
   const double bytes = (double)a.n * a.hw * a.c * sizeof(T);
@@ -510,7 +485,10 @@ static int gn_forward(GnArgs a, int keep, size_t ws, hipStream_t st) {
   }
   {
     KernelScope ks("gn_statistics", 0, 0, st);
-    GN_LAUNCH(gn_statistics_kernel, (long)a.n * a.groups, 64, st, a);
+    if (few_terms(a))
+      GN_LAUNCH(gn_statistics_kernel<64>, ceil_div((long)a.n * a.groups, 4), 256, st, a);
+    else
+      GN_LAUNCH(gn_statistics_kernel<256>, (long)a.n * a.groups, 256, st, a);
   }
   KernelScope ks("gn_apply", 0, 2 * bytes, st);
   GN_LAUNCH((gn_apply_kernel<T, V>), blocks, 256, st, a);
@@ -526,34 +504,37 @@ static int gn_backward(GnArgs a, hipStream_t st) {
     KernelScope ks("gn_grad_sums", 0, in, st);
     GN_LAUNCH((gn_grad_sums_kernel<T, V, SRC>), blocks, 256, st, a);
   }
-  {
-    KernelScope ks("gn_grad_totals", 0, 0, st);
-    GN_LAUNCH(gn_grad_totals_kernel, (long)a.n * a.groups + ceil_div(a.c, 16), 256, st, a);
-  }
+  AX_TRY(launch_totals(a, true, st));
   KernelScope ks("gn_grad_apply", 0, in + values * sizeof(T), st);
   GN_LAUNCH((gn_grad_apply_kernel<T, V, SRC>), blocks, 256, st, a);
   return ALEXNET_OK;
 }
 
+// Vectors wherever a row holds one.  Threads that share channels (group_norm.h) may not read what the other has overwritten
+// already, so odd rows in place go value by value, unless a workgroup reads all before it writes.
 template <typename T>
-static int gn_forward_type(const GnArgs& a, int keep, size_t ws, hipStream_t st) {
+static int gn_forward_type(const GnArgs& a, int type, int keep, hipStream_t st) {
   constexpr int V = 16 / sizeof(T);
-  const bool vec = a.c % V == 0 && rows_vec_ok(a.x, a.ld_x, sizeof(T)) && rows_vec_ok(a.out, a.ld_out, sizeof(T)) &&
-                   (keep == kKeepNone || (uintptr_t)a.keep % V == 0);
-  return vec ? gn_forward<T, V>(a, keep, ws, st) : gn_forward<T, 1>(a, keep, ws, st);
+  const SlabPlan p = slab_plan(a.n, a.hw, a.c, a.groups, V, kForwardRegs, keep != kKeepNone, 1, 12);
+  if (p.groups) return launch_gn_slab_forward(a, p, type, keep, st);
+  return a.c >= V && (a.c % V == 0 || a.x != a.out) ? gn_forward<T, V>(a, keep, st) : gn_forward<T, 1>(a, keep, st);
 }
 template <typename T, int SRC>
-static int gn_backward_src(const GnArgs& a, hipStream_t st) {
-  constexpr int V = 16 / sizeof(T);
-  const bool vec = a.c % V == 0 && (SRC == SRC_TENSOR ? rows_vec_ok(a.x, a.ld_x, sizeof(T)) : (uintptr_t)a.codes % V == 0) &&
-                   rows_vec_ok(a.dy, a.ld_dy, sizeof(T)) && rows_vec_ok(a.out, a.ld_out, sizeof(T));
-  return vec ? gn_backward<T, V, SRC>(a, st) : gn_backward<T, 1, SRC>(a, st);
+static int gn_backward_src(GnArgs a, int type, hipStream_t st) {
+  const SlabPlan p = slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, false, 2, 16);
+  if (p.groups) {
+    AX_TRY(launch_gn_slab_backward(a, p, type, SRC, st));
+    a.chunks = 1;
+    return a.n > 1 ? launch_totals(a, false, st) : ALEXNET_OK;
+  }
+  constexpr int V = kBackwardVec;
+  return a.c >= V && (a.c % V == 0 || (a.dy != a.out && a.x != a.out)) ? gn_backward<T, V, SRC>(a, st) : gn_backward<T, 1, SRC>(a, st);
 }
 template <typename T>
-static int gn_backward_type(const GnArgs& a, int src, hipStream_t st) {
-  return src == SRC_TENSOR ? gn_backward_src<T, SRC_TENSOR>(a, st)
-         : src == SRC_INT8 ? gn_backward_src<T, SRC_INT8>(a, st)
-                           : gn_backward_src<T, SRC_E4M3>(a, st);
+static int gn_backward_type(const GnArgs& a, int type, int src, hipStream_t st) {
+  return src == SRC_TENSOR ? gn_backward_src<T, SRC_TENSOR>(a, type, st)
+         : src == SRC_INT8 ? gn_backward_src<T, SRC_INT8>(a, type, st)
+                           : gn_backward_src<T, SRC_E4M3>(a, type, st);
 }
 static int gn_fill_empty(const alexnet_group_norm_t* cfg, float* mean, float* rstd, float* dgamma, float* dbeta, hipStream_t st) {
   const long stats = mean || rstd ? (long)cfg->n * cfg->groups : 0, n = std::max<long>(stats, dgamma || dbeta ? cfg->c : 0);
@@ -607,9 +588,9 @@ int alexnet_group_norm_forward(const alexnet_group_norm_t* cfg, const void* d_x,
     a.keep_scales = (uint8_t*)keep->d_scales;
   }
   gn_scratch(a, d_workspace, need);
-  return cfg->type == ALEXNET_TYPE_FP32   ? gn_forward_type<float>(a, code, need, st)
-         : cfg->type == ALEXNET_TYPE_BF16 ? gn_forward_type<__bf16>(a, code, need, st)
-                                          : gn_forward_type<_Float16>(a, code, need, st);
+  return cfg->type == ALEXNET_TYPE_FP32   ? gn_forward_type<float>(a, cfg->type, code, st)
+         : cfg->type == ALEXNET_TYPE_BF16 ? gn_forward_type<__bf16>(a, cfg->type, code, st)
+                                          : gn_forward_type<_Float16>(a, cfg->type, code, st);
 }
 
 int alexnet_group_norm_backward(const alexnet_group_norm_t* cfg, const void* d_x, int64_t ld_x,
@@ -649,9 +630,9 @@ int alexnet_group_norm_backward(const alexnet_group_norm_t* cfg, const void* d_x
   a.dbeta = d_dbeta;
   gn_scratch(a, d_workspace, need);
   const int src = !kept ? SRC_TENSOR : kept->code == ALEXNET_CODE_INT8 ? SRC_INT8 : SRC_E4M3;
-  return cfg->type == ALEXNET_TYPE_FP32   ? gn_backward_type<float>(a, src, st)
-         : cfg->type == ALEXNET_TYPE_BF16 ? gn_backward_type<__bf16>(a, src, st)
-                                          : gn_backward_type<_Float16>(a, src, st);
+  return cfg->type == ALEXNET_TYPE_FP32   ? gn_backward_type<float>(a, cfg->type, src, st)
+         : cfg->type == ALEXNET_TYPE_BF16 ? gn_backward_type<__bf16>(a, cfg->type, src, st)
+                                          : gn_backward_type<_Float16>(a, cfg->type, src, st);
 }
 
 }  // extern "C"

@@ -1,0 +1,64 @@
+// How group normalisation cuts a picture into slabs that workgroups hold in registers (plain host code: tests walk it on the CPU).
+#pragma once
+#include <algorithm>
+
+namespace ax {
+
+// A workgroup takes `groups` whole groups of a picture (the last slab those that are left): threads / cols pixels at a time,
+// cols threads side by side with V channels each, `regs` pixels to a thread.
+struct SlabPlan {
+  int groups = 0, slabs = 0;  // groups = 0: does not fit
+  int threads = 0, cols = 0, rpi = 0, regs = 0;
+};
+
+// V channels a thread and pixel, at most max_regs pixels a thread; blocks32: slabs and threads in whole blocks of 32 channels;
+// sums: values per channel that the workgroup adds up, in 64 KB of LDS at most; narrow: the least channels of a pixel that
+// 1024 threads take (unless those are all).
+//
+// A wider slab makes better use of memory lines, up to 32 channels or so; at most 512 threads let a second workgroup load while
+// the first one adds up.  So: the widest up to 32 channels that 512 threads hold, if those are 16 channels; else 1024 threads.
+// Forward, 256 x 729 x 256 bf16: 32 channels 52 us, 16 channels 62, 8 channels 76, three launches 85; 64 x 4096 x 128 bf16: 512
+// threads 36, 1024 threads 58, three launches 56.  Backward, 256 x 729 x 256 fp32: 16 channels and 512 threads 137, 32 channels
+// and 1024 threads 146, three launches 237; 128 x 3025 x 96 fp32: 12 channels and 1024 threads 229, three launches 175.
+inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, bool blocks32, int sums, int narrow) {
+  const int cpg = c / groups, lanes = blocks32 ? 32 / V : 1;
+  SlabPlan best, large;
+  // slabs start on whole blocks of 32 channels: their groups' channels are a multiple of 32, or all there are
+  int unit = 1;
+  if (blocks32)
+    while (unit < groups && (long)unit * cpg % 32 != 0) ++unit;
+  for (long k = unit;; k = std::min<long>(k + unit, groups)) {
+    const long width = k * cpg;
+    SlabPlan p;
+    p.groups = (int)k;
+    p.slabs = (int)((groups + k - 1) / k);
+    const long last = (groups - (p.slabs - 1) * k) * cpg;  // channels of the last slab
+    const long cols = ((width + V - 1) / V + lanes - 1) / lanes * lanes;
+    if (cols > 1024) break;
+    if (std::min(width, last) >= V) {
+      p.cols = (int)cols;
+      const bool few = (long)n * p.slabs < 128;  // then more threads, at four pixels each
+      for (int threads : {256, 512, 1024}) {
+        p.threads = threads;
+        p.rpi = (int)(threads / cols);
+        if (!p.rpi) continue;
+        p.regs = (hw + p.rpi - 1) / p.rpi;
+        if (p.regs <= (few ? std::min(4, max_regs) : max_regs)) break;
+      }
+      const long lds = 4L * ((long)sums * p.threads * V + 2 * k);
+      const bool fits = p.rpi > 0 && p.regs <= max_regs && lds <= 65536;
+      if (!fits && (best.groups || large.groups)) break;  // wider ones do not fit either
+      if (fits) {
+        if (p.threads < 1024 || few)
+          best = p;
+        else if (width >= narrow || k >= groups)
+          large = p;
+        if (width >= 32 || (width >= 16 && few)) break;
+      }
+    }
+    if (k >= groups) break;
+  }
+  return best.groups && ((long)best.groups * cpg >= 16 || !large.groups) ? best : large;
+}
+
+}  // namespace ax

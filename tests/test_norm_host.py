@@ -1,6 +1,9 @@
 """CPU-only: what group normalisation and the 8-bit checkpoints refuse, before any GPU work, and the tests' own references
 against brute force."""
 import ctypes as C
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -25,7 +28,7 @@ def cfg(B, **kw):
     (dict(type=3), "EINVAL"), (dict(type=-1), "EINVAL"), (dict(act=3), "EINVAL"), (dict(act=-1), "EINVAL"), (dict(eps=0.0), "EINVAL"),
     (dict(eps=-1.0), "EINVAL"), (dict(eps=float("nan")), "EINVAL"), (dict(eps=float("inf")), "EINVAL"), (dict(n=-1), "ESHAPE"),
     (dict(hw=-1), "ESHAPE"), (dict(c=0), "ESHAPE"), (dict(groups=0), "ESHAPE"), (dict(groups=3), "ESHAPE"),
-    (dict(c=(1 << 20) + 8), "ESHAPE"), (dict(hw=(1 << 28) + 1), "ESHAPE"), (dict(n=1 << 23, groups=2), "ESHAPE"),
+    (dict(c=(1 << 20) + 8), "ESHAPE"), (dict(hw=(1 << 28) + 1), "ESHAPE"), (dict(n=1 << 21, groups=2), "ESHAPE"),
     (dict(n=1 << 20, c=1 << 13, groups=1), "ESHAPE")])
 def test_configurations_that_are_refused(B, change, code):
     ws = C.c_size_t()
@@ -159,3 +162,12 @@ def test_the_reference_gradients_by_differences():
             e = np.eye(6)[i] * h
             assert abs((loss(x, gamma + e, beta) - loss(x, gamma - e, beta)) / (2 * h) - dgamma[i]) < 1e-7
             assert abs((loss(x, gamma, beta + e) - loss(x, gamma, beta - e)) / (2 * h) - dbeta[i]) < 1e-7
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
+def test_slabs_cover_the_picture_and_fit(tmp_path):
+    exe = str(tmp_path / "norm_plan_check")
+    src = os.path.join(os.path.dirname(os.path.abspath(__file__)), "emu", "norm_plan_check.cpp")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-fsanitize=address,undefined", "-o", exe, src], check=True, timeout=300)
+    out = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and out.stdout.startswith("OK"), out.stdout + out.stderr
