@@ -403,10 +403,12 @@ typedef struct {
   float eps;                /* > 0 */
 } alexnet_group_norm_t;
 
-/* Scratch of a call: d_workspace is 256-byte aligned and holds at least
- * workspace_bytes (null is fine when that is 0).  It is free again once the
- * call's work has run. */
-int alexnet_group_norm_query(const alexnet_group_norm_t* cfg, size_t* workspace_bytes);
+/* Scratch of a forward and of a backward call (keep != 0: of a forward call that
+ * leaves a checkpoint): d_workspace is 256-byte aligned and holds at least so
+ * many bytes; null is fine where that is 0, as it is for a forward call on maps
+ * whose groups fit a workgroup.  It is free again once the call's work has run. */
+int alexnet_group_norm_query(const alexnet_group_norm_t* cfg, int32_t keep, size_t* forward_bytes,
+                             size_t* backward_bytes);
 /* d_gamma / d_beta [c] may be null (1 / 0); d_mean / d_rstd [n][groups] (may be
  * null) receive m and r.  keep (may be null): where to leave the 8-bit
  * checkpoint of x as [n * hw][c], as alexnet_checkpoint_pack would. */

@@ -111,7 +111,7 @@ class GroupNormCfg(C.Structure):
 
 _i64, _kp, _gp = C.c_int64, C.POINTER(CheckpointArg), C.POINTER(GroupNormCfg)
 _SIGS.update({
-    "alexnet_group_norm_query": [_gp, C.POINTER(_sz)],
+    "alexnet_group_norm_query": [_gp, _i32, C.POINTER(_sz), C.POINTER(_sz)],
     "alexnet_group_norm_forward": [_gp, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _kp, _vp, _sz, _vp],
     "alexnet_group_norm_backward": [_gp, _vp, _i64, _kp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz,
                                     _vp],
@@ -614,16 +614,18 @@ class Checkpoint:
             raise ValueError(f"Checkpoint: codes are int8 or float8_e4m3fn and scales uint8, got {codes.dtype} and {scales.dtype}")
         if codes.dim() < 2 or codes.shape[:-1] != scales.shape[:-1] or scales.shape[-1] != -(-codes.shape[-1] // CODE_BLOCK):
             raise ValueError(f"Checkpoint: scales {list(scales.shape)} do not belong to codes {list(codes.shape)}")
-        if not codes.is_contiguous() or not scales.is_contiguous():
-            raise ValueError("Checkpoint: codes and scales must be contiguous")
+        if not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device:
+            raise ValueError("Checkpoint: codes and scales must be contiguous, on one device")
         self.codes, self.scales = codes, scales
 
     @staticmethod
-    def empty(shape, dtype: torch.dtype, device) -> "Checkpoint":
+    def _empty(shape, dtype: torch.dtype, device) -> "Checkpoint":
         if dtype not in _CODES:
             raise ValueError(f"a checkpoint's codes are int8 or float8_e4m3fn, got {dtype}")
-        return Checkpoint(torch.empty(shape, dtype=dtype, device=device),
-                          torch.empty((*shape[:-1], -(-shape[-1] // CODE_BLOCK)), dtype=torch.uint8, device=device))
+        kept = Checkpoint.__new__(Checkpoint)
+        kept.codes = torch.empty(shape, dtype=dtype, device=device)
+        kept.scales = torch.empty((*shape[:-1], -(-shape[-1] // CODE_BLOCK)), dtype=torch.uint8, device=device)
+        return kept
 
     @property
     def shape(self):
@@ -631,6 +633,10 @@ class Checkpoint:
 
     def _arg(self) -> CheckpointArg:
         return CheckpointArg(self.codes.data_ptr(), self.scales.data_ptr(), _CODES[self.codes.dtype])
+
+    def _need(self, what: str):
+        if not self.codes.is_cuda:
+            raise ValueError(f"{what}: expected a device tensor, got a checkpoint on {self.codes.device}")
 
 
 def _rows_stride(t, what: str) -> int:
@@ -651,7 +657,7 @@ def _rows_stride(t, what: str) -> int:
         if size == 1:
             continue
         if ld is None:
-            ld = reach = stride
+            ld = stride
         elif stride != reach:
             ld = -1
             break
@@ -663,75 +669,67 @@ def _rows_stride(t, what: str) -> int:
     return ld
 
 
-class _On:
-    """The device and stream of a call.  With a stream of its own, what the call allocates belongs to that stream's pool, and
-    the allocator learns of the use of its tensors on the other one."""
-
-    def __init__(self, first: torch.Tensor, stream):
-        self.dev, self.given = first.device, stream
-        if stream is not None and stream.device != self.dev:
-            raise ValueError(f"the stream belongs to {stream.device}, the tensors to {self.dev}")
-        self.ctx = (torch.cuda.stream(stream) if stream is not None else
-                    torch.cuda.device(self.dev) if self.dev.index != torch.cuda.current_device() else None)
-
-    def __enter__(self):
-        if self.ctx is not None:
-            if self.given is not None:
-                self.caller = torch.cuda.current_stream(self.dev)
-            self.ctx.__enter__()
-        self.raw = torch.cuda.current_stream(self.dev).cuda_stream
-        return self
-
-    def __exit__(self, *exc):
-        return self.ctx.__exit__(*exc) if self.ctx is not None else None
-
-    def used(self, inputs, outputs):
-        if self.given is None or self.given == self.caller:
-            return
-        for t in inputs:
-            if t is not None:
-                t.record_stream(self.given)
-        for t in outputs:
-            if t is not None:
-                t.record_stream(self.caller)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _same_device(first: torch.Tensor, what: str, *tensors):
-    for t in tensors:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"{what}: tensors on {first.device} and {t.device}")
+def _here(t: torch.Tensor, stream) -> bool:
+    """Whether a call on t runs on the current device and its current stream."""
+    return stream is None and t.get_device() == torch.cuda.current_device()
+
+
+def _there(t: torch.Tensor, stream, inputs, call):
+    """call() on t's device, on `stream` if that is given: what it allocates then belongs to that stream's pool, and the
+    allocator learns of the tensors that are used on a stream other than their own."""
+    if stream is None:
+        with torch.cuda.device(t.device):
+            return call()
+    if stream.device != t.device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {t.device}")
+    caller = torch.cuda.current_stream(t.device)
+    with torch.cuda.stream(stream):
+        result = call()
+    if stream != caller:
+        outputs = result if isinstance(result, tuple) else (result,)
+        for group, user in ((inputs, stream), (outputs, caller)):
+            for x in group:
+                for part in (x.codes, x.scales) if isinstance(x, Checkpoint) else (x,):
+                    if part is not None:
+                        part.record_stream(user)
+    return result
 
 
 def _vector(t, n: int, first: torch.Tensor, what: str):
-    if t is not None:
-        _need(t, torch.float32, n, what)
-        if t.numel() != n or t.device != first.device:
-            raise ValueError(f"{what}: expected {n} elements on {first.device}, got {t.numel()} on {t.device}")
+    if t is None:
+        return None
+    _need(t, torch.float32, n, what)
+    if t.numel() != n or t.device != first.device:
+        raise ValueError(f"{what}: expected {n} elements on {first.device}, got {t.numel()} on {t.device}")
+    return t.data_ptr()
 
 
 def _result(out, shape, dtype, device, what: str):
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
-        return out, shape[-1]
+        return torch.empty(shape, dtype=dtype, device=device), shape[-1]
     ld = _rows_stride(out, what)
     if out.shape != shape or out.dtype != dtype or out.device != device:
         raise ValueError(f"{what}: expected {dtype} {list(shape)} on {device}, got {out.dtype} {list(out.shape)} on {out.device}")
     return out, ld
 
 
+def _scratch(nbytes: int, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
 @functools.lru_cache(maxsize=256)
-def _group_norm_cfg(n: int, hw: int, c: int, groups: int, kind: int, act: int, eps: float):
-    if max(n, hw, c, groups) >= 1 << 31:
-        raise ValueError("group_norm: sizes of 2^31 and more are not supported")
-    cfg, ws = GroupNormCfg(n, hw, c, groups, kind, act, eps), _sz()
-    _check(_lib.alexnet_group_norm_query(C.byref(cfg), C.byref(ws)))
-    return cfg, ws.value
-
-
-def _activation(act: str) -> int:
+def _group_norm_cfg(n: int, hw: int, c: int, groups: int, kind: int, act: str, eps: float, keep: bool):
     if act not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {act!r}")
-    return ACTIVATIONS[act]
+    if max(n, hw, c, groups) >= 1 << 31:
+        raise ValueError("group_norm: sizes of 2^31 and more are not supported")
+    cfg, forward, backward = GroupNormCfg(n, hw, c, groups, kind, ACTIVATIONS[act], eps), _sz(), _sz()
+    _check(_lib.alexnet_group_norm_query(cfg, keep, forward, backward))
+    return cfg, forward.value, backward.value
 
 
 def group_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int,
@@ -740,22 +738,22 @@ def group_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Opt
     """y = act(group_norm(x) * gamma + beta) of x [n]...[c]: (y, mean [n][groups], rstd [n][groups], kept).  checkpoint: the
     type of the codes (torch.int8, torch.float8_e4m3fn) of an 8-bit copy of x to leave in `kept`, else that is None.  out: where y
     goes (may be x)."""
-    what = "group_norm_forward"
-    ld_x = _rows_stride(x, what + ": x")
-    n, c = x.shape[0], x.shape[-1]
-    cfg, ws_bytes = _group_norm_cfg(n, x.shape[1:-1].numel(), c, groups, _TYPES[x.dtype], _activation(act), eps)
-    _vector(gamma, c, x, what + ": gamma")
-    _vector(beta, c, x, what + ": beta")
-    with _On(x, stream) as on:
-        y, ld_y = _result(out, x.shape, x.dtype, x.device, what + ": out")
-        stats = torch.empty((2, n, groups), dtype=torch.float32, device=x.device)
-        mean, rstd = stats[0], stats[1]
-        kept = None if checkpoint is None else Checkpoint.empty(x.shape, checkpoint, x.device)
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device)
-        _check(_lib.alexnet_group_norm_forward(cfg, x.data_ptr(), ld_x, _ptr(gamma), _ptr(beta), y.data_ptr(), ld_y,
-                                               mean.data_ptr(), rstd.data_ptr(), None if kept is None else kept._arg(),
-                                               ws.data_ptr(), ws_bytes, on.raw))
-        on.used((x, gamma, beta, out), (y, stats) if kept is None else (y, stats, kept.codes, kept.scales))
+    ld_x = _rows_stride(x, "group_norm_forward: x")
+    if not _here(x, stream):
+        return _there(x, stream, (x, gamma, beta, out),
+                      lambda: group_norm_forward(x, gamma, beta, groups, eps, act, checkpoint, out))
+    shape, device = x.shape, x.device
+    n, c = shape[0], shape[-1]
+    cfg, ws_bytes, _ = _group_norm_cfg(n, shape[1:-1].numel(), c, groups, _TYPES[x.dtype], act, eps, checkpoint is not None)
+    p_gamma, p_beta = _vector(gamma, c, x, "group_norm_forward: gamma"), _vector(beta, c, x, "group_norm_forward: beta")
+    y, ld_y = _result(out, shape, x.dtype, device, "group_norm_forward: out")
+    mean = torch.empty((n, groups), dtype=torch.float32, device=device)
+    rstd = torch.empty_like(mean)
+    kept = None if checkpoint is None else Checkpoint._empty(shape, checkpoint, device)
+    ws = _scratch(ws_bytes, device)
+    _check(_lib.alexnet_group_norm_forward(cfg, x.data_ptr(), ld_x, p_gamma, p_beta, y.data_ptr(), ld_y, mean.data_ptr(),
+                                           rstd.data_ptr(), None if kept is None else kept._arg(),
+                                           None if ws is None else ws.data_ptr(), ws_bytes, _raw_stream(device.index)))
     return y, mean, rstd, kept
 
 
@@ -764,43 +762,45 @@ def group_norm_backward(x, dy: torch.Tensor, mean: torch.Tensor, rstd: torch.Ten
     """(dx, dgamma, dbeta) of group_norm_forward from x, or its Checkpoint, and the forward call's mean and rstd.  out: where dx
     goes (may be dy)."""
     what = "group_norm_backward"
-    kept = x if isinstance(x, Checkpoint) else None
-    ld_x = 0 if kept is not None else _rows_stride(x, what + ": x")
-    ld_dy = _rows_stride(dy, what + ": dy")
-    if x.shape != dy.shape or (kept is None and x.dtype != dy.dtype):
-        raise ValueError(f"{what}: x {list(x.shape)} and dy {list(dy.shape)} differ in shape or type")
-    n, c = dy.shape[0], dy.shape[-1]
+    ld_dy = _rows_stride(dy, "group_norm_backward: dy")
+    if not _here(dy, stream):
+        return _there(dy, stream, (x, dy, mean, rstd, gamma, beta, out),
+                      lambda: group_norm_backward(x, dy, mean, rstd, gamma, beta, act, out))
+    shape, device = dy.shape, dy.device
+    kept = p_x = None
+    ld_x = 0
+    if isinstance(x, Checkpoint):
+        kept, source = x._arg(), x.codes
+        x._need(what)
+    else:
+        ld_x, p_x, source = _rows_stride(x, "group_norm_backward: x"), x.data_ptr(), x
+    if source.shape != shape or source.device != device or (kept is None and x.dtype != dy.dtype):
+        raise ValueError(f"{what}: x {list(source.shape)} and dy {list(shape)} differ in shape, type or device")
+    n, c = shape[0], shape[-1]
     if mean.dim() != 2 or mean.shape[0] != n or mean.shape[1] < 1:
         raise ValueError(f"{what}: mean: expected [{n}][groups], got {list(mean.shape)}")
     groups = mean.shape[1]
-    _vector(mean, n * groups, dy, what + ": mean")
-    _vector(rstd, n * groups, dy, what + ": rstd")
-    _vector(gamma, c, dy, what + ": gamma")
-    _vector(beta, c, dy, what + ": beta")
-    source = (x,) if kept is None else (kept.codes, kept.scales)
-    _same_device(dy, what, *source)
-    cfg, ws_bytes = _group_norm_cfg(n, dy.shape[1:-1].numel(), c, groups, _TYPES[dy.dtype], _activation(act), 1e-5)
-    with _On(dy, stream) as on:
-        dx, ld_dx = _result(out, dy.shape, dy.dtype, dy.device, what + ": out")
-        grads = torch.empty((2, c), dtype=torch.float32, device=dy.device)
-        dgamma, dbeta = grads[0], grads[1]
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dy.device)
-        _check(_lib.alexnet_group_norm_backward(cfg, x.data_ptr() if kept is None else None, ld_x,
-                                                None if kept is None else kept._arg(), dy.data_ptr(), ld_dy, mean.data_ptr(),
-                                                rstd.data_ptr(), _ptr(gamma), _ptr(beta), dx.data_ptr(), ld_dx,
-                                                dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), ws_bytes, on.raw))
-        on.used((*source, dy, mean, rstd, gamma, beta, out), (dx, grads))
+    p_mean, p_rstd = _vector(mean, n * groups, dy, "group_norm_backward: mean"), _vector(rstd, n * groups, dy, "group_norm_backward: rstd")
+    p_gamma, p_beta = _vector(gamma, c, dy, "group_norm_backward: gamma"), _vector(beta, c, dy, "group_norm_backward: beta")
+    cfg, _, ws_bytes = _group_norm_cfg(n, shape[1:-1].numel(), c, groups, _TYPES[dy.dtype], act, 1e-5, False)
+    dx, ld_dx = _result(out, shape, dy.dtype, device, "group_norm_backward: out")
+    dgamma = torch.empty(c, dtype=torch.float32, device=device)
+    dbeta = torch.empty_like(dgamma)
+    ws = _scratch(ws_bytes, device)
+    _check(_lib.alexnet_group_norm_backward(cfg, p_x, ld_x, kept, dy.data_ptr(), ld_dy, p_mean, p_rstd, p_gamma, p_beta,
+                                            dx.data_ptr(), ld_dx, dgamma.data_ptr(), dbeta.data_ptr(),
+                                            None if ws is None else ws.data_ptr(), ws_bytes, _raw_stream(device.index)))
     return dx, dgamma, dbeta
 
 
 def checkpoint_pack(x: torch.Tensor, dtype: torch.dtype = torch.int8, stream=None) -> Checkpoint:
     """x [rows]...[c] in 8 bits: codes of `dtype` (torch.int8 or torch.float8_e4m3fn), a power-of-two scale per 32 channels."""
     ld = _rows_stride(x, "checkpoint_pack: x")
-    with _On(x, stream) as on:
-        kept = Checkpoint.empty(x.shape, dtype, x.device)
-        _check(_lib.alexnet_checkpoint_pack(x.data_ptr(), ld, _TYPES[x.dtype], x.shape[:-1].numel(), x.shape[-1],
-                                            kept._arg(), on.raw))
-        on.used((x,), (kept.codes, kept.scales))
+    if not _here(x, stream):
+        return _there(x, stream, (x,), lambda: checkpoint_pack(x, dtype))
+    kept = Checkpoint._empty(x.shape, dtype, x.device)
+    _check(_lib.alexnet_checkpoint_pack(x.data_ptr(), ld, _TYPES[x.dtype], x.shape[:-1].numel(), x.shape[-1], kept._arg(),
+                                        _raw_stream(x.get_device())))
     return kept
 
 
@@ -810,14 +810,12 @@ def checkpoint_unpack(kept: Checkpoint, dtype: torch.dtype = torch.float32, out:
     codes = kept.codes
     if dtype not in _TYPES:
         raise ValueError(f"checkpoint_unpack: expected float32, bfloat16 or float16, got {dtype}")
-    _need(codes, codes.dtype, 0, "checkpoint_unpack: codes")
-    _need(kept.scales, torch.uint8, 0, "checkpoint_unpack: scales")
-    _same_device(codes, "checkpoint_unpack", kept.scales)
-    with _On(codes, stream) as on:
-        x, ld = _result(out, codes.shape, dtype, codes.device, "checkpoint_unpack: out")
-        _check(_lib.alexnet_checkpoint_unpack(kept._arg(), codes.shape[:-1].numel(), codes.shape[-1], x.data_ptr(), ld,
-                                              _TYPES[dtype], on.raw))
-        on.used((codes, kept.scales, out), (x,))
+    kept._need("checkpoint_unpack")
+    if not _here(codes, stream):
+        return _there(codes, stream, (kept, out), lambda: checkpoint_unpack(kept, dtype, out))
+    x, ld = _result(out, codes.shape, dtype, codes.device, "checkpoint_unpack: out")
+    _check(_lib.alexnet_checkpoint_unpack(kept._arg(), codes.shape[:-1].numel(), codes.shape[-1], x.data_ptr(), ld,
+                                          _TYPES[dtype], _raw_stream(codes.get_device())))
     return x
 
 
@@ -831,27 +829,25 @@ def _checkpoint_fc_ws(rows: int, cols: int, out: int, kind: int) -> int:
 def checkpoint_fc_backward_weight(kept: Checkpoint, dy: torch.Tensor, dw: Optional[torch.Tensor] = None,
                                   db: Optional[torch.Tensor] = None, stream=None):
     """(dw [out][in], db [out]) in float32 of a dense layer, or of a 1 x 1 convolution over pixels, whose input [rows]...[in]
-    was kept as a Checkpoint, from dy [rows]...[out]."""
+    was kept as a Checkpoint, from dy [rows]...[out].  dw, db: where they go."""
     what = "checkpoint_fc_backward_weight"
     codes = kept.codes
-    ld = _rows_stride(dy, what + ": dy")
-    _need(codes, codes.dtype, 0, what + ": codes")
-    _need(kept.scales, torch.uint8, 0, what + ": scales")
-    if codes.shape[:-1].numel() != dy.shape[:-1].numel():
-        raise ValueError(f"{what}: a checkpoint {list(codes.shape)} and dy {list(dy.shape)} differ in their rows")
-    rows, cols, wide = codes.shape[:-1].numel(), codes.shape[-1], dy.shape[-1]
-    _same_device(dy, what, codes, kept.scales)
-    ws_bytes = _checkpoint_fc_ws(rows, cols, wide, _TYPES[dy.dtype])
-    if dw is not None:
-        _vector(dw, wide * cols, dy, what + ": dw")
-    if db is not None:
-        _vector(db, wide, dy, what + ": db")
-    with _On(dy, stream) as on:
-        given = (dw, db)
-        dw = torch.empty((wide, cols), dtype=torch.float32, device=dy.device) if dw is None else dw
-        db = torch.empty(wide, dtype=torch.float32, device=dy.device) if db is None else db
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dy.device)
-        _check(_lib.alexnet_checkpoint_fc_backward_weight(kept._arg(), dy.data_ptr(), ld, _TYPES[dy.dtype], rows, cols, wide,
-                                                          dw.data_ptr(), db.data_ptr(), ws.data_ptr(), ws_bytes, on.raw))
-        on.used((codes, kept.scales, dy, *given), (dw, db))
+    ld = _rows_stride(dy, "checkpoint_fc_backward_weight: dy")
+    kept._need(what)
+    if not _here(dy, stream):
+        return _there(dy, stream, (kept, dy, dw, db), lambda: checkpoint_fc_backward_weight(kept, dy, dw, db))
+    device = dy.device
+    rows, cols, wide, kind = codes.shape[:-1].numel(), codes.shape[-1], dy.shape[-1], _TYPES[dy.dtype]
+    if rows != dy.shape[:-1].numel() or codes.device != device:
+        raise ValueError(f"{what}: a checkpoint {list(codes.shape)} on {codes.device} and dy {list(dy.shape)} on {device} differ "
+                         "in their rows or device")
+    _vector(dw, wide * cols, dy, "checkpoint_fc_backward_weight: dw")
+    _vector(db, wide, dy, "checkpoint_fc_backward_weight: db")
+    ws_bytes = _checkpoint_fc_ws(rows, cols, wide, kind)
+    dw = torch.empty((wide, cols), dtype=torch.float32, device=device) if dw is None else dw
+    db = torch.empty(wide, dtype=torch.float32, device=device) if db is None else db
+    ws = _scratch(ws_bytes, device)
+    _check(_lib.alexnet_checkpoint_fc_backward_weight(kept._arg(), dy.data_ptr(), ld, kind, rows, cols, wide, dw.data_ptr(),
+                                                      db.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes,
+                                                      _raw_stream(device.index)))
     return dw, db

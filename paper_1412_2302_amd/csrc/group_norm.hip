@@ -446,21 +446,46 @@ static GnArgs gn_args(const alexnet_group_norm_t* cfg) {
   return a;
 }
 static bool empty(const alexnet_group_norm_t* cfg) { return cfg->n == 0 || cfg->hw == 0; }
-// The largest scratch of the ways to cut rows into threads: with one value a thread (tiny or in-place odd rows) or vectors
-static size_t gn_ws(const alexnet_group_norm_t* cfg) {
-  if (empty(cfg)) return 0;
-  size_t most = 0;
-  for (int V : {1, kBackwardVec, 16 / (int)type_size(cfg->type)})
-    for (int b = 0; b < 2; ++b) {
-      GnArgs a = gn_args(cfg);
-      split(a, V, b);
-      most = std::max(most, (size_t)a.n * a.chunks * 2 * a.c * sizeof(float));
-    }
-  return align256(most) + align256((size_t)cfg->n * cfg->groups * 2 * sizeof(float));
+static SlabPlan forward_plan(const GnArgs& a, size_t size, bool keep) {
+  return slab_plan(a.n, a.hw, a.c, a.groups, 16 / (int)size, kForwardRegs, keep, 1, 12);
 }
+static SlabPlan backward_plan(const GnArgs& a) {
+  return slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, false, 2, 16);
+}
+// Scratch: sums per chunk and channel, then the groups' statistics; for chunks the larger of the two ways to cut rows into
+// threads (one value a thread: tiny or in-place odd rows).
+static size_t stat_bytes(const GnArgs& a) { return align256((size_t)a.n * a.groups * 2 * sizeof(float)); }
+static size_t chunk_bytes(const GnArgs& args, int V, bool keep) {
+  size_t most = 0;
+  for (int v : {1, V}) {
+    GnArgs a = args;
+    split(a, v, keep);
+    most = std::max(most, (size_t)a.n * a.chunks * 2 * a.c * sizeof(float));
+  }
+  return align256(most);
+}
+static size_t forward_ws(const alexnet_group_norm_t* cfg, bool keep) {
+  const GnArgs a = gn_args(cfg);
+  const size_t size = type_size(cfg->type);
+  if (empty(cfg) || forward_plan(a, size, keep).groups) return 0;
+  return chunk_bytes(a, 16 / (int)size, keep) + stat_bytes(a);
+}
+static size_t backward_ws(const alexnet_group_norm_t* cfg) {
+  const GnArgs a = gn_args(cfg);
+  if (empty(cfg)) return 0;
+  if (backward_plan(a).groups) return a.n > 1 ? align256((size_t)a.n * 2 * a.c * sizeof(float)) : 0;
+  return chunk_bytes(a, kBackwardVec, false) + stat_bytes(a);
+}
+// the chunks' sums from the start, the statistics at the end
 static void gn_scratch(GnArgs& a, void* ws, size_t bytes) {
   a.part = (float*)ws;
-  a.stat = (float*)((char*)ws + bytes - align256((size_t)a.n * a.groups * 2 * sizeof(float)));
+  a.stat = (float*)((char*)ws + (bytes >= stat_bytes(a) ? bytes - stat_bytes(a) : 0));
+}
+static int check_scratch(const char* who, const void* ws, size_t bytes, size_t need) {
+  if (!need) return ALEXNET_OK;
+  AX_REQUIRE(ws && bytes >= need, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, ws ? bytes : (size_t)0, need);
+  AX_REQUIRE((uintptr_t)ws % 256 == 0, ALEXNET_EALIGN, "%s: workspace is not 256-byte aligned", who);
+  return ALEXNET_OK;
 }
 
 #define GN_LAUNCH(kernel, grid, block, st, a)                            \
@@ -515,13 +540,13 @@ static int gn_backward(GnArgs a, hipStream_t st) {
 template <typename T>
 static int gn_forward_type(const GnArgs& a, int type, int keep, hipStream_t st) {
   constexpr int V = 16 / sizeof(T);
-  const SlabPlan p = slab_plan(a.n, a.hw, a.c, a.groups, V, kForwardRegs, keep != kKeepNone, 1, 12);
+  const SlabPlan p = forward_plan(a, sizeof(T), keep != kKeepNone);
   if (p.groups) return launch_gn_slab_forward(a, p, type, keep, st);
   return a.c >= V && (a.c % V == 0 || a.x != a.out) ? gn_forward<T, V>(a, keep, st) : gn_forward<T, 1>(a, keep, st);
 }
 template <typename T, int SRC>
 static int gn_backward_src(GnArgs a, int type, hipStream_t st) {
-  const SlabPlan p = slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, false, 2, 16);
+  const SlabPlan p = backward_plan(a);
   if (p.groups) {
     AX_TRY(launch_gn_slab_backward(a, p, type, SRC, st));
     a.chunks = 1;
@@ -551,10 +576,11 @@ using namespace ax;
 
 extern "C" {
 
-int alexnet_group_norm_query(const alexnet_group_norm_t* cfg, size_t* workspace_bytes) {
+int alexnet_group_norm_query(const alexnet_group_norm_t* cfg, int32_t keep, size_t* forward_bytes, size_t* backward_bytes) {
   AX_TRY(gn_check(cfg, "alexnet_group_norm_query"));
-  AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_group_norm_query: null argument");
-  *workspace_bytes = gn_ws(cfg);
+  AX_REQUIRE(forward_bytes && backward_bytes, ALEXNET_EINVAL, "alexnet_group_norm_query: null argument");
+  *forward_bytes = forward_ws(cfg, keep != 0);
+  *backward_bytes = backward_ws(cfg);
   return ALEXNET_OK;
 }
 
@@ -563,7 +589,7 @@ int alexnet_group_norm_forward(const alexnet_group_norm_t* cfg, const void* d_x,
                                const alexnet_checkpoint_t* keep, void* d_workspace, size_t workspace_bytes, void* stream) {
   const char* who = "alexnet_group_norm_forward";
   AX_TRY(gn_check(cfg, who));
-  const size_t size = type_size(cfg->type), need = gn_ws(cfg);
+  const size_t size = type_size(cfg->type), need = forward_ws(cfg, keep != nullptr);
   hipStream_t st = (hipStream_t)stream;
   if (empty(cfg)) return gn_fill_empty(cfg, d_mean, d_rstd, nullptr, nullptr, st);
   AX_REQUIRE(d_x && d_y, ALEXNET_EINVAL, "%s: null argument", who);
@@ -571,8 +597,7 @@ int alexnet_group_norm_forward(const alexnet_group_norm_t* cfg, const void* d_x,
   AX_REQUIRE(((uintptr_t)d_x | (uintptr_t)d_y) % size == 0 && ((uintptr_t)d_gamma | (uintptr_t)d_beta | (uintptr_t)d_mean | (uintptr_t)d_rstd) % 4 == 0,
              ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
   if (keep) AX_TRY(check_checkpoint(keep, who));
-  AX_REQUIRE(workspace_bytes >= need && d_workspace, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, d_workspace ? workspace_bytes : (size_t)0, need);
-  AX_REQUIRE((uintptr_t)d_workspace % 256 == 0, ALEXNET_EALIGN, "%s: workspace is not 256-byte aligned", who);
+  AX_TRY(check_scratch(who, d_workspace, workspace_bytes, need));
   GnArgs a = gn_args(cfg);
   a.x = d_x;
   a.ld_x = ld_x;
@@ -599,7 +624,7 @@ int alexnet_group_norm_backward(const alexnet_group_norm_t* cfg, const void* d_x
                                 float* d_dgamma, float* d_dbeta, void* d_workspace, size_t workspace_bytes, void* stream) {
   const char* who = "alexnet_group_norm_backward";
   AX_TRY(gn_check(cfg, who));
-  const size_t size = type_size(cfg->type), need = gn_ws(cfg);
+  const size_t size = type_size(cfg->type), need = backward_ws(cfg);
   hipStream_t st = (hipStream_t)stream;
   if (empty(cfg)) return gn_fill_empty(cfg, nullptr, nullptr, d_dgamma, d_dbeta, st);
   AX_REQUIRE(d_dy && d_mean && d_rstd && d_dx, ALEXNET_EINVAL, "%s: null argument", who);
@@ -609,8 +634,7 @@ int alexnet_group_norm_backward(const alexnet_group_norm_t* cfg, const void* d_x
                  ((uintptr_t)d_gamma | (uintptr_t)d_beta | (uintptr_t)d_mean | (uintptr_t)d_rstd | (uintptr_t)d_dgamma | (uintptr_t)d_dbeta) % 4 == 0,
              ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
   if (kept) AX_TRY(check_checkpoint(kept, who));
-  AX_REQUIRE(workspace_bytes >= need && d_workspace, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, d_workspace ? workspace_bytes : (size_t)0, need);
-  AX_REQUIRE((uintptr_t)d_workspace % 256 == 0, ALEXNET_EALIGN, "%s: workspace is not 256-byte aligned", who);
+  AX_TRY(check_scratch(who, d_workspace, workspace_bytes, need));
   GnArgs a = gn_args(cfg);
   a.x = d_x;
   a.ld_x = ld_x;

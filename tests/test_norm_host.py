@@ -31,9 +31,9 @@ def cfg(B, **kw):
     (dict(c=(1 << 20) + 8), "ESHAPE"), (dict(hw=(1 << 28) + 1), "ESHAPE"), (dict(n=1 << 21, groups=2), "ESHAPE"),
     (dict(n=1 << 20, c=1 << 13, groups=1), "ESHAPE")])
 def test_configurations_that_are_refused(B, change, code):
-    ws = C.c_size_t()
+    ws, ws2 = C.c_size_t(), C.c_size_t()
     c = cfg(B, **change)
-    for rc in (B._lib.alexnet_group_norm_query(c, ws),
+    for rc in (B._lib.alexnet_group_norm_query(c, 0, ws, ws2),
                B._lib.alexnet_group_norm_forward(c, 256, 1 << 20, None, None, 512, 1 << 20, None, None, None, 1024, 1 << 40, None),
                B._lib.alexnet_group_norm_backward(c, 256, 1 << 20, None, 512, 1 << 20, 256, 256, None, None, 512, 1 << 20, None, None,
                                                   1024, 1 << 40, None)):
@@ -41,17 +41,20 @@ def test_configurations_that_are_refused(B, change, code):
 
 
 def test_arguments_that_are_refused(B):
-    ws = C.c_size_t()
-    c = cfg(B)
-    assert B._lib.alexnet_group_norm_query(None, ws) == B.EINVAL and B._lib.alexnet_group_norm_query(c, None) == B.EINVAL
-    assert B._lib.alexnet_group_norm_query(c, ws) == B.OK
-    need = ws.value
+    ws, ws2 = C.c_size_t(), C.c_size_t()
+    q = B._lib.alexnet_group_norm_query
+    assert q(None, 0, ws, ws2) == q(cfg(B), 0, None, ws2) == q(cfg(B), 0, ws, None) == B.EINVAL
+    # maps that no workgroup holds: both passes need scratch
+    c = cfg(B, n=3, hw=100000)
+    assert q(c, 0, ws, ws2) == B.OK
+    need, need_b = ws.value, ws2.value
+    assert need > 0 and need_b > 0
     kept = B.CheckpointArg(256, 512, 0)
 
-    def forward(x=256, ld_x=8, gamma=None, beta=None, y=512, ld_y=8, mean=None, rstd=None, keep=None, work=1024, size=need, conf=c):
+    def forward(x=256, ld_x=8, gamma=None, beta=None, y=512, ld_y=8, mean=None, rstd=None, keep=None, work=1024, size=1 << 40, conf=c):
         return B._lib.alexnet_group_norm_forward(conf, x, ld_x, gamma, beta, y, ld_y, mean, rstd, keep, work, size, None)
 
-    def backward(x=256, ld_x=8, kept=None, dy=512, ld_dy=8, mean=256, rstd=256, dx=512, ld_dx=8, dgamma=None, work=1024, size=need, conf=c):
+    def backward(x=256, ld_x=8, kept=None, dy=512, ld_dy=8, mean=256, rstd=256, dx=512, ld_dx=8, dgamma=None, work=1024, size=1 << 40, conf=c):
         return B._lib.alexnet_group_norm_backward(conf, x, ld_x, kept, dy, ld_dy, mean, rstd, None, None, dx, ld_dx, dgamma, None, work,
                                                   size, None)
 
@@ -61,10 +64,11 @@ def test_arguments_that_are_refused(B):
     assert forward(x=257, conf=cfg(B, type=1)) == B.EALIGN
     assert forward(keep=B.CheckpointArg(None, 512, 0)) == forward(keep=B.CheckpointArg(256, None, 0)) == B.EINVAL
     assert forward(keep=B.CheckpointArg(256, 512, 2)) == forward(keep=B.CheckpointArg(256, 512, -1)) == B.EINVAL
-    if need:
-        assert forward(size=need - 1) == forward(work=None) == B.ENOMEM and "workspace" in B.last_error()
-        assert forward(work=1028) == backward(work=1028) == B.EALIGN
-        assert backward(size=need - 1) == backward(work=None) == B.ENOMEM
+    assert forward(size=need - 1) == forward(work=None) == B.ENOMEM and "workspace" in B.last_error()
+    assert forward(work=1028) == backward(work=1028) == B.EALIGN
+    assert backward(size=need_b - 1) == backward(work=None) == B.ENOMEM
+    # one picture whose groups fit a workgroup: none
+    assert q(cfg(B, n=1), 1, ws, ws2) == B.OK and ws.value == 0 and ws2.value == 0
     assert backward(x=None) == backward(kept=kept) == backward(dy=None) == backward(mean=None) == backward(rstd=None) == B.EINVAL
     assert backward(dx=None) == B.EINVAL
     assert backward(ld_x=7) == backward(ld_dy=7) == backward(ld_dx=7) == backward(x=None, kept=kept, ld_dy=7) == B.ESHAPE
@@ -119,7 +123,7 @@ def test_the_binding_refuses_tensors_of_the_wrong_kind(B):
     with pytest.raises(ValueError, match="device tensor"):
         B.checkpoint_unpack(B.Checkpoint(torch.zeros(4, 40, dtype=torch.int8), torch.zeros(4, 2, dtype=torch.uint8)))
     with pytest.raises(ValueError, match="activation"):
-        B._activation("tanh")
+        B._group_norm_cfg(1, 4, 8, 2, 0, "tanh", 1e-5, False)
 
 
 def test_the_reference_codes_by_brute_force():
