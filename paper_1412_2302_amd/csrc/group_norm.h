@@ -33,7 +33,10 @@ struct GnArgs {
   // A launch over (column blocks, chunks of pixels, pictures) in one dimension, or over (slabs of whole groups, pictures).
   int colvecs, cols, rpi, col_blocks, chunk, chunks;  // cols: threads of a row (whole blocks of 32 where a checkpoint is written)
   int slab_groups, slabs;
-  float *part, *stat;  // [n][chunks][2][c]; [n][groups][2]
+  // Scratch.  part [n][chunks][2][slots]: what a chunk found for a group, per block of columns that the group lies in; that of
+  // group g in block b is slot g + b (going along the channels either the group or the block changes, so no two share a slot).
+  // part_c [n][chunks][2][c]: the same per channel (gradients only).  stat [n][groups][2].
+  float *part, *part_c, *stat;
 };
 
 // V channels from c on, of which the first `dup` are another thread's too
@@ -45,6 +48,8 @@ __device__ __forceinline__ Vec vec_of(int v, int c0, int width) {
   const int at = min(v * V, width - V);
   return Vec{c0 + at, v * V - at};
 }
+
+__host__ __device__ inline int slots_of(const GnArgs& a) { return a.groups + a.col_blocks - 1; }
 
 struct Spot {  // a thread's place in a launch over chunks
   int n, p0, p1, row, v, chunk;

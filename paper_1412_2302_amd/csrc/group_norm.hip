@@ -15,6 +15,29 @@ namespace ax {
 // ---- statistics -----------------------------------------------------------------
 constexpr int kUnroll = 4;  // pixels of a thread's loads in flight
 
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// The channels of this workgroup's block of columns, [lo, hi), and f(group, first, end) for every group that has some of them:
+// by one thread where groups are narrow (lane 0 of 1), else by the lanes of a wave.
+struct Columns {
+  int block, lo, hi;
+};
+template <int V>
+__device__ __forceinline__ Columns columns(const GnArgs& a, int b) {
+  const int block = b % a.col_blocks, width = a.cols * V;
+  return Columns{block, block * width, min(a.c, (block + 1) * width)};
+}
+template <typename F>
+__device__ __forceinline__ void each_group(const GnArgs& a, const Columns& c, F f) {
+  const int g0 = c.lo / a.cpg, g1 = (c.hi - 1) / a.cpg, team = a.cpg <= 16 ? 1 : 64, t = threadIdx.x;
+  for (int g = g0 + t / team; g <= g1; g += 256 / team) f(g, max(g * a.cpg, c.lo), min((g + 1) * a.cpg, c.hi), t % team, team);
+}
+__device__ __forceinline__ float team_sum(float v, int team) { return team == 1 ? v : wave_sum(v); }
+
 // Per channel and chunk of pixels the mean and the sum of squares about it.  Four pixels at a time: their own mean and squares
 // in registers, then joined to the running pair, so no pixel's size spoils the sum of the others.
 template <typename T, int V, int KEEP>
@@ -76,35 +99,55 @@ __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
     }
   }
   __syncthreads();
-  // one thread per channel joins the rows' pairs
+  // one thread per channel joins the rows' pairs, then one or a wave per group the channels'
   const int pixels = s.p1 - s.p0, width = a.cols * V;
-  for (int j = threadIdx.x; j < width; j += 256) {
-    const int at = ((int)blockIdx.x % a.col_blocks) * a.cols + j / V;
-    const Vec vj = vec_of<V>(at, 0, a.c);
-    if (at >= a.colvecs || j % V < vj.dup) continue;
-    const int ch = vj.c + j % V;
+  const Columns c = columns<V>(a, blockIdx.x);
+  float pm[V], pq[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int j = threadIdx.x + 256 * k;
+    if (j >= width) break;
     float sum = 0.f;
     for (int r = 0; r < a.rpi; ++r) {
-      const int k = r < pixels ? (pixels - r + a.rpi - 1) / a.rpi : 0;
-      sum = __builtin_fmaf((float)k, sm[r * width + j], sum);
+      const int cnt = r < pixels ? (pixels - r + a.rpi - 1) / a.rpi : 0;
+      sum = __builtin_fmaf((float)cnt, sm[r * width + j], sum);
     }
-    const float mean = sum / (float)max(pixels, 1);
-    float sq2 = 0.f;
+    pm[k] = sum / (float)pixels;
+    pq[k] = 0.f;
     for (int r = 0; r < a.rpi; ++r) {
-      const int k = r < pixels ? (pixels - r + a.rpi - 1) / a.rpi : 0;
-      const float d = sm[r * width + j] - mean;
-      if (k) sq2 += __builtin_fmaf(d * d, (float)k, sq[r * width + j]);
+      const int cnt = r < pixels ? (pixels - r + a.rpi - 1) / a.rpi : 0;
+      const float d = sm[r * width + j] - pm[k];
+      if (cnt) pq[k] += __builtin_fmaf(d * d, (float)cnt, sq[r * width + j]);
     }
-    float* const part = a.part + ((long)s.n * a.chunks + s.chunk) * 2 * a.c;
-    part[ch] = mean;
-    part[a.c + ch] = sq2;
   }
-}
-
-__device__ __forceinline__ float wave_sum(float v) {
+  __syncthreads();
 #pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  for (int k = 0; k < V; ++k) {
+    const int j = threadIdx.x + 256 * k;
+    if (j >= width) break;
+    const int at = c.block * a.cols + j / V;
+    const Vec vj = vec_of<V>(at, 0, a.c);
+    if (at >= a.colvecs || j % V < vj.dup) continue;
+    sm[vj.c + j % V - c.lo] = pm[k];
+    sq[vj.c + j % V - c.lo] = pq[k];
+  }
+  __syncthreads();
+  const int slots = slots_of(a);
+  float* const part = a.part + ((long)s.n * a.chunks + s.chunk) * 2 * slots;
+  each_group(a, c, [&](int g, int first, int end, int lane, int team) {
+    float sum = 0.f, total = 0.f;
+    for (int ch = first + lane; ch < end; ch += team) sum += sm[ch - c.lo];
+    const float mean = team_sum(sum, team) / (float)(end - first);
+    for (int ch = first + lane; ch < end; ch += team) {
+      const float d = sm[ch - c.lo] - mean;
+      total += __builtin_fmaf(d * d, (float)pixels, sq[ch - c.lo]);
+    }
+    total = team_sum(total, team);
+    if (lane == 0) {
+      part[g + c.block] = mean;
+      part[slots + g + c.block] = total;
+    }
+  });
 }
 
 // the sum over a workgroup of 256; everyone gets it
@@ -116,42 +159,49 @@ __device__ __forceinline__ float group_sum(float v, float* lds) {
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// A team of threads (a wave where a group has few terms, else the workgroup) joins the pairs of a group's channels and chunks,
-// four to a thread and trip so that their loads are in flight together.
+// the blocks of columns that a group lies in
+struct Span {
+  int first, blocks;
+};
+__device__ __forceinline__ Span span_of(const GnArgs& a, int g, int width) {
+  const int first = g * a.cpg / width;
+  return Span{first, ((g + 1) * a.cpg - 1) / width - first + 1};
+}
+
+// A team of threads (a wave where a group has few terms, else the workgroup) joins the pairs of a group's chunks and blocks of
+// columns, four to a thread and trip so that their loads are in flight together.  width: channels of a block.
 template <int TEAM>
-__global__ void __launch_bounds__(256) gn_statistics_kernel(GnArgs a) {
+__global__ void __launch_bounds__(256) gn_statistics_kernel(GnArgs a, int width) {
   __shared__ float lds[4];
   const int id = blockIdx.x * (256 / TEAM) + (int)threadIdx.x / TEAM, t = threadIdx.x % TEAM;
   if (TEAM == 64 && id >= a.n * a.groups) return;
   const auto total_of = [&](float v) { return TEAM == 64 ? wave_sum(v) : group_sum(v, lds); };
-  const int n = id / a.groups, g = id - n * a.groups;
-  const float* const part = a.part + (long)n * a.chunks * 2 * a.c + (long)g * a.cpg;
+  const int n = id / a.groups, g = id - n * a.groups, slots = slots_of(a);
+  const Span span = span_of(a, g, width);
+  const float* const part = a.part + (long)n * a.chunks * 2 * slots + g + span.first;
   const float total = (float)a.hw * (float)a.cpg;
-  const int terms = a.chunks * a.cpg;
-  float sum = 0.f;
+  const int terms = a.chunks * span.blocks;
+  const auto pair = [&](int i, float& m, float& q, float& w) {
+    const int at = min(i, terms - 1), k = at / span.blocks, b = at - k * span.blocks;
+    const int c0 = max(g * a.cpg, (span.first + b) * width), c1 = min((g + 1) * a.cpg, (span.first + b + 1) * width);
+    m = part[(long)k * 2 * slots + b];
+    q = part[(long)k * 2 * slots + slots + b];
+    w = i < terms ? (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) * (float)(c1 - c0) : 0.f;
+  };
+  float sum = 0.f, sq = 0.f;
   for (int i0 = t; i0 < terms; i0 += 4 * TEAM) {
-    float m[4], w[4];
+    float m[4], q[4], w[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = min(i0 + TEAM * u, terms - 1), k = i / a.cpg, j = i - k * a.cpg;
-      m[u] = part[(long)k * 2 * a.c + j];
-      w[u] = i0 + TEAM * u < terms ? (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) : 0.f;
-    }
+    for (int u = 0; u < 4; ++u) pair(i0 + TEAM * u, m[u], q[u], w[u]);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
       if (w[u] != 0.f) sum = __builtin_fmaf(w[u], m[u], sum);
   }
   const float mean = total_of(sum) / total;
-  float sq = 0.f;
   for (int i0 = t; i0 < terms; i0 += 4 * TEAM) {
-    float m[4], w[4], q[4];
+    float m[4], q[4], w[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = min(i0 + TEAM * u, terms - 1), k = i / a.cpg, j = i - k * a.cpg;
-      m[u] = part[(long)k * 2 * a.c + j];
-      q[u] = part[(long)k * 2 * a.c + a.c + j];
-      w[u] = i0 + TEAM * u < terms ? (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) : 0.f;
-    }
+    for (int u = 0; u < 4; ++u) pair(i0 + TEAM * u, m[u], q[u], w[u]);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const float d = m[u] - mean;
@@ -253,46 +303,72 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
   }
   __syncthreads();
   const int width = a.cols * V;
-  for (int j = threadIdx.x; j < width; j += 256) {
-    const int at = ((int)blockIdx.x % a.col_blocks) * a.cols + j / V;
+  const Columns c = columns<V>(a, blockIdx.x);
+  float* const part_c = a.part_c + ((long)s.n * a.chunks + s.chunk) * 2 * a.c;
+  float pb[V], pg[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int j = threadIdx.x + 256 * k;
+    pb[k] = pg[k] = 0.f;
+    if (j >= width) break;
+    for (int r = 0; r < a.rpi; ++r) {
+      pb[k] += sm[r * width + j];
+      pg[k] += sq[r * width + j];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int j = threadIdx.x + 256 * k;
+    if (j >= width) break;
+    const int at = c.block * a.cols + j / V;
     const Vec vj = vec_of<V>(at, 0, a.c);
     if (at >= a.colvecs || j % V < vj.dup) continue;
     const int ch = vj.c + j % V;
-    float b = 0.f, g = 0.f;
-    for (int r = 0; r < a.rpi; ++r) {
-      b += sm[r * width + j];
-      g += sq[r * width + j];
-    }
-    float* const part = a.part + ((long)s.n * a.chunks + s.chunk) * 2 * a.c;
-    part[ch] = b;
-    part[a.c + ch] = g;
+    const float w = a.gamma ? a.gamma[ch] : 1.f;
+    part_c[ch] = pb[k];
+    part_c[a.c + ch] = pg[k];
+    sm[ch - c.lo] = w * pb[k];
+    sq[ch - c.lo] = w * pg[k];
   }
+  __syncthreads();
+  const int slots = slots_of(a);
+  float* const part = a.part + ((long)s.n * a.chunks + s.chunk) * 2 * slots;
+  each_group(a, c, [&](int g, int first, int end, int lane, int team) {
+    float sb = 0.f, sg = 0.f;
+    for (int ch = first + lane; ch < end; ch += team) {
+      sb += sm[ch - c.lo];
+      sg += sq[ch - c.lo];
+    }
+    sb = team_sum(sb, team);
+    sg = team_sum(sg, team);
+    if (lane == 0) {
+      part[g + c.block] = sb;
+      part[slots + g + c.block] = sg;
+    }
+  });
 }
 
-// A group whose terms (chunks times channels) are few is a wave's work, not a workgroup's: 4096 groups of 48 terms took 21 us
-// with a workgroup of 1024 each.
-static bool few_terms(const GnArgs& a) { return (long)a.chunks * a.cpg <= 512; }
-
 // Workgroups [0, group_blocks): the means that dx subtracts, mean(gamma dz) and mean(gamma dz xhat), sixteen groups each where
-// SHORT (a wave to a group), else one; then, sixteen channels a workgroup, the sums over pictures and chunks that are dbeta and
-// dgamma.
+// SHORT (a wave to a group), else one; then, eight channels a workgroup, the sums over pictures and chunks that are dbeta and
+// dgamma.  width: channels of a block of columns.
 template <bool SHORT>
-__global__ void __launch_bounds__(1024) gn_grad_totals_kernel(GnArgs a, int group_blocks) {
+__global__ void __launch_bounds__(1024) gn_grad_totals_kernel(GnArgs a, int group_blocks, int width) {
   __shared__ float sb[1024], sg[1024];
   const int t = threadIdx.x;
   float b = 0.f, g = 0.f;
   if ((int)blockIdx.x < group_blocks) {
     const int id = SHORT ? blockIdx.x * 16 + (t >> 6) : blockIdx.x, team = SHORT ? 64 : 1024, lane = SHORT ? t & 63 : t;
     if (SHORT && id >= a.n * a.groups) return;
-    const int n = id / a.groups, group = id - n * a.groups;
-    const float* const part = a.part + (long)n * a.chunks * 2 * a.c + (long)group * a.cpg;
-    const int terms = a.chunks * a.cpg;
+    const int n = id / a.groups, group = id - n * a.groups, slots = slots_of(a);
+    const Span span = span_of(a, group, width);
+    const float* const part = a.part + (long)n * a.chunks * 2 * slots + group + span.first;
+    const int terms = a.chunks * span.blocks;
 #pragma unroll 4
     for (int i = lane; i < terms; i += team) {
-      const int k = i / a.cpg, j = i - k * a.cpg;
-      const float w = a.gamma ? a.gamma[group * a.cpg + j] : 1.f;
-      b = __builtin_fmaf(w, part[(long)k * 2 * a.c + j], b);
-      g = __builtin_fmaf(w, part[(long)k * 2 * a.c + a.c + j], g);
+      const int k = i / span.blocks, j = i - k * span.blocks;
+      b += part[(long)k * 2 * slots + j];
+      g += part[(long)k * 2 * slots + slots + j];
     }
     b = wave_sum(b);
     g = wave_sum(g);
@@ -312,41 +388,44 @@ __global__ void __launch_bounds__(1024) gn_grad_totals_kernel(GnArgs a, int grou
     }
     return;
   }
-  const int ch = ((int)blockIdx.x - group_blocks) * 16 + (t & 15);
+  const int ch = ((int)blockIdx.x - group_blocks) * 8 + (t & 7);
   const long rows = (long)a.n * a.chunks;
   if (ch < a.c) {
 #pragma unroll 8
-    for (long r = t >> 4; r < rows; r += 64) {
-      b += a.part[r * 2 * a.c + ch];
-      g += a.part[r * 2 * a.c + a.c + ch];
+    for (long r = t >> 3; r < rows; r += 128) {
+      b += a.part_c[r * 2 * a.c + ch];
+      g += a.part_c[r * 2 * a.c + a.c + ch];
     }
   }
   sb[t] = b;
   sg[t] = g;
   __syncthreads();
 #pragma unroll
-  for (int d = 512; d >= 16; d >>= 1) {
+  for (int d = 512; d >= 8; d >>= 1) {
     if (t < d) {
       sb[t] += sb[t + d];
       sg[t] += sg[t + d];
     }
     __syncthreads();
   }
-  if (t < 16 && ch < a.c) {
+  if (t < 8 && ch < a.c) {
     if (a.dbeta) a.dbeta[ch] = sb[t];
     if (a.dgamma) a.dgamma[ch] = sg[t];
   }
 }
-static int launch_totals(const GnArgs& a, bool groups, hipStream_t st) {
-  const bool few = few_terms(a);
+// a group whose terms are few is a wave's work, not a workgroup's: 4096 groups of 48 terms took 21 us with 1024 threads each
+static bool few_terms(const GnArgs& a, int width) { return (long)a.chunks * (a.cpg / width + 2) <= 512; }
+static int launch_totals(const GnArgs& a, bool groups, int width, hipStream_t st) {
+  const bool few = few_terms(a, width);
   const int group_blocks = !groups ? 0 : few ? ceil_div((long)a.n * a.groups, 16) : a.n * a.groups;
-  const int channel_blocks = a.dbeta || a.dgamma ? ceil_div(a.c, 16) : 0;
+  const int channel_blocks = a.dbeta || a.dgamma ? ceil_div(a.c, 8) : 0;
   if (group_blocks + channel_blocks == 0) return ALEXNET_OK;
   KernelScope ks("gn_grad_totals", 0, 0, st);
+  const dim3 grid((unsigned)(group_blocks + channel_blocks)), block(1024);
   if (few)
-    hipLaunchKernelGGL(gn_grad_totals_kernel<true>, dim3((unsigned)(group_blocks + channel_blocks)), dim3(1024), 0, st, a, group_blocks);
+    hipLaunchKernelGGL(gn_grad_totals_kernel<true>, grid, block, 0, st, a, group_blocks, width);
   else
-    hipLaunchKernelGGL(gn_grad_totals_kernel<false>, dim3((unsigned)(group_blocks + channel_blocks)), dim3(1024), 0, st, a, group_blocks);
+    hipLaunchKernelGGL(gn_grad_totals_kernel<false>, grid, block, 0, st, a, group_blocks, width);
   AX_LAUNCH_CHECK();
   return ALEXNET_OK;
 }
@@ -417,7 +496,7 @@ static void split(GnArgs& a, int V, bool blocks32) {
   a.col_blocks = ceil_div(a.colvecs, a.cols);
   const long round = (long)a.rpi * kUnroll;
   const long want = std::max<long>(1, 2048 / ((long)a.n * a.col_blocks));  // chunks of a picture
-  a.chunk = (int)std::min<long>(a.hw, std::max<long>(2 * round, ceil_div(ceil_div(a.hw, want), round) * round));
+  a.chunk = (int)std::min<long>(a.hw, std::max<long>(4 * round, ceil_div(ceil_div(a.hw, want), round) * round));
   a.chunks = ceil_div(a.hw, a.chunk);
 }
 static int gn_check(const alexnet_group_norm_t* cfg, const char* who) {
@@ -455,12 +534,12 @@ static SlabPlan backward_plan(const GnArgs& a) {
 // Scratch: sums per chunk and channel, then the groups' statistics; for chunks the larger of the two ways to cut rows into
 // threads (one value a thread: tiny or in-place odd rows).
 static size_t stat_bytes(const GnArgs& a) { return align256((size_t)a.n * a.groups * 2 * sizeof(float)); }
-static size_t chunk_bytes(const GnArgs& args, int V, bool keep) {
+static size_t chunk_bytes(const GnArgs& args, int V, bool keep, bool grads) {
   size_t most = 0;
   for (int v : {1, V}) {
     GnArgs a = args;
     split(a, v, keep);
-    most = std::max(most, (size_t)a.n * a.chunks * 2 * a.c * sizeof(float));
+    most = std::max(most, (size_t)a.n * a.chunks * 2 * (slots_of(a) + (grads ? a.c : 0)) * sizeof(float));
   }
   return align256(most);
 }
@@ -468,13 +547,13 @@ static size_t forward_ws(const alexnet_group_norm_t* cfg, bool keep) {
   const GnArgs a = gn_args(cfg);
   const size_t size = type_size(cfg->type);
   if (empty(cfg) || forward_plan(a, size, keep).groups) return 0;
-  return chunk_bytes(a, 16 / (int)size, keep) + stat_bytes(a);
+  return chunk_bytes(a, 16 / (int)size, keep, false) + stat_bytes(a);
 }
 static size_t backward_ws(const alexnet_group_norm_t* cfg) {
   const GnArgs a = gn_args(cfg);
   if (empty(cfg)) return 0;
   if (backward_plan(a).groups) return a.n > 1 ? align256((size_t)a.n * 2 * a.c * sizeof(float)) : 0;
-  return chunk_bytes(a, kBackwardVec, false) + stat_bytes(a);
+  return chunk_bytes(a, kBackwardVec, false, true) + stat_bytes(a);
 }
 // the chunks' sums from the start, the statistics at the end
 static void gn_scratch(GnArgs& a, void* ws, size_t bytes) {
@@ -510,10 +589,12 @@ static int gn_forward(GnArgs a, int keep, hipStream_t st) {
   }
   {
     KernelScope ks("gn_statistics", 0, 0, st);
-    if (few_terms(a))
-      GN_LAUNCH(gn_statistics_kernel<64>, ceil_div((long)a.n * a.groups, 4), 256, st, a);
+    const int width = a.cols * V;
+    if (few_terms(a, width))
+      hipLaunchKernelGGL(gn_statistics_kernel<64>, dim3((unsigned)ceil_div((long)a.n * a.groups, 4)), dim3(256), 0, st, a, width);
     else
-      GN_LAUNCH(gn_statistics_kernel<256>, (long)a.n * a.groups, 256, st, a);
+      hipLaunchKernelGGL(gn_statistics_kernel<256>, dim3((unsigned)(a.n * a.groups)), dim3(256), 0, st, a, width);
+    AX_LAUNCH_CHECK();
   }
   KernelScope ks("gn_apply", 0, 2 * bytes, st);
   GN_LAUNCH((gn_apply_kernel<T, V>), blocks, 256, st, a);
@@ -523,13 +604,14 @@ static int gn_forward(GnArgs a, int keep, hipStream_t st) {
 template <typename T, int V, int SRC>
 static int gn_backward(GnArgs a, hipStream_t st) {
   split(a, V, false);
+  a.part_c = a.part + (size_t)a.n * a.chunks * 2 * slots_of(a);
   const long blocks = (long)a.n * a.chunks * a.col_blocks;
   const double values = (double)a.n * a.hw * a.c, in = values * (sizeof(T) + (SRC == SRC_TENSOR ? sizeof(T) : 1));
   {
     KernelScope ks("gn_grad_sums", 0, in, st);
     GN_LAUNCH((gn_grad_sums_kernel<T, V, SRC>), blocks, 256, st, a);
   }
-  AX_TRY(launch_totals(a, true, st));
+  AX_TRY(launch_totals(a, true, a.cols * V, st));
   KernelScope ks("gn_grad_apply", 0, in + values * sizeof(T), st);
   GN_LAUNCH((gn_grad_apply_kernel<T, V, SRC>), blocks, 256, st, a);
   return ALEXNET_OK;
@@ -548,9 +630,10 @@ template <typename T, int SRC>
 static int gn_backward_src(GnArgs a, int type, hipStream_t st) {
   const SlabPlan p = backward_plan(a);
   if (p.groups) {
+    a.part_c = a.part;
+    a.chunks = a.col_blocks = 1;
     AX_TRY(launch_gn_slab_backward(a, p, type, SRC, st));
-    a.chunks = 1;
-    return a.n > 1 ? launch_totals(a, false, st) : ALEXNET_OK;
+    return a.n > 1 ? launch_totals(a, false, a.c, st) : ALEXNET_OK;
   }
   constexpr int V = kBackwardVec;
   return a.c >= V && (a.c % V == 0 || (a.dy != a.out && a.x != a.out)) ? gn_backward<T, V, SRC>(a, st) : gn_backward<T, 1, SRC>(a, st);

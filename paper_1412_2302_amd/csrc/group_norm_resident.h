@@ -9,7 +9,7 @@ namespace ax {
 // eight 16-bit ones what it knows per channel would take half its registers.
 constexpr int kForwardRegs = 16, kBackwardRegs = 8, kBackwardVec = 4;
 int launch_gn_slab_forward(GnArgs a, const SlabPlan& p, int type, int keep, hipStream_t st);
-// a.part: [n][2][c], untouched for one picture
+// a.part_c: [n][2][c], untouched for one picture
 int launch_gn_slab_backward(GnArgs a, const SlabPlan& p, int type, int src, hipStream_t st);
 
 }  // namespace ax

@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(1024) gn_slab_forward_kernel(GnArgs a) {
   }
 }
 
-// sums of a slab's channels go to part [n][2][c] (one picture: to dbeta and dgamma themselves)
+// sums of a slab's channels go to part_c [n][2][c] (one picture: to dbeta and dgamma themselves)
 template <typename T, int V, int SRC, int R>
 __global__ void __launch_bounds__(1024) gn_slab_backward_kernel(GnArgs a) {
   extern __shared__ float lds[];  // threads * V twice, then as many as groups twice
@@ -244,8 +244,8 @@ __global__ void __launch_bounds__(1024) gn_slab_backward_kernel(GnArgs a) {
   float* const totals = lds + 2 * stride;
   const float gamma_t = a.gamma && (int)threadIdx.x < w ? a.gamma[s.c0 + threadIdx.x] : 1.f;
   channel_sums<V, 2>(a, s, v, sums, lds);
-  float* const out_b = a.n == 1 ? a.dbeta : a.part + (long)s.n * 2 * a.c;
-  float* const out_g = a.n == 1 ? a.dgamma : a.part + (long)s.n * 2 * a.c + a.c;
+  float* const out_b = a.n == 1 ? a.dbeta : a.part_c + (long)s.n * 2 * a.c;
+  float* const out_g = a.n == 1 ? a.dgamma : a.part_c + (long)s.n * 2 * a.c + a.c;
   for (int j = threadIdx.x; j < w; j += blockDim.x) {
     const float g = j == (int)threadIdx.x ? gamma_t : a.gamma ? a.gamma[s.c0 + j] : 1.f;
     const float b = lds[j], d = lds[stride + j];

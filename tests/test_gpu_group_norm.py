@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 SIZES = [
     (1, 1, 4, 1), (1, 1, 1, 1), (2, 1, 7, 7), (3, 5, 6, 2), (2, 49, 24, 3), (1, 300, 96, 32), (4, 63, 40, 8), (2, 1030, 64, 16),
     (1, 17, 2050, 2), (2, 9, 4100, 1), (1, 5000, 3, 1), (5, 169, 384, 32), (3, 1, 4096, 32), (2, 3025, 48, 16), (70, 4, 64, 32),
-    (1, 20011, 8, 2), (2, 33, 37, 37),
+    (1, 20011, 8, 2), (2, 33, 37, 37), (1, 3001, 1500, 3), (1, 2000, 1025, 5), (2, 1500, 1100, 275), (1, 9000, 300, 2),
 ]
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 CODES = [None, torch.int8, torch.float8_e4m3fn]
