@@ -70,20 +70,31 @@ __device__ __forceinline__ Spot spot(const GnArgs& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == ALEXNET_ACT_RELU) return z < 0.f ? 0.f : z;  // a NaN stays one
-  if (act == ALEXNET_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));  // one ulp each
+// f with the activation as a constant: a loop asks once, not at every value
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  if (act == ALEXNET_ACT_RELU)
+    f(std::integral_constant<int, ALEXNET_ACT_RELU>());
+  else if (act == ALEXNET_ACT_SILU)
+    f(std::integral_constant<int, ALEXNET_ACT_SILU>());
+  else
+    f(std::integral_constant<int, ALEXNET_ACT_NONE>());
+}
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if (ACT == ALEXNET_ACT_RELU) return z < 0.f ? 0.f : z;  // a NaN stays one
+  if (ACT == ALEXNET_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));  // one ulp each
   return z;
 }
 
 // d := d * act'(z) of V values, hat := (x - mean) * rstd.  A relu's gate within rounding of its border is decided in 64 bits: a
 // gate that falls the other way is an error as large as the gradient itself, and one value in some ten million is that near.
-template <int V>
+template <int V, int ACT>
 __device__ __forceinline__ void gate(float* d, const float* x, float* hat, const float* mean, const float* rstd, const float* gamma,
-                                     const float* beta, int act) {
+                                     const float* beta) {
 #pragma unroll
   for (int i = 0; i < V; ++i) hat[i] = (x[i] - mean[i]) * rstd[i];
-  if (act == ALEXNET_ACT_RELU) {
+  if constexpr (ACT == ALEXNET_ACT_RELU) {
     bool near = false, open[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -101,7 +112,7 @@ __device__ __forceinline__ void gate(float* d, const float* x, float* hat, const
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) d[i] = open[i] ? d[i] : 0.f;
-  } else if (act == ALEXNET_ACT_SILU) {
+  } else if constexpr (ACT == ALEXNET_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float z = __builtin_fmaf(hat[i], gamma[i], beta[i]), s = __builtin_amdgcn_rcpf(1.f + __expf(-z));

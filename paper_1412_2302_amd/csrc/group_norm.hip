@@ -230,21 +230,23 @@ __global__ void __launch_bounds__(256) gn_apply_kernel(GnArgs a) {
     scale[i] = a.stat[2 * g + 1] * (a.gamma ? a.gamma[ch] : 1.f);
     beta[i] = a.beta ? a.beta[ch] : 0.f;
   }
-  for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
-    typename Pack<T, V>::Raw r[kUnroll];
+  with_act(a.act, [&](auto act) {
+    for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
+      typename Pack<T, V>::Raw r[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (p + u * a.rpi < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_x + v.c);
+      for (int u = 0; u < kUnroll; ++u)
+        if (p + u * a.rpi < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_x + v.c);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (p + u * a.rpi < s.p1) {
-        float f[V];
-        Pack<T, V>::widen(r[u], f);
+      for (int u = 0; u < kUnroll; ++u)
+        if (p + u * a.rpi < s.p1) {
+          float f[V];
+          Pack<T, V>::widen(r[u], f);
 #pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = activate(__builtin_fmaf(f[i] - mean[i], scale[i], beta[i]), a.act);
-        Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, f);
-      }
-  }
+          for (int i = 0; i < V; ++i) f[i] = activate<decltype(act)::value>(__builtin_fmaf(f[i] - mean[i], scale[i], beta[i]));
+          Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, f);
+        }
+    }
+  });
 }
 
 // ---- gradients ------------------------------------------------------------------
@@ -267,32 +269,34 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
       gamma[i] = a.gamma ? a.gamma[ch] : 1.f;
       beta[i] = a.beta ? a.beta[ch] : 0.f;
     }
-    for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
-      typename Source<T, V, SRC>::Raw x[kUnroll];
-      typename Pack<T, V>::Raw d[kUnroll];
+    with_act(a.act, [&](auto act) {
+      for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
+        typename Source<T, V, SRC>::Raw x[kUnroll];
+        typename Pack<T, V>::Raw d[kUnroll];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (p + u * a.rpi < s.p1) {
-          const long row = (long)s.n * a.hw + p + u * a.rpi;
-          Source<T, V, SRC>::load(a, row, v, x[u]);
-          d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
-        }
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (p + u * a.rpi < s.p1) {
-          float xf[V], df[V];
-          Source<T, V, SRC>::widen(x[u], v, xf);
-          Pack<T, V>::widen(d[u], df);
-          float hat[V];
-          gate<V>(df, xf, hat, mean, rstd, gamma, beta, a.act);
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            db[i] += df[i];
-            dg[i] = __builtin_fmaf(df[i], hat[i], dg[i]);
+        for (int u = 0; u < kUnroll; ++u)
+          if (p + u * a.rpi < s.p1) {
+            const long row = (long)s.n * a.hw + p + u * a.rpi;
+            Source<T, V, SRC>::load(a, row, v, x[u]);
+            d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
           }
-          __builtin_amdgcn_sched_barrier(0);  // pixel by pixel: side by side they take twice the registers
-        }
-    }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (p + u * a.rpi < s.p1) {
+            float xf[V], df[V];
+            Source<T, V, SRC>::widen(x[u], v, xf);
+            Pack<T, V>::widen(d[u], df);
+            float hat[V];
+            gate<V, decltype(act)::value>(df, xf, hat, mean, rstd, gamma, beta);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              db[i] += df[i];
+              dg[i] = __builtin_fmaf(df[i], hat[i], dg[i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);  // pixel by pixel: side by side they take twice the registers
+          }
+      }
+    });
   }
   if (s.on) {
 #pragma unroll
@@ -446,30 +450,32 @@ __global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a) {
     ma[i] = a.stat[2 * g];
     mb[i] = a.stat[2 * g + 1];
   }
-  for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
-    typename Source<T, V, SRC>::Raw x[kUnroll];
-    typename Pack<T, V>::Raw d[kUnroll];
+  with_act(a.act, [&](auto act) {
+    for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
+      typename Source<T, V, SRC>::Raw x[kUnroll];
+      typename Pack<T, V>::Raw d[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (p + u * a.rpi < s.p1) {
-        const long row = (long)s.n * a.hw + p + u * a.rpi;
-        Source<T, V, SRC>::load(a, row, v, x[u]);
-        d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
-      }
+      for (int u = 0; u < kUnroll; ++u)
+        if (p + u * a.rpi < s.p1) {
+          const long row = (long)s.n * a.hw + p + u * a.rpi;
+          Source<T, V, SRC>::load(a, row, v, x[u]);
+          d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
+        }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (p + u * a.rpi < s.p1) {
-        float xf[V], df[V];
-        Source<T, V, SRC>::widen(x[u], v, xf);
-        Pack<T, V>::widen(d[u], df);
-        float hat[V];
-        gate<V>(df, xf, hat, mean, rstd, gamma, beta, a.act);
+      for (int u = 0; u < kUnroll; ++u)
+        if (p + u * a.rpi < s.p1) {
+          float xf[V], df[V];
+          Source<T, V, SRC>::widen(x[u], v, xf);
+          Pack<T, V>::widen(d[u], df);
+          float hat[V];
+          gate<V, decltype(act)::value>(df, xf, hat, mean, rstd, gamma, beta);
 #pragma unroll
-        for (int i = 0; i < V; ++i) df[i] = rstd[i] * (__builtin_fmaf(gamma[i], df[i], -ma[i]) - hat[i] * mb[i]);
-        Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, df);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-  }
+          for (int i = 0; i < V; ++i) df[i] = rstd[i] * (__builtin_fmaf(gamma[i], df[i], -ma[i]) - hat[i] * mb[i]);
+          Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, df);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  });
 }
 
 // what an empty batch or map leaves
@@ -526,10 +532,10 @@ static GnArgs gn_args(const alexnet_group_norm_t* cfg) {
 }
 static bool empty(const alexnet_group_norm_t* cfg) { return cfg->n == 0 || cfg->hw == 0; }
 static SlabPlan forward_plan(const GnArgs& a, size_t size, bool keep) {
-  return slab_plan(a.n, a.hw, a.c, a.groups, 16 / (int)size, kForwardRegs, keep, 1, 12);
+  return slab_plan(a.n, a.hw, a.c, a.groups, 16 / (int)size, kForwardRegs, kForwardRegs, keep, 1, 12);
 }
 static SlabPlan backward_plan(const GnArgs& a) {
-  return slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, false, 2, 16);
+  return slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, kBackwardRegs1024, false, 2, 16);
 }
 // Scratch: sums per chunk and channel, then the groups' statistics; for chunks the larger of the two ways to cut rows into
 // threads (one value a thread: tiny or in-place odd rows).

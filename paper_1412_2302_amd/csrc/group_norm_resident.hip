@@ -180,21 +180,23 @@ __global__ void __launch_bounds__(1024) gn_slab_forward_kernel(GnArgs a) {
   if (!s.has) return;
 #pragma unroll
   for (int i = 0; i < V; ++i) gamma[i] *= rstds[group[i]];
+  with_act(a.act, [&](auto act) {
 #pragma unroll
-  for (int u = 0; u < R; ++u) {
-    const int p = s.row + u * a.rpi;
-    if (p >= a.hw) break;
-    float f[V];
-    Pack<T, V>::widen(x[u], f);
+    for (int u = 0; u < R; ++u) {
+      const int p = s.row + u * a.rpi;
+      if (p >= a.hw) break;
+      float f[V];
+      Pack<T, V>::widen(x[u], f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = activate(__builtin_fmaf(f[i] - mean[i], gamma[i], beta[i]), a.act);
-    Pack<T, V>::store((T*)a.out + (row0 + p) * a.ld_out + v.c, f);
-  }
+      for (int i = 0; i < V; ++i) f[i] = activate<decltype(act)::value>(__builtin_fmaf(f[i] - mean[i], gamma[i], beta[i]));
+      Pack<T, V>::store((T*)a.out + (row0 + p) * a.ld_out + v.c, f);
+    }
+  });
 }
 
 // sums of a slab's channels go to part_c [n][2][c] (one picture: to dbeta and dgamma themselves)
 template <typename T, int V, int SRC, int R>
-__global__ void __launch_bounds__(1024) gn_slab_backward_kernel(GnArgs a) {
+__global__ void __launch_bounds__(R > kBackwardRegs1024 ? 512 : 1024) gn_slab_backward_kernel(GnArgs a) {
   extern __shared__ float lds[];  // threads * V twice, then as many as groups twice
   const Slab s = slab(a, V);
   const Vec v = vec_of<V>(s.col, s.c0, s.width);
@@ -226,20 +228,22 @@ __global__ void __launch_bounds__(1024) gn_slab_backward_kernel(GnArgs a) {
     sums[0][i] = sums[1][i] = 0.f;
   }
   float dz[R][V];
+  with_act(a.act, [&](auto act) {
 #pragma unroll
-  for (int u = 0; u < R; ++u) {
-    if (!s.has || s.row + u * a.rpi >= a.hw) break;
-    float xf[V], hat[V];
-    Source<T, V, SRC>::widen(x[u], v, xf);
-    Pack<T, V>::widen(d[u], dz[u]);
-    gate<V>(dz[u], xf, hat, mean, rstd, gamma, beta, a.act);
+    for (int u = 0; u < R; ++u) {
+      if (!s.has || s.row + u * a.rpi >= a.hw) break;
+      float xf[V], hat[V];
+      Source<T, V, SRC>::widen(x[u], v, xf);
+      Pack<T, V>::widen(d[u], dz[u]);
+      gate<V, decltype(act)::value>(dz[u], xf, hat, mean, rstd, gamma, beta);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      sums[0][i] += dz[u][i];
-      sums[1][i] = __builtin_fmaf(dz[u][i], hat[i], sums[1][i]);
+      for (int i = 0; i < V; ++i) {
+        sums[0][i] += dz[u][i];
+        sums[1][i] = __builtin_fmaf(dz[u][i], hat[i], sums[1][i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // pixel by pixel: side by side they take twice the registers
     }
-    __builtin_amdgcn_sched_barrier(0);  // pixel by pixel: side by side they take twice the registers
-  }
+  });
   const int w = s.width, stride = blockDim.x * V;
   float* const totals = lds + 2 * stride;
   const float gamma_t = a.gamma && (int)threadIdx.x < w ? a.gamma[s.c0 + threadIdx.x] : 1.f;
@@ -293,6 +297,7 @@ static int forward_keep(const GnArgs& a, const SlabPlan& p, hipStream_t st) {
   return p.regs <= 1    ? forward_regs<T, KEEP, 1>(a, p, st)
          : p.regs <= 2  ? forward_regs<T, KEEP, 2>(a, p, st)
          : p.regs <= 4  ? forward_regs<T, KEEP, 4>(a, p, st)
+         : p.regs <= 6  ? forward_regs<T, KEEP, 6>(a, p, st)
          : p.regs <= 8  ? forward_regs<T, KEEP, 8>(a, p, st)
          : p.regs <= 12 ? forward_regs<T, KEEP, 12>(a, p, st)
                         : forward_regs<T, KEEP, 16>(a, p, st);
@@ -331,6 +336,7 @@ static int backward_src(const GnArgs& a, const SlabPlan& p, hipStream_t st) {
   return p.regs <= 1   ? backward_regs<T, SRC, 1>(a, p, st)
          : p.regs <= 2 ? backward_regs<T, SRC, 2>(a, p, st)
          : p.regs <= 4 ? backward_regs<T, SRC, 4>(a, p, st)
+         : p.regs <= 6 ? backward_regs<T, SRC, 6>(a, p, st)
                        : backward_regs<T, SRC, 8>(a, p, st);
 }
 template <typename T>

@@ -11,7 +11,7 @@ struct SlabPlan {
   int threads = 0, cols = 0, rpi = 0, regs = 0;
 };
 
-// V channels a thread and pixel, at most max_regs pixels a thread; blocks32: slabs and threads in whole blocks of 32 channels;
+// V channels a thread and pixel, at most max_regs pixels a thread (max_regs_1024 of 1024 threads); blocks32: slabs and threads in whole blocks of 32 channels;
 // sums: values per channel that the workgroup adds up, in 64 KB of LDS at most; narrow: the least channels of a pixel that
 // 1024 threads take (unless those are all).
 //
@@ -20,7 +20,7 @@ struct SlabPlan {
 // Forward, 256 x 729 x 256 bf16: 32 channels 52 us, 16 channels 62, 8 channels 76, three launches 85; 64 x 4096 x 128 bf16: 512
 // threads 36, 1024 threads 58, three launches 56.  Backward, 256 x 729 x 256 fp32: 16 channels and 512 threads 137, 32 channels
 // and 1024 threads 146, three launches 237; 128 x 3025 x 96 fp32: 12 channels and 1024 threads 229, three launches 175.
-inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, bool blocks32, int sums, int narrow) {
+inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, int max_regs_1024, bool blocks32, int sums, int narrow) {
   const int cpg = c / groups, lanes = blocks32 ? 32 / V : 1;
   SlabPlan best, large;
   // slabs start on whole blocks of 32 channels: their groups' channels are a multiple of 32, or all there are
@@ -43,10 +43,10 @@ inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs,
         p.rpi = (int)(threads / cols);
         if (!p.rpi) continue;
         p.regs = (hw + p.rpi - 1) / p.rpi;
-        if (p.regs <= (few ? std::min(4, max_regs) : max_regs)) break;
+        if (p.regs <= (few ? 4 : threads == 1024 ? max_regs_1024 : max_regs)) break;
       }
       const long lds = 4L * ((long)sums * p.threads * V + 2 * k);
-      const bool fits = p.rpi > 0 && p.regs <= max_regs && lds <= 65536;
+      const bool fits = p.rpi > 0 && p.regs <= (p.threads == 1024 ? max_regs_1024 : max_regs) && lds <= 65536;
       if (!fits && (best.groups || large.groups)) break;  // wider ones do not fit either
       if (fits) {
         if (p.threads < 1024 || few)

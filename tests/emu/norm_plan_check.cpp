@@ -14,16 +14,16 @@ static int fail(const char* what, int n, int hw, int c, int g, int V) {
   return 1;
 }
 
-static int check(int n, int hw, int c, int g, int V, int regs, bool b32, int sums, int narrow, long* taken) {
+static int check(int n, int hw, int c, int g, int V, int regs, int regs1024, bool b32, int sums, int narrow, long* taken) {
   const int cpg = c / g;
-  const SlabPlan p = slab_plan(n, hw, c, g, V, regs, b32, sums, narrow);
+  const SlabPlan p = slab_plan(n, hw, c, g, V, regs, regs1024, b32, sums, narrow);
   if (!p.groups) return 0;
   ++*taken;
 #define NEED(x) \
   if (!(x)) return fail(#x, n, hw, c, g, V)
   NEED(p.threads == 256 || p.threads == 512 || p.threads == 1024);
   NEED(p.rpi >= 1 && p.rpi * p.cols <= p.threads);
-  NEED((long)p.rpi * p.regs >= hw && p.regs <= regs);
+  NEED((long)p.rpi * p.regs >= hw && p.regs <= (p.threads == 1024 ? regs1024 : regs));
   NEED(p.slabs == (g + p.groups - 1) / p.groups);
   NEED(4L * ((long)sums * p.threads * V + 2 * p.groups) <= 65536);
   if (b32) NEED(p.cols % (32 / V) == 0);
@@ -61,8 +61,8 @@ int main() {
           for (int n : {1, 7, 300})
             for (int b32 = 0; b32 < 2; ++b32) {
               ++all;
-              if (check(n, hw, g * cpg, g, V, 16, b32, 1, 12, &taken)) return 1;
-              if (!b32 && V == 4 && check(n, hw, g * cpg, g, V, 8, false, 2, 16, &taken)) return 1;
+              if (check(n, hw, g * cpg, g, V, 16, 16, b32, 1, 12, &taken)) return 1;
+              if (!b32 && V == 4 && check(n, hw, g * cpg, g, V, 8, 6, false, 2, 16, &taken)) return 1;
             }
   for (int c : {1, 3, 7, 96, 1000, 1024, 4096, 4100, 8192, 10000, 1 << 20})
     for (int g : {1, 2, 4, 32, 1000})
@@ -71,8 +71,8 @@ int main() {
           for (int V : {4, 8})
             for (int b32 = 0; b32 < 2; ++b32) {
               ++all;
-              if (check(3, hw, c, g, V, 16, b32, 1, 12, &taken)) return 1;
-              if (V == 4 && check(3, hw, c, g, V, 8, false, 2, 16, &taken)) return 1;
+              if (check(3, hw, c, g, V, 16, 16, b32, 1, 12, &taken)) return 1;
+              if (V == 4 && check(3, hw, c, g, V, 8, 6, false, 2, 16, &taken)) return 1;
             }
   printf("OK %ld plans of %ld sizes\n", taken, all);
   return 0;
