@@ -270,23 +270,25 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
       beta[i] = a.beta ? a.beta[ch] : 0.f;
     }
     with_act(a.act, [&](auto act) {
-      for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
-        typename Source<T, V, SRC>::Raw x[kUnroll];
-        typename Pack<T, V>::Raw d[kUnroll];
+      struct Round {
+        typename Source<T, V, SRC>::Raw x[2];
+        typename Pack<T, V>::Raw d[2];
+      };
+      const auto load = [&](Round& r, int p) {  // past the end the last pixel again
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (p + u * a.rpi < s.p1) {
-            const long row = (long)s.n * a.hw + p + u * a.rpi;
-            Source<T, V, SRC>::load(a, row, v, x[u]);
-            d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
-          }
+        for (int u = 0; u < 2; ++u) {
+          const long row = (long)s.n * a.hw + min(p + u * a.rpi, s.p1 - 1);
+          Source<T, V, SRC>::load(a, row, v, r.x[u]);
+          r.d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
+        }
+      };
+      const auto take = [&](const Round& r, int p) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
+        for (int u = 0; u < 2; ++u)
           if (p + u * a.rpi < s.p1) {
-            float xf[V], df[V];
-            Source<T, V, SRC>::widen(x[u], v, xf);
-            Pack<T, V>::widen(d[u], df);
-            float hat[V];
+            float xf[V], df[V], hat[V];
+            Source<T, V, SRC>::widen(r.x[u], v, xf);
+            Pack<T, V>::widen(r.d[u], df);
             gate<V, decltype(act)::value>(df, xf, hat, mean, rstd, gamma, beta);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -295,6 +297,19 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
             }
             __builtin_amdgcn_sched_barrier(0);  // pixel by pixel: side by side they take twice the registers
           }
+      };
+      Round r0, r1, r2;  // two rounds of loads ahead
+      int p = s.p0 + s.row;
+      const int step = 2 * a.rpi;
+      load(r0, p);
+      load(r1, p + step);
+      for (; p < s.p1; p += 3 * step) {
+        load(r2, p + 2 * step);
+        take(r0, p);
+        load(r0, p + 3 * step);
+        take(r1, p + step);
+        load(r1, p + 4 * step);
+        take(r2, p + 2 * step);
       }
     });
   }
@@ -353,50 +368,45 @@ __global__ void __launch_bounds__(256) gn_grad_sums_kernel(GnArgs a) {
   });
 }
 
-// Workgroups [0, group_blocks): the means that dx subtracts, mean(gamma dz) and mean(gamma dz xhat), sixteen groups each where
-// SHORT (a wave to a group), else one; then, eight channels a workgroup, the sums over pictures and chunks that are dbeta and
-// dgamma.  width: channels of a block of columns.
-template <bool SHORT>
-__global__ void __launch_bounds__(1024) gn_grad_totals_kernel(GnArgs a, int group_blocks, int width) {
-  __shared__ float sb[1024], sg[1024];
-  const int t = threadIdx.x;
+// The means that dx subtracts, mean(gamma dz) and mean(gamma dz xhat), by a team of threads per group (a wave where its terms
+// are few: 4096 groups of 48 terms took 21 us with 1024 threads each).  width: channels of a block of columns.
+template <int TEAM>
+__global__ void __launch_bounds__(256) gn_grad_means_kernel(GnArgs a, int width) {
+  __shared__ float lds[4];
+  const int id = blockIdx.x * (256 / TEAM) + (int)threadIdx.x / TEAM, t = threadIdx.x % TEAM;
+  if (TEAM == 64 && id >= a.n * a.groups) return;
+  const int n = id / a.groups, group = id - n * a.groups, slots = slots_of(a);
+  const Span span = span_of(a, group, width);
+  const float* const part = a.part + (long)n * a.chunks * 2 * slots + group + span.first;
+  const int terms = a.chunks * span.blocks;
   float b = 0.f, g = 0.f;
-  if ((int)blockIdx.x < group_blocks) {
-    const int id = SHORT ? blockIdx.x * 16 + (t >> 6) : blockIdx.x, team = SHORT ? 64 : 1024, lane = SHORT ? t & 63 : t;
-    if (SHORT && id >= a.n * a.groups) return;
-    const int n = id / a.groups, group = id - n * a.groups, slots = slots_of(a);
-    const Span span = span_of(a, group, width);
-    const float* const part = a.part + (long)n * a.chunks * 2 * slots + group + span.first;
-    const int terms = a.chunks * span.blocks;
 #pragma unroll 4
-    for (int i = lane; i < terms; i += team) {
-      const int k = i / span.blocks, j = i - k * span.blocks;
-      b += part[(long)k * 2 * slots + j];
-      g += part[(long)k * 2 * slots + slots + j];
-    }
-    b = wave_sum(b);
-    g = wave_sum(g);
-    if (!SHORT) {
-      if ((t & 63) == 0) sb[t >> 6] = b, sg[t >> 6] = g;
-      __syncthreads();
-      if (t == 0)
-        for (int k = 1; k < 16; ++k) {
-          b += sb[k];
-          g += sg[k];
-        }
-    }
-    if (lane == 0) {
-      const float inv = 1.f / ((float)a.hw * (float)a.cpg);
-      a.stat[2 * (long)id] = b * inv;
-      a.stat[2 * (long)id + 1] = g * inv;
-    }
-    return;
+  for (int i = t; i < terms; i += TEAM) {
+    const int k = i / span.blocks, j = i - k * span.blocks;
+    b += part[(long)k * 2 * slots + j];
+    g += part[(long)k * 2 * slots + slots + j];
   }
-  const int ch = ((int)blockIdx.x - group_blocks) * 8 + (t & 7);
+  b = TEAM == 64 ? wave_sum(b) : group_sum(b, lds);
+  g = TEAM == 64 ? wave_sum(g) : group_sum(g, lds);
+  if (t == 0) {
+    const float inv = 1.f / ((float)a.hw * (float)a.cpg);
+    a.stat[2 * (long)id] = b * inv;
+    a.stat[2 * (long)id + 1] = g * inv;
+  }
+}
+static bool few_terms(const GnArgs& a, int width) { return (long)a.chunks * (a.cpg / width + 2) <= 512; }
+
+// dbeta and dgamma of eight channels, the sums over pictures and chunks, by a workgroup of THREADS; lds: 2 * THREADS floats
+constexpr int kTotalChannels = 8;
+template <int THREADS>
+__device__ __forceinline__ void channel_totals(const GnArgs& a, int block, float* lds) {
+  float *const sb = lds, *const sg = lds + THREADS;
+  const int t = threadIdx.x, ch = block * kTotalChannels + t % kTotalChannels;
   const long rows = (long)a.n * a.chunks;
+  float b = 0.f, g = 0.f;
   if (ch < a.c) {
 #pragma unroll 8
-    for (long r = t >> 3; r < rows; r += 128) {
+    for (long r = t / kTotalChannels; r < rows; r += THREADS / kTotalChannels) {
       b += a.part_c[r * 2 * a.c + ch];
       g += a.part_c[r * 2 * a.c + a.c + ch];
     }
@@ -405,37 +415,32 @@ __global__ void __launch_bounds__(1024) gn_grad_totals_kernel(GnArgs a, int grou
   sg[t] = g;
   __syncthreads();
 #pragma unroll
-  for (int d = 512; d >= 8; d >>= 1) {
+  for (int d = THREADS / 2; d >= kTotalChannels; d >>= 1) {
     if (t < d) {
       sb[t] += sb[t + d];
       sg[t] += sg[t + d];
     }
     __syncthreads();
   }
-  if (t < 8 && ch < a.c) {
+  if (t < kTotalChannels && ch < a.c) {
     if (a.dbeta) a.dbeta[ch] = sb[t];
     if (a.dgamma) a.dgamma[ch] = sg[t];
   }
 }
-// a group whose terms are few is a wave's work, not a workgroup's: 4096 groups of 48 terms took 21 us with 1024 threads each
-static bool few_terms(const GnArgs& a, int width) { return (long)a.chunks * (a.cpg / width + 2) <= 512; }
-static int launch_totals(const GnArgs& a, bool groups, int width, hipStream_t st) {
-  const bool few = few_terms(a, width);
-  const int group_blocks = !groups ? 0 : few ? ceil_div((long)a.n * a.groups, 16) : a.n * a.groups;
-  const int channel_blocks = a.dbeta || a.dgamma ? ceil_div(a.c, 8) : 0;
-  if (group_blocks + channel_blocks == 0) return ALEXNET_OK;
-  KernelScope ks("gn_grad_totals", 0, 0, st);
-  const dim3 grid((unsigned)(group_blocks + channel_blocks)), block(1024);
-  if (few)
-    hipLaunchKernelGGL(gn_grad_totals_kernel<true>, grid, block, 0, st, a, group_blocks, width);
-  else
-    hipLaunchKernelGGL(gn_grad_totals_kernel<false>, grid, block, 0, st, a, group_blocks, width);
-  AX_LAUNCH_CHECK();
-  return ALEXNET_OK;
+__global__ void __launch_bounds__(1024) gn_channel_totals_kernel(GnArgs a) {
+  __shared__ float lds[2048];
+  channel_totals<1024>(a, blockIdx.x, lds);
 }
+static int total_blocks(const GnArgs& a) { return a.dbeta || a.dgamma ? ceil_div(a.c, kTotalChannels) : 0; }
 
+// Its first workgroups, total_blocks of them, leave dbeta and dgamma meanwhile.
 template <typename T, int V, int SRC>
-__global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a) {
+__global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a, int total_blocks) {
+  __shared__ float lds[512];
+  if ((int)blockIdx.x < total_blocks) {
+    channel_totals<256>(a, blockIdx.x, lds);
+    return;
+  }
   const Spot s = spot(a, gridDim.x - 1 - blockIdx.x);  // backwards, as in gn_apply_kernel
   if (!s.has) return;
   const Vec v = vec_of<V>(s.v, 0, a.c);
@@ -617,9 +622,19 @@ static int gn_backward(GnArgs a, hipStream_t st) {
     KernelScope ks("gn_grad_sums", 0, in, st);
     GN_LAUNCH((gn_grad_sums_kernel<T, V, SRC>), blocks, 256, st, a);
   }
-  AX_TRY(launch_totals(a, true, a.cols * V, st));
+  {
+    KernelScope ks("gn_grad_means", 0, 0, st);
+    const int width = a.cols * V;
+    if (few_terms(a, width))
+      hipLaunchKernelGGL(gn_grad_means_kernel<64>, dim3((unsigned)ceil_div((long)a.n * a.groups, 4)), dim3(256), 0, st, a, width);
+    else
+      hipLaunchKernelGGL(gn_grad_means_kernel<256>, dim3((unsigned)(a.n * a.groups)), dim3(256), 0, st, a, width);
+    AX_LAUNCH_CHECK();
+  }
   KernelScope ks("gn_grad_apply", 0, in + values * sizeof(T), st);
-  GN_LAUNCH((gn_grad_apply_kernel<T, V, SRC>), blocks, 256, st, a);
+  const int totals = total_blocks(a);
+  hipLaunchKernelGGL((gn_grad_apply_kernel<T, V, SRC>), dim3((unsigned)(blocks + totals)), dim3(256), 0, st, a, totals);
+  AX_LAUNCH_CHECK();
   return ALEXNET_OK;
 }
 
@@ -639,7 +654,11 @@ static int gn_backward_src(GnArgs a, int type, hipStream_t st) {
     a.part_c = a.part;
     a.chunks = a.col_blocks = 1;
     AX_TRY(launch_gn_slab_backward(a, p, type, SRC, st));
-    return a.n > 1 ? launch_totals(a, false, a.c, st) : ALEXNET_OK;
+    const int totals = total_blocks(a);
+    if (a.n == 1 || !totals) return ALEXNET_OK;
+    KernelScope ks("gn_grad_totals", 0, 0, st);
+    GN_LAUNCH(gn_channel_totals_kernel, totals, 1024, st, a);
+    return ALEXNET_OK;
   }
   constexpr int V = kBackwardVec;
   return a.c >= V && (a.c % V == 0 || (a.dy != a.out && a.x != a.out)) ? gn_backward<T, V, SRC>(a, st) : gn_backward<T, 1, SRC>(a, st);
