@@ -67,31 +67,30 @@ template <int NB, int... I>
 __device__ __forceinline__ void row_scales(float s, float* out, std::integer_sequence<int, I...>) {
   ((out[I] = row_scale<I, NB>(s)), ...);
 }
-// eight rows of NB codes to one unit per column
-template <int CODE, int NB>
-__device__ __forceinline__ void codes_to_units(const uint32_t* w, const float* s, Unit* u) {
+// The unit of column E of eight rows' codes (E4M3: of columns E and E + 1, E even; one instruction widens two columns)
+template <int CODE, int NB, int E>
+__device__ __forceinline__ void codes_to_units(const uint32_t* w, const float* s, Unit* lds) {
+  Unit u, v;
   if constexpr (CODE == ALEXNET_CODE_INT8) {
 #pragma unroll
-    for (int e = 0; e < NB; ++e)
+    for (int i = 0; i < 4; ++i)
+      u[i] = upper_halves((float)(int8_t)(w[2 * i] >> 8 * E) * s[2 * i], (float)(int8_t)(w[2 * i + 1] >> 8 * E) * s[2 * i + 1]);
+    lds[E * 64] = u;
+  } else if constexpr (E % 2 == 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        u[e][i] = upper_halves((float)(int8_t)(w[2 * i] >> 8 * e) * s[2 * i], (float)(int8_t)(w[2 * i + 1] >> 8 * e) * s[2 * i + 1]);
-  } else {
-    // two columns to an instruction, already bf16
-    typedef __bf16 Two __attribute__((ext_vector_type(2)));
-#pragma unroll
-    for (int e = 0; e < NB; e += 2)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const Two lo = e ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], s[2 * i], true)
-                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], s[2 * i], false);
-        const Two hi = e ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], s[2 * i + 1], true)
-                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], s[2 * i + 1], false);
-        const uint32_t l = __builtin_bit_cast(uint32_t, lo), h = __builtin_bit_cast(uint32_t, hi);
-        u[e][i] = __builtin_amdgcn_perm(h, l, 0x05040100u);
-        if (e + 1 < NB) u[e + 1][i] = __builtin_amdgcn_perm(h, l, 0x07060302u);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t l = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i], s[2 * i], E != 0));
+      const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + 1], s[2 * i + 1], E != 0));
+      u[i] = __builtin_amdgcn_perm(h, l, 0x05040100u);
+      v[i] = __builtin_amdgcn_perm(h, l, 0x07060302u);
+    }
+    lds[E * 64] = u;
+    if constexpr (E + 1 < NB) lds[(E + 1) * 64] = v;
   }
+}
+template <typename F, int... I>
+__device__ __forceinline__ void for_each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
 }
 
 template <typename T, int CODE, int NA, int NB>
@@ -127,17 +126,17 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
   const char* pa;
   const uint8_t *pb, *ps;
   const long row_a = a.ld_dy * (long)sizeof(T);
-  // WHOLE: a step that is; else rows past its end repeat the last one, read in bounds and zeroed below
-  auto load = [&](Rows& v, auto whole) {
+  // WHOLE: a step that is; else rows past its end repeat the last one, read in bounds and zeroed below.  (The offsets are opaque
+  // here, so that a load is one instruction with a scalar base; and the compiler would put the loads off to behind the
+  // products, whose time they need.)
+  auto load_a = [&](Rows& v, auto whole) {
     constexpr bool WHOLE = decltype(whole)::value;
-    // (opaque here, so that a load is one instruction with a scalar base and this offset)
-    uint32_t oa = off_a, ob = off_b, os = off_s;
-    asm volatile("" : "+v"(oa), "+v"(ob), "+v"(os));
-    const int last = WHOLE ? 7 : odd - 1 - oct * 8;  // of the patch; below zero: none of it
+    uint32_t oa = off_a;
+    asm volatile("" : "+v"(oa));
+    const int last = odd - 1 - oct * 8;  // of the first step's patch; below zero: none of it
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int r = WHOLE ? i : min(i, last);
-      const char* const qa = pa + r * row_a;
+      const char* const qa = pa + (WHOLE ? i : min(i, last)) * row_a;
       if constexpr (NA == 1) {
         v.a[i][0] = *(const T*)(qa + oa);
       } else {
@@ -145,7 +144,18 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
 #pragma unroll
         for (int e = 0; e < NA; ++e) v.a[i][e] = w[e];
       }
-      const uint8_t* const qb = pb + (long)r * a.in;
+    }
+    pa += (WHOLE ? kStep : odd) * row_a;
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto load_b = [&](Rows& v, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    uint32_t ob = off_b, os = off_s;
+    asm volatile("" : "+v"(ob), "+v"(os));
+    const int last = odd - 1 - oct * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint8_t* const qb = pb + (long)(WHOLE ? i : min(i, last)) * a.in;
       if constexpr (NB == 4)
         v.b[i] = reinterpret_cast<const Loose<uint32_t>*>(qb + ob)->v;
       else if constexpr (NB == 2)
@@ -158,85 +168,106 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
     else
       v.s = ps[(long)min(scale_row, last) * a.nb + min(block, a.nb - 1)];
     const int next = WHOLE ? kStep : odd;
-    pa += next * row_a;
     pb += (long)next * a.in;
     ps += (long)next * a.nb;
-    // the compiler would put the loads off to behind the products, whose time they need
     __builtin_amdgcn_sched_barrier(0);
   };
+  auto load = [&](Rows& v, auto whole) {
+    load_a(v, whole);
+    load_b(v, whole);
+  };
   float sum[NA];
-  // FIX: infinities leave no rest (inf - inf is not a number)
-  auto put = [&](const Rows& v, int stage, auto whole, auto fix) {
+  // The work of putting a step's values into LDS, in pieces: NA * TERMS of dy, one for the scales, NB of x.
+  // FIX: infinities leave no rest (inf - inf is not a number).
+  constexpr int kPieces = NA * TERMS + 1 + NB;
+  float f[8], s[8];
+  const int left = odd - oct * 8;  // rows of the first step's patch
+  auto piece = [&](auto index, const Rows& v, int stage, auto whole, auto fix) {
+    constexpr int I = decltype(index)::value;
     constexpr bool WHOLE = decltype(whole)::value, FIX = decltype(fix)::value;
-    const int left = odd - oct * 8;  // rows of the first step's patch
+    if constexpr (I < NA * TERMS) {
+      constexpr int e = I / TERMS, term = I % TERMS;
+      if constexpr (term == 0) {
 #pragma unroll
-    for (int e = 0; e < NA; ++e) {
-      float f[8];
+        for (int i = 0; i < 8; ++i) {
+          f[i] = (float)v.a[i][e];
+          if (!WHOLE) f[i] = i < left ? f[i] : 0.f;
+          sum[e] += f[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = FIX && fabsf(f[i]) == __builtin_inff() ? 0.f : f[i] - upper(f[i]);
+      }
+      Unit u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = upper_halves(f[2 * i], f[2 * i + 1]);
+      sa[stage][term][oct][e * 64 + g] = u;
+    } else if constexpr (I == NA * TERMS) {
+      row_scales<NB>(code_scale(v.s), s, std::make_integer_sequence<int, 8>());
+    } else if constexpr (I < kPieces) {
+      uint32_t w[8];
+      float r[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        f[i] = (float)v.a[i][e];
-        if (!WHOLE) f[i] = i < left ? f[i] : 0.f;
-        sum[e] += f[i];
+        w[i] = !WHOLE && i >= left ? 0u : v.b[i];
+        r[i] = !WHOLE && i >= left ? 1.f : s[i];
       }
-#pragma unroll
-      for (int term = 0; term < TERMS; ++term) {
-        Unit u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = upper_halves(f[2 * i], f[2 * i + 1]);
-        sa[stage][term][oct][e * 64 + g] = u;
-        if (term + 1 < TERMS) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] = FIX && fabsf(f[i]) == __builtin_inff() ? 0.f : f[i] - upper(f[i]);
-        }
-      }
+      codes_to_units<CODE, NB, I - NA * TERMS - 1>(w, r, &sb[stage][oct][g]);
     }
-    float s[8];
-    row_scales<NB>(code_scale(v.s), s, std::make_integer_sequence<int, 8>());
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      w[i] = v.b[i];
-      if (!WHOLE) {
-        w[i] = i < left ? w[i] : 0u;
-        s[i] = i < left ? s[i] : 1.f;
-      }
-    }
-    Unit u[NB];
-    codes_to_units<CODE, NB>(w, s, u);
-#pragma unroll
-    for (int e = 0; e < NB; ++e) sb[stage][oct][e * 64 + g] = u[e];
+  };
+  auto put = [&](const Rows& v, int stage, auto whole, auto fix) {
+    for_each([&](auto i) { piece(i, v, stage, whole, fix); }, std::make_integer_sequence<int, kPieces>());
   };
 
   Acc acc[NA][NB];
   const int wm = (wave >> 1) * 32 + (lane & 31), wn = (wave & 1) * 32 + (lane & 31), half = lane >> 5;
-  auto multiply = [&](int stage) {
+  // A step's products: 2 * TERMS * NA groups of NB, the smallest terms first.  After each of them between(group).
+  constexpr int kGroups = 2 * TERMS * NA;
+  auto multiply = [&](int stage, auto between) {
+    Frag b[2][NB], fa[2];
+    auto read_a = [&](int group, Frag& to) {
+      const int h = group / (TERMS * NA), term = TERMS - 1 - group % (TERMS * NA) / NA, j = group % NA;
+      to = __builtin_bit_cast(Frag, sa[stage][term][2 * h + half][j * 64 + wm]);
+    };
+    auto read_b = [&](int h) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      Frag b[NB];
+      for (int k = 0; k < NB; ++k) b[h][k] = __builtin_bit_cast(Frag, sb[stage][2 * h + half][k * 64 + wn]);
+    };
+    read_a(0, fa[0]);
+    read_b(0);
+    for_each(
+        [&](auto group) {
+          constexpr int G = decltype(group)::value, H = G / (TERMS * NA);
+          if constexpr (G + 1 < kGroups) read_a(G + 1, fa[(G + 1) & 1]);
+          if constexpr (G + 1 == TERMS * NA) read_b(1);
 #pragma unroll
-      for (int k = 0; k < NB; ++k) b[k] = __builtin_bit_cast(Frag, sb[stage][2 * h + half][k * 64 + wn]);
-#pragma unroll
-      for (int term = TERMS - 1; term >= 0; --term)
-#pragma unroll
-        for (int j = 0; j < NA; ++j) {
-          const Frag f = __builtin_bit_cast(Frag, sa[stage][term][2 * h + half][j * 64 + wm]);
-#pragma unroll
-          for (int k = 0; k < NB; ++k) acc[j][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, b[k], acc[j][k], 0, 0, 0);
-        }
-    }
+          for (int k = 0; k < NB; ++k)
+            acc[G % NA][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[G & 1], b[H][k], acc[G % NA][k], 0, 0, 0);
+          between(group);
+          // Held to this order; small tiles have too few products for that, and more workgroups to fill the gaps
+          if constexpr (NB == 4) __builtin_amdgcn_sched_barrier(0);
+        },
+        std::make_integer_sequence<int, kGroups>());
   };
-  auto mix = [&]() {
-#pragma unroll
-    for (int i = 0; i < 2 * TERMS * NA * NB; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
-      __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // vector instructions
-      __builtin_amdgcn_sched_group_barrier(0x300, 1, 0);  // an access to LDS
-    }
+  // The same with the pieces of the next step's values between: the vector unit works while the products run.  AHEAD: the
+  // registers that they leave take the loads of the step after.
+  auto multiply_and_put = [&](int stage, Rows& v, auto ahead, auto fix) {
+    constexpr int kEach = (kPieces + kGroups - 1) / kGroups;
+    constexpr bool AHEAD = decltype(ahead)::value;
+    multiply(stage, [&](auto group) {
+      for_each(
+          [&](auto i) {
+            constexpr int I = decltype(group)::value * kEach + decltype(i)::value;
+            piece(std::integral_constant<int, I>(), v, stage ^ 1, std::true_type(), fix);
+            if constexpr (AHEAD && I == (NA - 1) * TERMS) load_a(v, std::true_type());
+            if constexpr (AHEAD && I == kPieces - 1) load_b(v, std::true_type());
+          },
+          std::make_integer_sequence<int, kEach>());
+    });
   };
+  auto nothing = [](auto) {};
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
-  // Two steps of loads in flight; a step's values go to LDS between the products of the step before, which leave the vector
-  // unit idle most of the time.
   auto run = [&](auto fix) {
 #pragma unroll
     for (int j = 0; j < NA; ++j)
@@ -249,35 +280,50 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
     pa = (const char*)dy + (long)oct * 8 * row_a;
     pb = codes + (long)oct * 8 * a.in;
     ps = scales + (long)oct * 8 * a.nb;
-    Rows u, v;
+    Rows u;
     load(u, no);
-    if (steps > 1) load(v, yes);
-    put(u, 0, no, fix);
     int step = 0;
-    for (; step + 3 < steps; step += 2) {
+    if constexpr (NB == 4) {  // the products of a step take long enough for the next loads: one set of registers
+      put(u, 0, no, fix);
+      if (steps > 1) load(u, yes);
+      for (; step + 2 < steps; ++step) {
+        __syncthreads();
+        multiply_and_put(step & 1, u, yes, fix);
+      }
+      if (step + 1 < steps) {
+        __syncthreads();
+        multiply_and_put(step & 1, u, no, fix);
+        ++step;
+      }
       __syncthreads();
-      load(u, yes);
-      multiply(0);
-      put(v, 1, yes, fix);
-      mix();
+      multiply(step & 1, nothing);
+    } else {  // two steps of loads in flight
+      Rows v;
+      if (steps > 1) load(v, yes);
+      put(u, 0, no, fix);
+      for (; step + 3 < steps; step += 2) {
+        __syncthreads();
+        load(u, yes);
+        multiply_and_put(0, v, no, fix);
+        __syncthreads();
+        load(v, yes);
+        multiply_and_put(1, u, no, fix);
+      }
+      __syncthreads();  // one to three steps are left, the first in LDS, the second in v
+      if (step + 1 >= steps) {
+        multiply(0, nothing);
+        return;
+      }
+      if (step + 2 < steps) load(u, yes);
+      multiply_and_put(0, v, no, fix);
       __syncthreads();
-      load(v, yes);
-      multiply(1);
-      put(u, 0, yes, fix);
-      mix();
-    }
-    __syncthreads();  // one to three steps are left, the first in LDS, the second in v
-    if (step + 2 < steps) load(u, yes);
-    multiply(0);
-    if (step + 1 < steps) {
-      put(v, 1, yes, fix);
+      if (step + 2 >= steps) {
+        multiply(1, nothing);
+        return;
+      }
+      multiply_and_put(1, u, no, fix);
       __syncthreads();
-      multiply(1);
-    }
-    if (step + 2 < steps) {
-      put(u, 0, yes, fix);
-      __syncthreads();
-      multiply(0);
+      multiply(0, nothing);
     }
   };
   run(no);
@@ -372,12 +418,12 @@ struct FcPlan {
 };
 // The tile and the number of slices that a model of the measured times makes cheapest.  A step of a workgroup that has a
 // compute unit to itself takes kAloneUs microseconds, one among as many as fit kStepUs of the unit's time; slices are written
-// and read once more each.  256 x 9216 x 4096 fp32 (few rows, large dw): 128 x 256 tiles 75 us, 64 x 128 ones 76, 64 x 64 about
-// 110, two slices 179; 43264 x 384 x 384 bf16: 64 x 128 tiles in 56 slices 38 us, in 24 slices 45, in 12 slices 78, 128 x 256
-// tiles in 86 slices 39, 64 x 64 ones in 64 slices 56.
+// and read once more each.  256 x 9216 x 4096 fp32 (few rows, large dw): 128 x 256 tiles 63 us, 64 x 128 ones 84, two slices 180;
+// 43264 x 384 x 384 bf16: 128 x 256 tiles in 86 slices 37 us, in 43 slices 54, 64 x 128 ones in 56 slices 38, in 12 slices 78,
+// 64 x 64 ones in 64 slices 53; 100000 x 96 x 64 fp32: 64 x 64 tiles in 128 slices 34, 64 x 128 ones in 192 slices 36.
 static FcPlan fc_plan(long rows, int in, int out, int type) {
-  static const double kStepUs[3][3] = {{0.17, 0.26, 0.34}, {0.22, 0.39, 0.57}, {0.61, 0.95, 1.3}};  // [tile][terms - 1]
-  static const double kAloneUs[3][3] = {{0.44, 0.52, 0.6}, {0.57, 0.73, 0.89}, {1.03, 1.48, 1.92}};
+  static const double kStepUs[3][3] = {{0.19, 0.24, 0.33}, {0.21, 0.3, 0.52}, {0.45, 0.75, 1.06}};  // [tile][terms - 1]
+  static const double kAloneUs[3][3] = {{0.3, 0.45, 0.51}, {0.48, 0.56, 0.68}, {0.8, 1.2, 1.57}};
   static const int kFit[3] = {4, 4, 2};  // workgroups on a compute unit
   FcPlan best = {};
   double least = 1e300;
@@ -398,7 +444,7 @@ static FcPlan fc_plan(long rows, int in, int out, int type) {
       p.slices = (int)((steps + p.steps - 1) / p.steps);
       const double units = tiles * p.slices / 256, full = std::floor(units / fit), rest = std::ceil(units - full * fit);
       const double each = full * std::max(alone, us * fit) + (rest > 0 ? std::max(alone, us * rest) : 0.0);
-      const double cost = p.steps * each + p.slices * bytes / 10.8e6 + (p.slices > 1 ? 5.6 + p.slices * bytes / 8.9e6 : 0.0);
+      const double cost = p.steps * each + p.slices * bytes / 8.8e6 + (p.slices > 1 ? 6.8 + p.slices * bytes / 7.1e6 : 0.0);
       if (cost < least) {
         least = cost;
         best = p;
