@@ -381,28 +381,56 @@ __global__ void __launch_bounds__(256, 2) fc_weight_kernel(FcArgs a) {
   }
 }
 
-// dst[i] = the sum of src[slice][i]; the gradients of the weights, then of the biases (may be null)
+// dst[i] = the sum of src[slice][i]; the gradients of the weights, then of the biases (may be null).  A thread adds up every
+// TEAM-th slice of four values; small gradients of many slices want larger teams (6144 values of 512 slices: 40 us with one
+// thread to four values).
+template <int TEAM>
 __global__ void __launch_bounds__(256) fc_slices_kernel(const float* __restrict__ dw, const float* __restrict__ db, int slices, long n,
                                                         long slab, int out, float* __restrict__ dw_out, float* __restrict__ db_out,
                                                         int dw_blocks) {
   typedef float V4 __attribute__((ext_vector_type(4)));
+  constexpr int kQuads = 256 / TEAM;
+  __shared__ V4 part[TEAM > 1 ? 256 : 1];
   const bool bias = (int)blockIdx.x >= dw_blocks;
-  const long i = ((long)(bias ? blockIdx.x - dw_blocks : blockIdx.x) * 256 + threadIdx.x) * 4;
+  const int t = threadIdx.x, member = t / kQuads;
+  const long i = ((long)(bias ? blockIdx.x - dw_blocks : blockIdx.x) * kQuads + t % kQuads) * 4;
   const long end = bias ? out : n, step = bias ? out : slab;
   const float* const s = (bias ? db : dw) + i;
+  V4 v = {0.f, 0.f, 0.f, 0.f};
+  if (i + 4 <= end) {
+#pragma unroll 4
+    for (int k = member; k < slices; k += TEAM) v += reinterpret_cast<const Loose<V4>*>(s + k * step)->v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < end)
+        for (int k = member; k < slices; k += TEAM) v[e] += s[k * step + e];
+  }
+  if constexpr (TEAM > 1) {
+    part[t] = v;
+    __syncthreads();
+    if (member) return;
+#pragma unroll
+    for (int k = 1; k < TEAM; ++k) v += part[k * kQuads + t];
+  }
   float* const d = (bias ? db_out : dw_out) + i;
   if (i + 4 <= end) {
-    V4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k = 0; k < slices; ++k) v += reinterpret_cast<const Loose<V4>*>(s + k * step)->v;
     reinterpret_cast<Loose<V4>*>(d)->v = v;
   } else {
-    for (int e = 0; i + e < end; ++e) {
-      float v = 0.f;
-      for (int k = 0; k < slices; ++k) v += s[k * step + e];
-      d[e] = v;
-    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < end) d[e] = v[e];
   }
+}
+template <int TEAM>
+static int fc_sum(const FcArgs& a, float* dw, float* db, hipStream_t st) {
+  const long n = (long)a.in * a.out;
+  const int per = 4 * 256 / TEAM, dw_blocks = ceil_div(n, per), blocks = dw_blocks + (db ? ceil_div(a.out, per) : 0);
+  KernelScope ks("checkpoint_weight_sum", 0, 4.0 * n * (a.slices + 1), st);
+  hipLaunchKernelGGL(fc_slices_kernel<TEAM>, dim3((unsigned)blocks), dim3(256), 0, st, a.dw, a.db, a.slices, n, a.dw_slab, a.out, dw, db,
+                     dw_blocks);
+  AX_LAUNCH_CHECK();
+  return ALEXNET_OK;
 }
 
 // zero rows: nothing is summed
@@ -418,12 +446,12 @@ struct FcPlan {
 };
 // The tile and the number of slices that a model of the measured times makes cheapest.  A step of a workgroup that has a
 // compute unit to itself takes kAloneUs microseconds, one among as many as fit kStepUs of the unit's time; slices are written
-// and read once more each.  256 x 9216 x 4096 fp32 (few rows, large dw): 128 x 256 tiles 63 us, 64 x 128 ones 84, two slices 180;
-// 43264 x 384 x 384 bf16: 128 x 256 tiles in 86 slices 37 us, in 43 slices 54, 64 x 128 ones in 56 slices 38, in 12 slices 78,
-// 64 x 64 ones in 64 slices 53; 100000 x 96 x 64 fp32: 64 x 64 tiles in 128 slices 34, 64 x 128 ones in 192 slices 36.
+// and read once more each.  256 x 9216 x 4096 fp32 (few rows, large dw): 128 x 256 tiles 60 us, 64 x 128 ones 84, two slices 180;
+// 43264 x 384 x 384 bf16: 128 x 256 tiles in 86 slices 36 us, in 43 slices 54, 64 x 128 ones in 56 slices 38, in 12 slices 78,
+// 64 x 64 ones in 64 slices 53; 100000 x 96 x 64 fp32: 64 x 128 tiles in 512 slices 20, 64 x 64 ones in 64 slices 41.
 static FcPlan fc_plan(long rows, int in, int out, int type) {
-  static const double kStepUs[3][3] = {{0.19, 0.24, 0.33}, {0.21, 0.3, 0.52}, {0.45, 0.75, 1.06}};  // [tile][terms - 1]
-  static const double kAloneUs[3][3] = {{0.3, 0.45, 0.51}, {0.48, 0.56, 0.68}, {0.8, 1.2, 1.57}};
+  static const double kStepUs[3][3] = {{0.19, 0.25, 0.32}, {0.21, 0.32, 0.44}, {0.46, 0.78, 1.1}};  // [tile][terms - 1]
+  static const double kAloneUs[3][3] = {{0.3, 0.4, 0.48}, {0.5, 0.56, 0.62}, {0.8, 1.1, 1.33}};
   static const int kFit[3] = {4, 4, 2};  // workgroups on a compute unit
   FcPlan best = {};
   double least = 1e300;
@@ -444,7 +472,7 @@ static FcPlan fc_plan(long rows, int in, int out, int type) {
       p.slices = (int)((steps + p.steps - 1) / p.steps);
       const double units = tiles * p.slices / 256, full = std::floor(units / fit), rest = std::ceil(units - full * fit);
       const double each = full * std::max(alone, us * fit) + (rest > 0 ? std::max(alone, us * rest) : 0.0);
-      const double cost = p.steps * each + p.slices * bytes / 8.8e6 + (p.slices > 1 ? 6.8 + p.slices * bytes / 7.1e6 : 0.0);
+      const double cost = p.steps * each + p.slices * bytes / 8.8e6 + (p.slices > 1 ? 4.3 + p.slices * bytes / 6.4e6 : 0.0);
       if (cost < least) {
         least = cost;
         best = p;
@@ -539,12 +567,9 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
   }
   if (!split) return ALEXNET_OK;
   const long n = (long)in * out;
-  const int dw_blocks = ceil_div(n, 1024), blocks = dw_blocks + (d_db ? ceil_div(out, 1024) : 0);
-  KernelScope ks("checkpoint_weight_sum", 0, 4.0 * n * (p.slices + 1), st);
-  hipLaunchKernelGGL(fc_slices_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a.dw, a.db, p.slices, n, (long)p.slab, out, d_dw,
-                     d_db, dw_blocks);
-  AX_LAUNCH_CHECK();
-  return ALEXNET_OK;
+  return n < 1 << 16 && p.slices > 16 ? fc_sum<16>(a, d_dw, d_db, st)
+         : n < 1 << 18 && p.slices > 4 ? fc_sum<4>(a, d_dw, d_db, st)
+                                       : fc_sum<1>(a, d_dw, d_db, st);
 }
 
 }  // extern "C"
