@@ -361,7 +361,7 @@ int alexnet_softmax_xent_static(const float* d_logits, const int32_t* d_labels, 
  * block's largest magnitude is at most 127 (448) and rounds each value to the
  * nearest code (ties to even): off by at most half a step, which is
  * 2^(s - 128) for INT8.  A block with an infinity or a NaN is packed as s = 255
- * and reads back as NaN throughout. */
+ * and reads back as NaN throughout.  One call takes 2^35 values and 2^29 rows. */
 #define ALEXNET_CODE_INT8 0
 #define ALEXNET_CODE_E4M3 1
 typedef struct {
@@ -382,7 +382,8 @@ int alexnet_checkpoint_unpack(const alexnet_checkpoint_t* in, int64_t rows, int3
  * with dy [rows][out] of `type` at row stride ld_dy, products of the unpacked
  * values, float32 sums and results.  No operand is rounded: x is exact in
  * bfloat16 and dy is multiplied as one (BF16), two (FP16) or three (FP32)
- * bfloat16 terms.  rows may be 0 (the gradients are then zero). */
+ * bfloat16 terms; only what lies under 2^-133, the smallest bfloat16 number, is
+ * left off a float32 dy.  rows may be 0 (the gradients are then zero). */
 int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes);
 int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const void* d_dy, int64_t ld_dy, int32_t type,
                                           int64_t rows, int32_t in, int32_t out, float* d_dw, float* d_db,
@@ -394,7 +395,8 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
  *   z = (x - m) * r * gamma[c] + beta[c],  y = act(z)
  * ld_* are pixel strides in elements (>= c): a call can work on a slice of the
  * channels of a wider tensor; pictures follow each other (hw * ld_*).  y may be
- * x and dx may be dy (same pointer and stride); other overlaps are not allowed.
+ * x, and dx may be dy or x (same pointer and stride); other overlaps are refused.
+ * Squares are float32: where deviations from the mean pass 10^19, v is infinite.
  * n and hw may be 0: nothing is read then, the statistics are m = 0 and
  * r = 1/sqrt(eps), the parameter gradients 0. */
 typedef struct {

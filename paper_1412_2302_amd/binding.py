@@ -612,7 +612,8 @@ class Checkpoint:
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         if codes.dtype not in _CODES or scales.dtype != torch.uint8:
             raise ValueError(f"Checkpoint: codes are int8 or float8_e4m3fn and scales uint8, got {codes.dtype} and {scales.dtype}")
-        if codes.dim() < 2 or codes.shape[:-1] != scales.shape[:-1] or scales.shape[-1] != -(-codes.shape[-1] // CODE_BLOCK):
+        if (codes.dim() < 2 or not 1 <= codes.shape[-1] < 1 << 31 or codes.shape[:-1] != scales.shape[:-1]
+                or scales.shape[-1] != -(-codes.shape[-1] // CODE_BLOCK)):
             raise ValueError(f"Checkpoint: scales {list(scales.shape)} do not belong to codes {list(codes.shape)}")
         if not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device:
             raise ValueError("Checkpoint: codes and scales must be contiguous, on one device")
@@ -647,7 +648,7 @@ def _rows_stride(t, what: str) -> int:
         raise ValueError(f"{what}: expected a device tensor, got one on {t.device}")
     if t.dtype not in _TYPES:
         raise ValueError(f"{what}: expected float32, bfloat16 or float16, got {t.dtype}")
-    if t.dim() < 2 or t.shape[-1] < 1:
+    if t.dim() < 2 or not 1 <= t.shape[-1] < 1 << 31:
         raise ValueError(f"{what}: expected [rows]...[channels], got {list(t.shape)}")
     c = t.shape[-1]
     if t.is_contiguous():
@@ -760,7 +761,7 @@ def group_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Opt
 def group_norm_backward(x, dy: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
                         beta: Optional[torch.Tensor], act: str = "none", out: Optional[torch.Tensor] = None, stream=None):
     """(dx, dgamma, dbeta) of group_norm_forward from x, or its Checkpoint, and the forward call's mean and rstd.  out: where dx
-    goes (may be dy)."""
+    goes (may be dy, or x)."""
     what = "group_norm_backward"
     ld_dy = _rows_stride(dy, "group_norm_backward: dy")
     if not _here(dy, stream):

@@ -470,6 +470,7 @@ static FcPlan fc_plan(long rows, int in, int out, int type) {
     for (long s = std::max<long>(1, (rows + kSliceRows - 1) / kSliceRows); s <= std::min<long>(steps, kMaxSlices); s += 1 + s / 8) {
       p.steps = (int)((steps + s - 1) / s);
       p.slices = (int)((steps + p.steps - 1) / p.steps);
+      if (tiles * p.slices >= 1 << 24) continue;  // past the threads of a grid
       const double units = tiles * p.slices / 256, full = std::floor(units / fit), rest = std::ceil(units - full * fit);
       const double each = full * std::max(alone, us * fit) + (rest > 0 ? std::max(alone, us * rest) : 0.0);
       const double cost = p.steps * each + p.slices * bytes / 8.8e6 + (p.slices > 1 ? 4.3 + p.slices * bytes / 6.4e6 : 0.0);
@@ -518,7 +519,10 @@ extern "C" {
 int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes) {
   AX_TRY(fc_check("alexnet_checkpoint_fc_query", rows, in, out, type));
   AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_checkpoint_fc_query: null argument");
-  *workspace_bytes = fc_plan(rows, in, out, type).ws;
+  const FcPlan p = fc_plan(rows, in, out, type);
+  AX_REQUIRE(rows == 0 || p.slices, ALEXNET_ESHAPE, "alexnet_checkpoint_fc_query: %ld rows of %d by %d are more than one launch covers",
+             (long)rows, in, out);
+  *workspace_bytes = p.ws;
   return ALEXNET_OK;
 }
 int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const void* d_dy, int64_t ld_dy, int32_t type,
@@ -535,6 +539,7 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
   AX_TRY(check_checkpoint(x, who));
   AX_REQUIRE(ld_dy >= out, ALEXNET_ESHAPE, "%s: row stride %ld is under %d columns", who, (long)ld_dy, out);
   const FcPlan p = fc_plan(rows, in, out, type);
+  AX_REQUIRE(p.slices, ALEXNET_ESHAPE, "%s: %ld rows of %d by %d are more than one launch covers", who, (long)rows, in, out);
   if (p.ws) {
     AX_REQUIRE(workspace_bytes >= p.ws && d_workspace, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who,
                d_workspace ? workspace_bytes : (size_t)0, p.ws);

@@ -194,6 +194,39 @@ def test_weight_gradient_shows_what_is_not_finite(lib):
     assert torch.equal(dw[rest][:, 64:], clean[rest][:, 64:])
 
 
+def test_weight_gradient_of_a_tiny_dy(lib):
+    """Under 2^-126 down to nothing: what a float32 has under 2^-133 is left off, bfloat16 and float16 lose nothing."""
+    rows, cols, out = 48, 64, 32
+    gen = torch.Generator().manual_seed(12)
+    x = (torch.randn((rows, cols), generator=gen) * 2.0 ** 40).cuda()
+    kept = lib.checkpoint_pack(x, torch.int8)
+    values = f64(lib.checkpoint_unpack(kept))
+    for dtype, scale, lost in ((torch.float32, 2.0 ** -128, 2.0 ** -133), (torch.bfloat16, 2.0 ** -128, 0.0), (torch.float16, 2.0 ** -20, 0.0)):
+        dy = (torch.randn((rows, out), generator=gen).double() * scale).to(dtype).cuda()
+        dw, _ = lib.checkpoint_fc_backward_weight(kept, dy)
+        want, size = f64(dy).T @ values, np.abs(f64(dy)).T @ np.abs(values)
+        assert np.all(np.abs(f64(dw) - want) <= (rows + 64) * R.EPS32 * size + lost * np.abs(values).sum(0))
+        assert np.linalg.norm(want) > 0
+
+
+@pytest.mark.parametrize("code", CODES, ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols,out", [(70, 96, 40), (300, 1030, 257)])
+def test_weight_gradient_of_what_is_not_finite(lib, code, dtype, rows, cols, out):
+    """An infinity or a NaN of dy reaches its own row of dw, a block that is not finite its own columns, and nothing else."""
+    gen = torch.Generator().manual_seed(rows)
+    x, dy = torch.rand((rows, cols), generator=gen) + 0.5, torch.randn((rows, out), generator=gen).to(dtype)
+    clean, clean_b = lib.checkpoint_fc_backward_weight(lib.checkpoint_pack(x.cuda(), code), dy.cuda())
+    dy[0, 1], dy[rows - 1, out - 1] = float("-inf"), float("nan")
+    x[rows - 2, cols - 1] = float("nan")
+    dw, db = lib.checkpoint_fc_backward_weight(lib.checkpoint_pack(x.cuda(), code), dy.cuda())
+    last = (cols - 1) // 32 * 32  # the block
+    assert bool((dw[1, :last] == float("-inf")).all()) and bool(torch.isnan(dw[out - 1]).all()) and bool(torch.isnan(dw[:, last:]).all())
+    assert float(db[1]) == float("-inf") and bool(torch.isnan(db[out - 1]))
+    rest = [i for i in range(out) if i not in (1, out - 1)]
+    assert torch.equal(dw[rest, :last], clean[rest, :last]) and torch.equal(db[rest], clean_b[rest])
+
+
 def test_on_given_buffers_captured_and_on_another_stream(lib):
     gen = torch.Generator().manual_seed(2)
     x, dy = torch.randn((3000, 64), generator=gen).cuda(), torch.randn((3000, 48), generator=gen).cuda()

@@ -76,6 +76,28 @@ def test_arguments_that_are_refused(B):
     assert backward(x=None, kept=B.CheckpointArg(256, 512, 7)) == B.EINVAL
 
 
+def test_results_that_overlap_an_input_are_refused(B):
+    """In place means the same pixels; another place has no byte of the input's."""
+    n, hw, c, ld = 2, 9, 8, 24
+    conf = cfg(B, n=n, hw=hw, c=c)
+    reach = ((n * hw - 1) * ld + c) * 4
+    x = 1 << 20
+
+    def forward(y, ld_y=ld):
+        return B._lib.alexnet_group_norm_forward(conf, x, ld, None, None, y, ld_y, None, None, None, None, 0, None)
+
+    def backward(dx, dy, ld_dx=ld, x=x):
+        ws = 1 << 30  # scratch of two pictures
+        return B._lib.alexnet_group_norm_backward(conf, x, ld, None, dy, ld, 256, 256, None, None, dx, ld_dx, None, None, ws, 1 << 20,
+                                                  None)
+
+    for y, ld_y in [(x + 4, ld), (x - 4, ld), (x + 28, ld), (x - 28, ld), (x + ld * 4, ld), (x + 68, ld), (x, ld + 1), (x, c),
+                    (x + reach - 4, ld), (x + reach - 4, c), (x - reach + 4, ld)]:
+        assert forward(y, ld_y) == B.EINVAL and "overlaps" in B.last_error(), (y - x, ld_y)
+        assert backward(y, 1 << 25, ld_y) == B.EINVAL and "overlaps" in B.last_error()
+        assert backward(y, x, ld_y, 1 << 25) == B.EINVAL and "overlaps" in B.last_error()
+
+
 def test_checkpoint_arguments_that_are_refused(B):
     k = B.CheckpointArg(256, 512, 0)
     pack, unpack, fc = B._lib.alexnet_checkpoint_pack, B._lib.alexnet_checkpoint_unpack, B._lib.alexnet_checkpoint_fc_backward_weight
@@ -92,6 +114,7 @@ def test_checkpoint_arguments_that_are_refused(B):
     assert q(4, 8, 8, 5, ws) == q(4, 8, 8, 0, None) == B.EINVAL
     assert q(-1, 8, 8, 0, ws) == q(4, 0, 8, 0, ws) == q(4, 8, 0, 0, ws) == q(4, 1 << 21, 8, 0, ws) == B.ESHAPE
     assert q(5000, 256, 64, 0, ws) == B.OK
+    assert q(1 << 22, 1 << 17, 1 << 16, 0, ws) == B.ESHAPE and "launch" in B.last_error()  # 1024 slices of 2^17 tiles and more
     big = 1 << 40
 
     def weight(x=k, dy=256, ld=8, kind=0, rows=4, cols=8, out=8, dw=512, db=None, work=1024, size=big):
@@ -118,6 +141,8 @@ def test_the_binding_refuses_tensors_of_the_wrong_kind(B):
         B.Checkpoint(torch.zeros(4, 40, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8))
     with pytest.raises(ValueError, match="int8 or float8"):
         B.Checkpoint(torch.zeros(4, 40), torch.zeros(4, 2, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="belong"):
+        B.Checkpoint(torch.empty(1, 1 << 31, dtype=torch.int8, device="meta"), torch.empty(1, 1 << 26, dtype=torch.uint8, device="meta"))
     with pytest.raises(ValueError, match="contiguous"):
         B.Checkpoint(torch.zeros(40, 4, dtype=torch.int8).t(), torch.zeros(4, 2, dtype=torch.uint8))
     with pytest.raises(ValueError, match="device tensor"):
