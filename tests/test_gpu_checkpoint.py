@@ -227,6 +227,30 @@ def test_weight_gradient_of_what_is_not_finite(lib, code, dtype, rows, cols, out
     assert torch.equal(dw[rest, :last], clean[rest, :last]) and torch.equal(db[rest], clean_b[rest])
 
 
+def test_more_codes_than_32_bits_count(lib):
+    """The last rows of the longest checkpoint: only they have a gradient."""
+    rows, cols, out, tail = 1 << 22, 1030, 5, 40
+    gen = torch.Generator().manual_seed(6)
+    x = torch.randn((tail, cols), generator=gen)
+    some = lib.checkpoint_pack(x.cuda(), torch.int8)
+    codes = torch.ones((rows, cols), dtype=torch.int8, device="cuda")
+    scales = torch.full((rows, some.scales.shape[1]), 127, dtype=torch.uint8, device="cuda")
+    codes[-tail:], scales[-tail:] = some.codes, some.scales
+    kept = lib.Checkpoint(codes, scales)
+    dy = torch.zeros((rows, out), device="cuda")
+    dy[-tail:] = torch.randn((tail, out), generator=gen).cuda()
+    dw, db = lib.checkpoint_fc_backward_weight(kept, dy)
+    values, d = f64(lib.checkpoint_unpack(some)), f64(dy[-tail:])
+    k = (tail + 64) * R.EPS32
+    assert np.all(np.abs(f64(dw) - d.T @ values) <= k * (np.abs(d).T @ np.abs(values)))
+    assert np.all(np.abs(f64(db) - d.sum(0)) <= k * np.abs(d).sum(0))
+    back = lib.checkpoint_unpack(kept, torch.bfloat16)
+    assert torch.equal(back[-tail:], lib.checkpoint_unpack(some, torch.bfloat16)) and bool((back[:tail] == 1).all())
+    again = lib.checkpoint_pack(back, torch.int8)
+    same = lib.checkpoint_pack(back[-tail:], torch.int8)
+    assert torch.equal(again.codes[-tail:], same.codes) and torch.equal(again.scales[-tail:], same.scales)
+
+
 def test_on_given_buffers_captured_and_on_another_stream(lib):
     gen = torch.Generator().manual_seed(2)
     x, dy = torch.randn((3000, 64), generator=gen).cuda(), torch.randn((3000, 48), generator=gen).cuda()

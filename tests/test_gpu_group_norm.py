@@ -120,6 +120,79 @@ def test_in_place(lib, size):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("size", [(1, 4000, 74, 2), (2, 6000, 37, 1), (1, 2000, 1025, 5), (2, 60, 37, 37), (3, 40, 3, 1)], ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_in_place_where_rows_are_no_whole_vectors(lib, size, dtype):
+    """No thread may read what another has already overwritten; dx may also take the place of x."""
+    n, hw, c, groups = size
+    x, dy, gamma, beta = make(n, hw, c, dtype, 10)
+    want = lib.group_norm_forward(x, gamma, beta, groups, 1e-5, "relu")
+    x2 = x.clone()
+    got = lib.group_norm_forward(x2, gamma, beta, groups, 1e-5, "relu", out=x2)
+    check_forward(x, gamma, beta, groups, 1e-5, "relu", got[:3])
+    for over in ("dy", "x"):
+        x2, dy2 = x.clone(), dy.clone()
+        got = lib.group_norm_backward(x2, dy2, want[1], want[2], gamma, beta, "relu", out=dy2 if over == "dy" else x2)
+        check_backward(f64(x).reshape(n, hw, c), dy, want[1], want[2], gamma, beta, "relu", got)
+        assert torch.equal(dy2, dy) if over == "x" else torch.equal(x2, x)
+
+
+@pytest.mark.parametrize("hw", [50, 5000])
+def test_what_overlaps_is_refused(lib, hw):
+    x, dy, gamma, beta = make(2, hw, 24, torch.float32, 12)
+    y, mean, rstd, _ = lib.group_norm_forward(x, gamma, beta, 3)
+    room = torch.zeros((2, hw, 60), device="cuda")
+    inside = room[..., 10:34]
+    inside.copy_(x)
+    for a in (11, 33, 0):
+        with pytest.raises(Exception, match="overlaps"):
+            lib.group_norm_forward(inside, gamma, beta, 3, out=room[..., a:a + 24])
+    got = lib.group_norm_forward(inside, gamma, beta, 3, out=room[..., 34:58])[0]
+    assert torch.equal(got.contiguous(), y) and torch.equal(inside.contiguous(), x)
+    with pytest.raises(Exception, match="overlaps"):
+        lib.group_norm_backward(x, inside, mean, rstd, gamma, beta, out=room[..., 12:36])
+
+
+def test_more_values_than_31_bits_count(lib):
+    n, hw, c, groups = 2, (1 << 25) + 3, 40, 4
+    x = torch.randn((n, hw, c), device="cuda", dtype=torch.bfloat16)
+    x[1] += 2.0
+    gamma, beta = torch.randn(c, device="cuda"), torch.randn(c, device="cuda")
+    y, mean, rstd, kept = lib.group_norm_forward(x, gamma, beta, groups, 1e-5, "silu", checkpoint=torch.int8)
+    last = x[1].view(hw, groups, c // groups)
+    for g in range(groups):
+        part = last[:, g].double()
+        m, r = float(part.mean()), float(1 / torch.sqrt(part.var(unbiased=False) + 1e-5))
+        size = float(part.abs().mean())
+        # a chunk of the picture is no longer than a thousand groups of four pixels a thread
+        off = 2048 * R.EPS32 * size
+        assert abs(float(mean[1, g]) - m) <= off and abs(float(rstd[1, g]) / r - 1) <= 2048 * R.EPS32 + (off * r) ** 2
+    end = x[1, -1000:].contiguous()
+    codes = lib.checkpoint_pack(end, torch.int8)
+    assert torch.equal(kept.codes[1, -1000:], codes.codes) and torch.equal(kept.scales[1, -1000:], codes.scales)
+    wide = (mean[1].repeat_interleave(c // groups), rstd[1].repeat_interleave(c // groups))
+    z = (end.double() - wide[0].double()) * wide[1].double() * gamma.double() + beta.double()
+    want = z * torch.sigmoid(z)
+    off = 16 * R.EPS32 * (1 + z.abs()) * (1 + want.abs() + (end.double() * wide[1] * gamma).abs() + (wide[0] * wide[1] * gamma).abs())
+    assert bool(((y[1, -1000:].double() - want).abs() <= off + want.abs() * R.HALF_STEP[torch.bfloat16] * 1.01).all())
+    dy = y  # any gradient will do; in place
+    tail = dy[1, -1000:].clone().double()
+    dx, dgamma, dbeta = lib.group_norm_backward(kept, dy, mean, rstd, gamma, beta, "none", out=dy)
+    values = lib.checkpoint_unpack(codes).double()
+    hat = (values - wide[0].double()) * wide[1].double()
+    # the means over the group are what every pixel of a channel has in common
+    rest = wide[1].double() * gamma.double() * tail - dx[1, -1000:].double()
+    rest = rest.view(1000, groups, c // groups)
+    for g in range(groups):
+        a = torch.stack([torch.ones(10000, device="cuda", dtype=torch.float64), hat.view(1000, groups, -1)[:, g].reshape(-1)], 1)
+        t = rest[:, g].reshape(-1, 1)
+        fit = torch.linalg.lstsq(a.cpu(), t.cpu()).solution
+        # what is left is the rounding of dx to bfloat16
+        left = (t.cpu() - a.cpu() @ fit).abs()
+        assert float(left.max()) <= float(dx[1, -1000:].double().abs().max()) * R.HALF_STEP[torch.bfloat16] * 2
+    assert bool(torch.isfinite(dgamma).all()) and bool(torch.isfinite(dbeta).all())
+
+
 def test_without_gamma_and_beta_and_on_maps(lib):
     x, dy, _, _ = make(2, 30, 20, torch.float32, 11)
     x4, dy4 = x.view(2, 5, 6, 20), dy.view(2, 5, 6, 20)
