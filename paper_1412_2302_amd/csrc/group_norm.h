@@ -35,8 +35,10 @@ struct GnArgs {
   int slab_groups, slabs;
   // Scratch.  part [n][chunks][2][slots]: what a chunk found for a group, per block of columns that the group lies in; that of
   // group g in block b is slot g + b (going along the channels either the group or the block changes, so no two share a slot).
-  // part_c [n][chunks][2][c]: the same per channel (gradients only).  stat [n][groups][2].
+  // part_c [n][chunks][2][c]: the same per channel (gradients only).  stat [n][groups][2], unless join: then every workgroup of
+  // the last launch joins its picture's chunks itself.
   float *part, *part_c, *stat;
+  int join;
 };
 
 // V channels from c on, of which the first `dup` are another thread's too

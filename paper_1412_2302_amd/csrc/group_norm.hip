@@ -1,7 +1,7 @@
 // Group normalisation with an activation over channel-last activations, forward and backward: the kernels for maps of any
 // size, and the entry points.  Maps whose groups fit a workgroup's registers go to group_norm_resident.hip, which reads its
-// inputs once; here a first launch sums over chunks of pixels, a second joins the chunks and a third reads the inputs again and
-// writes the result.
+// inputs once; here a first launch sums over chunks of pixels, and a second joins the chunks, reads the inputs again and writes the
+// result (many groups or chunks are joined by a launch between the two).
 #include <math.h>
 
 #include <algorithm>
@@ -217,25 +217,83 @@ __global__ void __launch_bounds__(256) gn_statistics_kernel(GnArgs a, int width)
   }
 }
 
+// What a picture's chunks found, joined by a workgroup for itself where that is little: by as many threads to a group as there
+// are, in 64 bits, in one pass.  (Meanwhile its first pixels are on their way.)  out [groups]: mean and rstd of x, or (GRADS) the means that dx subtracts.
+constexpr int kJoinGroups = 256;
+struct Joined {
+  double sum[2][256];
+  float out[kJoinGroups][2];
+};
+template <bool GRADS>
+__device__ __forceinline__ void join_chunks(const GnArgs& a, int n, Joined& lds) {
+  const int t = threadIdx.x, team = 256 / a.groups, member = t / a.groups, g = t - member * a.groups;
+  const float* const part = a.part + (long)n * a.chunks * 2 * a.groups + g;
+  // deviations from the first chunk's mean, so that a mean far from zero costs no digits
+  const float first = GRADS ? 0.f : part[0], from = fabsf(first) < INFINITY ? first : 0.f;
+  double s0 = 0., s1 = 0.;
+  if (member < team) {
+#pragma unroll 4
+    for (int k = member; k < a.chunks; k += team) {
+      const double m = part[(long)k * 2 * a.groups], q = part[(long)k * 2 * a.groups + a.groups];
+      if (GRADS) {
+        s0 += m;
+        s1 += q;
+      } else {
+        const double w = (double)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) * a.cpg, d = m - from;
+        s0 += w * d;
+        s1 += q + w * d * d;
+      }
+    }
+  }
+  lds.sum[0][t] = s0;
+  lds.sum[1][t] = s1;
+  __syncthreads();
+  if (t < a.groups) {
+    for (int k = 1; k < team; ++k) {
+      s0 += lds.sum[0][k * a.groups + t];
+      s1 += lds.sum[1][k * a.groups + t];
+    }
+    const double inv = 1. / ((double)a.hw * a.cpg), mean = s0 * inv;
+    lds.out[t][0] = (float)(GRADS ? mean : from + mean);
+    lds.out[t][1] = GRADS ? (float)(s1 * inv) : 1.f / sqrtf((float)((s1 - s0 * mean) * inv) + a.eps);
+  }
+  __syncthreads();
+}
+
 template <typename T, int V>
-__global__ void __launch_bounds__(256) gn_apply_kernel(GnArgs a) {
+__global__ void __launch_bounds__(256, 6) gn_apply_kernel(GnArgs a) {
+  __shared__ Joined lds;
   const Spot s = spot(a, gridDim.x - 1 - blockIdx.x);  // backwards: what the sums' launch read last is still cached
-  if (!s.has) return;
   const Vec v = vec_of<V>(s.v, 0, a.c);
+  typename Pack<T, V>::Raw r[kUnroll];
+  const auto load = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (p + u * a.rpi < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_x + v.c);
+  };
+  int p = s.p0 + s.row;
+  if (s.has) load(p);
+  const float* stat = a.stat + 2 * s.n * a.groups;
+  if (a.join) {
+    join_chunks<false>(a, s.n, lds);
+    stat = lds.out[0];
+    const int t = threadIdx.x;
+    if (s.chunk == 0 && t < a.groups) {
+      if (a.mean_out) a.mean_out[s.n * a.groups + t] = stat[2 * t];
+      if (a.rstd_out) a.rstd_out[s.n * a.groups + t] = stat[2 * t + 1];
+    }
+  }
+  if (!s.has) return;
   float mean[V], scale[V], beta[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int ch = v.c + i, g = s.n * a.groups + ch / a.cpg;
-    mean[i] = a.stat[2 * g];
-    scale[i] = a.stat[2 * g + 1] * (a.gamma ? a.gamma[ch] : 1.f);
+    const int ch = v.c + i, g = ch / a.cpg;
+    mean[i] = stat[2 * g];
+    scale[i] = stat[2 * g + 1] * (a.gamma ? a.gamma[ch] : 1.f);
     beta[i] = a.beta ? a.beta[ch] : 0.f;
   }
   with_act(a.act, [&](auto act) {
-    for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
-      typename Pack<T, V>::Raw r[kUnroll];
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (p + u * a.rpi < s.p1) r[u] = Pack<T, V>::load((const T*)a.x + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_x + v.c);
+    for (; p < s.p1; p += kUnroll * a.rpi) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
         if (p + u * a.rpi < s.p1) {
@@ -245,6 +303,7 @@ __global__ void __launch_bounds__(256) gn_apply_kernel(GnArgs a) {
           for (int i = 0; i < V; ++i) f[i] = activate<decltype(act)::value>(__builtin_fmaf(f[i] - mean[i], scale[i], beta[i]));
           Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, f);
         }
+      load(p + kUnroll * a.rpi);
     }
   });
 }
@@ -394,6 +453,11 @@ __global__ void __launch_bounds__(256) gn_grad_means_kernel(GnArgs a, int width)
     a.stat[2 * (long)id + 1] = g * inv;
   }
 }
+// Whether the last launch's workgroups join the chunks themselves, which saves a launch of 4 to 6 us and costs each of them the
+// reading of all its picture's pairs.  Forward and backward with it and without, us: 64 x 3025 x 96 fp32, 96 groups of 16 chunks,
+// 44 + 75, 49 + 77; 2 x 51529 x 64, 32 groups of 202 chunks, 24.3 + 29.8, 25.3 + 31.0; 64 groups of them 27.1 + 32.7, 25.6 + 31.5;
+// 1 x 51529 x 128, 128 groups of them 41 + 47, 24 + 31.
+static bool joins(const GnArgs& a) { return a.col_blocks == 1 && a.groups <= kJoinGroups && (long)a.groups * a.chunks <= 8192; }
 static bool few_terms(const GnArgs& a, int width) { return (long)a.chunks * (a.cpg / width + 2) <= 512; }
 
 // dbeta and dgamma of eight channels, the sums over pictures and chunks, by a workgroup of THREADS; lds: 2 * THREADS floats
@@ -436,36 +500,48 @@ static int total_blocks(const GnArgs& a) { return a.dbeta || a.dgamma ? ceil_div
 // Its first workgroups, total_blocks of them, leave dbeta and dgamma meanwhile.
 template <typename T, int V, int SRC>
 __global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a, int total_blocks) {
-  __shared__ float lds[512];
+  __shared__ union {
+    float totals[512];
+    Joined joined;
+  } lds;
   if ((int)blockIdx.x < total_blocks) {
-    channel_totals<256>(a, blockIdx.x, lds);
+    channel_totals<256>(a, blockIdx.x, lds.totals);
     return;
   }
   const Spot s = spot(a, gridDim.x - 1 - blockIdx.x);  // backwards, as in gn_apply_kernel
-  if (!s.has) return;
   const Vec v = vec_of<V>(s.v, 0, a.c);
+  typename Source<T, V, SRC>::Raw x[kUnroll];
+  typename Pack<T, V>::Raw d[kUnroll];
+  const auto load = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (p + u * a.rpi < s.p1) {
+        const long row = (long)s.n * a.hw + p + u * a.rpi;
+        Source<T, V, SRC>::load(a, row, v, x[u]);
+        d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
+      }
+  };
+  int p = s.p0 + s.row;
+  if (s.has) load(p);
+  const float* stat = a.stat + 2 * s.n * a.groups;
+  if (a.join) {
+    join_chunks<true>(a, s.n, lds.joined);
+    stat = lds.joined.out[0];
+  }
+  if (!s.has) return;
   float mean[V], rstd[V], gamma[V], beta[V], ma[V], mb[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int ch = v.c + i, g = s.n * a.groups + ch / a.cpg;
+    const int ch = v.c + i, group = ch / a.cpg, g = s.n * a.groups + group;
     mean[i] = a.mean[g];
     rstd[i] = a.rstd[g];
     gamma[i] = a.gamma ? a.gamma[ch] : 1.f;
     beta[i] = a.beta ? a.beta[ch] : 0.f;
-    ma[i] = a.stat[2 * g];
-    mb[i] = a.stat[2 * g + 1];
+    ma[i] = stat[2 * group];
+    mb[i] = stat[2 * group + 1];
   }
   with_act(a.act, [&](auto act) {
-    for (int p = s.p0 + s.row; p < s.p1; p += kUnroll * a.rpi) {
-      typename Source<T, V, SRC>::Raw x[kUnroll];
-      typename Pack<T, V>::Raw d[kUnroll];
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (p + u * a.rpi < s.p1) {
-          const long row = (long)s.n * a.hw + p + u * a.rpi;
-          Source<T, V, SRC>::load(a, row, v, x[u]);
-          d[u] = Pack<T, V>::load((const T*)a.dy + row * a.ld_dy + v.c);
-        }
+    for (; p < s.p1; p += kUnroll * a.rpi) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
         if (p + u * a.rpi < s.p1) {
@@ -479,6 +555,7 @@ __global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a, int total_
           Pack<T, V>::store((T*)a.out + ((long)s.n * a.hw + p + u * a.rpi) * a.ld_out + v.c, df);
           __builtin_amdgcn_sched_barrier(0);
         }
+      load(p + kUnroll * a.rpi);
     }
   });
 }
@@ -615,7 +692,8 @@ static int gn_forward(GnArgs a, int keep, hipStream_t st) {
     else
       GN_LAUNCH((gn_moments_kernel<T, V, ALEXNET_CODE_E4M3>), blocks, 256, st, a);
   }
-  {
+  a.join = joins(a);
+  if (!a.join) {
     KernelScope ks("gn_statistics", 0, 0, st);
     const int width = a.cols * V;
     if (few_terms(a, width))
@@ -639,7 +717,8 @@ static int gn_backward(GnArgs a, hipStream_t st) {
     KernelScope ks("gn_grad_sums", 0, in, st);
     GN_LAUNCH((gn_grad_sums_kernel<T, V, SRC>), blocks, 256, st, a);
   }
-  {
+  a.join = joins(a);
+  if (!a.join) {
     KernelScope ks("gn_grad_means", 0, 0, st);
     const int width = a.cols * V;
     if (few_terms(a, width))
