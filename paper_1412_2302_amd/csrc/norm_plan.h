@@ -20,8 +20,9 @@ struct SlabPlan {
 // Forward, 256 x 729 x 256 bf16: 32 channels 52 us, 16 channels 62, 8 channels 76, three launches 85; 64 x 4096 x 128 bf16: 512
 // threads 36, 1024 threads 58, three launches 56.  Backward, 256 x 729 x 256 fp32: 16 channels and 512 threads 137, 32 channels
 // and 1024 threads 146, three launches 237; 128 x 3025 x 96 fp32: 12 channels and 1024 threads 229, three launches 175.
-inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, int max_regs_1024, bool blocks32, int sums, int narrow) {
+inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, int max_regs_1024, bool blocks32, int sums, int narrow, int line) {
   const int cpg = c / groups, lanes = blocks32 ? 32 / V : 1;
+  const int enough = (long)n * ((c + line - 1) / line) >= 512 ? line : 32;
   SlabPlan best, large;
   // slabs start on whole blocks of 32 channels: their groups' channels are a multiple of 32, or all there are
   int unit = 1;
@@ -53,7 +54,7 @@ inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs,
           best = p;
         else if (width >= narrow || k >= groups)
           large = p;
-        if (width >= 32 || (width >= 16 && few)) break;
+        if (width >= enough || (width >= 16 && few)) break;
       }
     }
     if (k >= groups) break;
