@@ -614,10 +614,10 @@ static GnArgs gn_args(const alexnet_group_norm_t* cfg) {
 }
 static bool empty(const alexnet_group_norm_t* cfg) { return cfg->n == 0 || cfg->hw == 0; }
 static SlabPlan forward_plan(const GnArgs& a, size_t size, bool keep) {
-  return slab_plan(a.n, a.hw, a.c, a.groups, 16 / (int)size, kForwardRegs, kForwardRegs, keep, 1, 12, 128 / (int)size);
+  return slab_plan(a.n, a.hw, a.c, a.groups, 16 / (int)size, kForwardRegs, kForwardRegs, keep, 1, 12, 128 / (int)size, 32 / (int)size);
 }
-static SlabPlan backward_plan(const GnArgs& a) {
-  return slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, kBackwardRegs1024, false, 2, 16, 32);
+static SlabPlan backward_plan(const GnArgs& a, size_t size) {
+  return slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, kBackwardRegs1024, false, 2, 16, 32, 32 / (int)size);
 }
 // Scratch: sums per chunk and channel, then the groups' statistics; for chunks the larger of the two ways to cut rows into
 // threads (one value a thread: tiny or in-place odd rows).
@@ -640,7 +640,7 @@ static size_t forward_ws(const alexnet_group_norm_t* cfg, bool keep) {
 static size_t backward_ws(const alexnet_group_norm_t* cfg) {
   const GnArgs a = gn_args(cfg);
   if (empty(cfg)) return 0;
-  if (backward_plan(a).groups) return a.n > 1 ? align256((size_t)a.n * 2 * a.c * sizeof(float)) : 0;
+  if (backward_plan(a, type_size(cfg->type)).groups) return a.n > 1 ? align256((size_t)a.n * 2 * a.c * sizeof(float)) : 0;
   return chunk_bytes(a, kBackwardVec, false, true) + stat_bytes(a);
 }
 // the chunks' sums from the start, the statistics at the end
@@ -745,7 +745,7 @@ static int gn_forward_type(const GnArgs& a, int type, int keep, hipStream_t st) 
 }
 template <typename T, int SRC>
 static int gn_backward_src(GnArgs a, int type, hipStream_t st) {
-  const SlabPlan p = backward_plan(a);
+  const SlabPlan p = backward_plan(a, sizeof(T));
   if (p.groups) {
     a.part_c = a.part;
     a.chunks = a.col_blocks = 1;

@@ -20,7 +20,7 @@ struct SlabPlan {
 // Forward, 256 x 729 x 256 bf16: 32 channels 52 us, 16 channels 62, 8 channels 76, three launches 85; 64 x 4096 x 128 bf16: 512
 // threads 36, 1024 threads 58, three launches 56.  Backward, 256 x 729 x 256 fp32: 16 channels and 512 threads 137, 32 channels
 // and 1024 threads 146, three launches 237; 128 x 3025 x 96 fp32: 12 channels and 1024 threads 229, three launches 175.
-inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, int max_regs_1024, bool blocks32, int sums, int narrow, int line) {
+inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, int max_regs_1024, bool blocks32, int sums, int narrow, int line, int least) {
   const int cpg = c / groups, lanes = blocks32 ? 32 / V : 1;
   const int enough = (long)n * ((c + line - 1) / line) >= 512 ? line : 32;
   SlabPlan best, large;
@@ -48,8 +48,8 @@ inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs,
       }
       const long lds = 4L * ((long)sums * p.threads * V + 2 * k);
       const bool fits = p.rpi > 0 && p.regs <= (p.threads == 1024 ? max_regs_1024 : max_regs) && lds <= 65536;
-      if (!fits && (best.groups || large.groups)) break;  // wider ones do not fit either
-      if (fits) {
+      if (!fits) break;  // wider ones do not fit either
+      if (width >= least || k >= groups) {
         if (p.threads < 1024 || few)
           best = p;
         else if (width >= narrow || k >= groups)

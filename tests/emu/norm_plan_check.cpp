@@ -16,7 +16,7 @@ static int fail(const char* what, int n, int hw, int c, int g, int V) {
 
 static int check(int n, int hw, int c, int g, int V, int regs, int regs1024, bool b32, int sums, int narrow, long* taken) {
   const int cpg = c / g;
-  const SlabPlan p = slab_plan(n, hw, c, g, V, regs, regs1024, b32, sums, narrow, sums == 1 ? 8 * V : 32);
+  const SlabPlan p = slab_plan(n, hw, c, g, V, regs, regs1024, b32, sums, narrow, sums == 1 ? 8 * V : 32, 8);
   if (!p.groups) return 0;
   ++*taken;
 #define NEED(x) \
