@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
   }
   __syncthreads();
   // one thread per channel joins the rows' pairs, then one or a wave per group the channels'
-  const int pixels = s.p1 - s.p0, width = a.cols * V;
+  const int pixels = s.p1 - s.p0, width = a.cols * V, each = pixels / a.rpi, rest = pixels - each * a.rpi;
   const Columns c = columns<V>(a, blockIdx.x);
   float pm[V], pq[V];
 #pragma unroll
@@ -108,16 +108,15 @@ __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
     const int j = threadIdx.x + 256 * k;
     if (j >= width) break;
     float sum = 0.f;
-    for (int r = 0; r < a.rpi; ++r) {
-      const int cnt = r < pixels ? (pixels - r + a.rpi - 1) / a.rpi : 0;
-      sum = __builtin_fmaf((float)cnt, sm[r * width + j], sum);
-    }
+#pragma unroll 4
+    for (int r = 0; r < a.rpi; ++r) sum = __builtin_fmaf((float)(each + (r < rest)), sm[r * width + j], sum);
     pm[k] = sum / (float)pixels;
     pq[k] = 0.f;
-    for (int r = 0; r < a.rpi; ++r) {
-      const int cnt = r < pixels ? (pixels - r + a.rpi - 1) / a.rpi : 0;
-      const float d = sm[r * width + j] - pm[k];
-      if (cnt) pq[k] += __builtin_fmaf(d * d, (float)cnt, sq[r * width + j]);
+#pragma unroll 4
+    for (int r = 0; r < a.rpi; ++r) {  // rows of no pixel have left zeros
+      const int cnt = each + (r < rest);
+      const float d = cnt ? sm[r * width + j] - pm[k] : 0.f;
+      pq[k] += __builtin_fmaf(d * d, (float)cnt, sq[r * width + j]);
     }
   }
   __syncthreads();

@@ -45,7 +45,7 @@ __device__ __forceinline__ void channel_sums(const GnArgs& a, const Slab& s, Vec
         if (i >= v.dup) lds[k * stride + s.row * w + v.c - s.c0 + i] = x[k][i];
   }
   __syncthreads();
-  const int parts = threads / w;  // 0: more channels than threads, at most V rows of them
+  const int parts = min(threads / w, 24);  // 0: more channels than threads, at most V rows of them
   if (a.rpi == 1) return;
   if (parts > 1) {
     const int part = t / w, ch = t - part * w;

@@ -11,15 +11,19 @@ struct SlabPlan {
   int threads = 0, cols = 0, rpi = 0, regs = 0;
 };
 
-// V channels a thread and pixel, at most max_regs pixels a thread (max_regs_1024 of 1024 threads); blocks32: slabs and threads in whole blocks of 32 channels;
-// sums: values per channel that the workgroup adds up, in 64 KB of LDS at most; narrow: the least channels of a pixel that
-// 1024 threads take (unless those are all).
+// V channels a thread and pixel, at most max_regs pixels a thread (max_regs_1024 of 1024 threads); blocks32: slabs and threads in
+// whole blocks of 32 channels; sums: values per channel that the workgroup adds up, in 64 KB of LDS at most; narrow: the least
+// channels of a pixel that 1024 threads take (unless those are all); line: channels of a 128-byte line; least: of 32 bytes.
 //
-// A wider slab makes better use of memory lines, up to 32 channels or so; at most 512 threads let a second workgroup load while
-// the first one adds up.  So: the widest up to 32 channels that 512 threads hold, if those are 16 channels; else 1024 threads.
-// Forward, 256 x 729 x 256 bf16: 32 channels 52 us, 16 channels 62, 8 channels 76, three launches 85; 64 x 4096 x 128 bf16: 512
-// threads 36, 1024 threads 58, three launches 56.  Backward, 256 x 729 x 256 fp32: 16 channels and 512 threads 137, 32 channels
-// and 1024 threads 146, three launches 237; 128 x 3025 x 96 fp32: 12 channels and 1024 threads 229, three launches 175.
+// A wider slab makes better use of memory lines; at most 512 threads let a second workgroup load while the first one adds up; and
+// few workgroups want few pixels a thread.  So: the widest up to 32 channels (a line, if 512 workgroups are left then) that 512
+// threads hold, if those are 16 channels; else 1024 threads, with more than eight pixels each only in 1024 workgroups or on half
+// lines; under 256 workgroups four pixels a thread if that can be; and chunks where only slabs of less than 32 bytes would fit.
+// Measured, us.  Forward, 256 x 729 x 256 bf16: 64 channels 46, 32 channels 49, 16 channels 58, 8 channels 75, chunks 63;
+// 64 x 1024 x 128 bf16: 32 channels 15.4, 64 channels (128 workgroups) 19.0; 64 x 4096 x 128 fp32: 16 channels and 1024 threads
+// 58, chunks 85; 16 x 3025 x 384 fp32: 12 channels and 1024 threads of nine pixels 51, chunks 44; 16 x 2000 x 128 fp32: 512
+// threads of 16 pixels 21.6, 1024 threads of eight 14.6.  Backward, 256 x 729 x 256 fp32: 16 channels and 512 threads 127, 8
+// channels 162, chunks 191; 64 x 4096 x 128 bf16: 4 channels 132, chunks 69.
 inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs, int max_regs_1024, bool blocks32, int sums, int narrow, int line, int least) {
   const int cpg = c / groups, lanes = blocks32 ? 32 / V : 1;
   const int enough = (long)n * ((c + line - 1) / line) >= 512 ? line : 32;
@@ -38,18 +42,20 @@ inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs,
     if (cols > 1024) break;
     if (std::min(width, last) >= V) {
       p.cols = (int)cols;
-      const bool few = (long)n * p.slabs < 128;  // then more threads, at four pixels each
+      const long wgs = (long)n * p.slabs;
+      const bool few = wgs < 256;  // then more threads, at four pixels each
+      const int most_1024 = wgs >= 1024 || (!few && width >= line / 2) ? max_regs_1024 : std::min(8, max_regs_1024);
       for (int threads : {256, 512, 1024}) {
         p.threads = threads;
         p.rpi = (int)(threads / cols);
         if (!p.rpi) continue;
         p.regs = (hw + p.rpi - 1) / p.rpi;
-        if (p.regs <= (few ? 4 : threads == 1024 ? max_regs_1024 : max_regs)) break;
+        if (p.regs <= (few ? 4 : threads == 1024 ? most_1024 : max_regs)) break;
       }
       const long lds = 4L * ((long)sums * p.threads * V + 2 * k);
       const bool fits = p.rpi > 0 && p.regs <= (p.threads == 1024 ? max_regs_1024 : max_regs) && lds <= 65536;
       if (!fits) break;  // wider ones do not fit either
-      if (width >= least || k >= groups) {
+      if ((width >= (few ? least / 2 : least) || k >= groups) && (p.threads < 1024 || p.regs <= most_1024)) {
         if (p.threads < 1024 || few)
           best = p;
         else if (width >= narrow || k >= groups)
