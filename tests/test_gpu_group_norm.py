@@ -87,6 +87,20 @@ def test_forward_and_backward(lib, size, dtype):
         check_backward(xf, dy, mean, rstd, gamma, beta, act, got)
 
 
+@pytest.mark.parametrize("size", [(2, 3000, 300, 300), (1, 60000, 128, 128), (1, 60000, 128, 8), (3, 9000, 256, 256), (2, 4000, 64, 2)], ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_groups_and_chunks_of_every_number(lib, size, dtype):
+    """Few pairs of a picture are joined where they are used, many by a launch of their own."""
+    n, hw, c, groups = size
+    x, dy, gamma, beta = make(n, hw, c, dtype, 77)
+    y, mean, rstd, _ = lib.group_norm_forward(x, gamma, beta, groups, 1e-5, "silu")
+    check_forward(x, gamma, beta, groups, 1e-5, "silu", (y, mean, rstd))
+    check_backward(f64(x), dy, mean, rstd, gamma, beta, "silu", lib.group_norm_backward(x, dy, mean, rstd, gamma, beta, "silu"))
+    x += 300  # a mean far from zero
+    y, mean, rstd, _ = lib.group_norm_forward(x, gamma, beta, groups, 1e-5, "none")
+    check_forward(x, gamma, beta, groups, 1e-5, "none", (y, mean, rstd))
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("wide", [1, 8, 32])
 def test_slices_of_wider_tensors_leave_the_rest_alone(lib, dtype, wide):
