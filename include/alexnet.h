@@ -342,7 +342,10 @@ int alexnet_softmax_xent_static(const float* d_logits, const int32_t* d_labels, 
  *
  * TYPE: elements of activations and their gradients; everything else
  * (statistics, gamma, beta and their gradients, sums) is float32.  Pointers are
- * aligned to their element and no more. */
+ * aligned to their element and no more.  What a call writes (results, a
+ * checkpoint, scratch) may overlap neither what it reads nor what else it
+ * writes, or it is refused; where a result may take an input's place, the call
+ * says so. */
 #define ALEXNET_TYPE_FP32 0
 #define ALEXNET_TYPE_BF16 1
 #define ALEXNET_TYPE_FP16 2
@@ -395,7 +398,7 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
  *   z = (x - m) * r * gamma[c] + beta[c],  y = act(z)
  * ld_* are pixel strides in elements (>= c): a call can work on a slice of the
  * channels of a wider tensor; pictures follow each other (hw * ld_*).  y may be
- * x, and dx may be dy or x (same pointer and stride); other overlaps are refused.
+ * x, and dx may be dy or x (same pointer and stride).
  * Squares are float32: where deviations from the mean pass 10^19, v is infinite.
  * n and hw may be 0: nothing is read then, the statistics are m = 0 and
  * r = 1/sqrt(eps), the parameter gradients 0. */

@@ -124,6 +124,12 @@ static int checkpoint_call(const char* who, const alexnet_checkpoint_t* k, const
   AX_TRY(check_checkpoint(k, who));
   AX_REQUIRE(ld >= cols, ALEXNET_ESHAPE, "%s: row stride %ld is under %d columns", who, (long)ld, cols);
   AX_REQUIRE(((uintptr_t)x | (uintptr_t)out) % type_size(type) == 0, ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
+  const Buffer map = {x ? "x" : "the result", Region(x ? x : out, rows, ld * (long)type_size(type), cols * (long)type_size(type)), false};
+  const Buffer codes = {"the checkpoint's codes", codes_of(k, rows, cols), false}, scales = {"the checkpoint's scales", scales_of(k, rows, cols), false};
+  if (x)
+    AX_TRY(check_apart(who, {map}, {codes, scales}));
+  else
+    AX_TRY(check_apart(who, {codes, scales}, {map}));
   CodeArgs a = {};
   a.x = x;
   a.out = out;

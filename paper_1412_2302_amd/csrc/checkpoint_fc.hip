@@ -548,6 +548,14 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
                d_workspace ? workspace_bytes : (size_t)0, p.ws);
     AX_REQUIRE((uintptr_t)d_workspace % 256 == 0, ALEXNET_EALIGN, "%s: workspace is not 256-byte aligned", who);
   }
+  const long size = (long)type_size(type);
+  AX_TRY(check_apart(who,
+                     {{"the checkpoint's codes", codes_of(x, rows, in), false},
+                      {"the checkpoint's scales", scales_of(x, rows, in), false},
+                      {"dy", Region(d_dy, rows, ld_dy * size, out * size), false}},
+                     {{"dw", Region(d_dw, 4L * in * out), false},
+                      {"db", Region(d_db, 4L * out), false},
+                      {"the workspace", Region(p.ws ? d_workspace : nullptr, (long)p.ws), false}}));
   FcArgs a = {};
   a.codes = (const uint8_t*)x->d_codes;
   a.scales = (const uint8_t*)x->d_scales;

@@ -7,7 +7,10 @@
 // bits: bf16 holds it exactly, so the matrix instructions take a checkpoint without rounding it a second time.  A block with
 // an infinity or a NaN gets scale code 255 and reads back as NaN: a diverged layer stays visible.
 #pragma once
+#include <initializer_list>
+
 #include "common.h"
+#include "overlap.h"
 
 namespace ax {
 
@@ -30,6 +33,28 @@ inline bool type_ok(int type) { return type >= ALEXNET_TYPE_FP32 && type <= ALEX
 
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 inline size_t type_size(int type) { return type == ALEXNET_TYPE_FP32 ? 4 : 2; }
+
+// A buffer of a call.  map: activations, of which a result may take the place of an input, pixel for pixel.
+struct Buffer {
+  const char* name;
+  Region at;
+  bool map;
+};
+// Workgroups read while others write: what a call writes lies apart from what it reads, and from what else it writes.
+inline int check_apart(const char* who, std::initializer_list<Buffer> reads, std::initializer_list<Buffer> writes) {
+  for (const Buffer* w = writes.begin(); w != writes.end(); ++w) {
+    for (const Buffer& r : reads)
+      AX_REQUIRE((w->map && r.map && w->at.same(r.at)) || !w->at.meets(r.at), ALEXNET_EINVAL, "%s: %s overlaps %s%s", who, w->name, r.name,
+                 w->map && r.map ? " without being in its place" : "");
+    for (const Buffer* v = writes.begin(); v != w; ++v)
+      AX_REQUIRE(!w->at.meets(v->at), ALEXNET_EINVAL, "%s: %s overlaps %s", who, w->name, v->name);
+  }
+  return ALEXNET_OK;
+}
+inline Region codes_of(const alexnet_checkpoint_t* k, long rows, long cols) { return Region(k ? k->d_codes : nullptr, rows * cols); }
+inline Region scales_of(const alexnet_checkpoint_t* k, long rows, long cols) {
+  return Region(k ? k->d_scales : nullptr, rows * ceil_div(cols, kCodeBlock));
+}
 
 // A type that may be read or written at any address: the hardware takes vector accesses at any
 template <typename R>

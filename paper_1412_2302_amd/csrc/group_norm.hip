@@ -657,22 +657,13 @@ static int check_scratch(const char* who, const void* ws, size_t bytes, size_t n
   return ALEXNET_OK;
 }
 
-// Whether two maps of `rows` pixels of c elements share memory: ranges that lie apart do not, nor do slices of the same pixels
-// that have no channel in common; of different strides none are taken apart.
-static bool share(const void* p, long ld_p, const void* q, long ld_q, long rows, long c, long size) {
-  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-  if (a + (uintptr_t)(((rows - 1) * ld_p + c) * size) <= b || b + (uintptr_t)(((rows - 1) * ld_q + c) * size) <= a) return false;
-  if (ld_p != ld_q) return true;
-  const uintptr_t pixel = ld_p * size, d = a <= b ? (b - a) % pixel : pixel - 1 - (a - b - 1) % pixel;
-  return d < (uintptr_t)(c * size) || pixel - d < (uintptr_t)(c * size);
+// a map of the call, and what a call holds per picture and group, or per channel
+static Region map_of(const alexnet_group_norm_t* cfg, const void* p, long ld) {
+  const long size = (long)type_size(cfg->type);
+  return Region(p, (long)cfg->n * cfg->hw, ld * size, cfg->c * size);
 }
-// a result where an input is: all of it, pixel for pixel, or none
-static int check_overlap(const char* who, const alexnet_group_norm_t* cfg, const void* in, long ld_in, const void* out, long ld_out) {
-  AX_REQUIRE((in == out && ld_in == ld_out) ||
-                 !share(in, ld_in, out, ld_out, (long)cfg->n * cfg->hw, cfg->c, (long)type_size(cfg->type)),
-             ALEXNET_EINVAL, "%s: the result overlaps an input without being in its place", who);
-  return ALEXNET_OK;
-}
+static Region stats_of(const alexnet_group_norm_t* cfg, const float* p) { return Region(p, 4L * cfg->n * cfg->groups); }
+static Region channels_of(const alexnet_group_norm_t* cfg, const float* p) { return Region(p, 4L * cfg->c); }
 
 #define GN_LAUNCH(kernel, grid, block, st, a)                            \
   do {                                                                   \
@@ -804,7 +795,14 @@ int alexnet_group_norm_forward(const alexnet_group_norm_t* cfg, const void* d_x,
              ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
   if (keep) AX_TRY(check_checkpoint(keep, who));
   AX_TRY(check_scratch(who, d_workspace, workspace_bytes, need));
-  AX_TRY(check_overlap(who, cfg, d_x, ld_x, d_y, ld_y));
+  const long rows = (long)cfg->n * cfg->hw;
+  AX_TRY(check_apart(who, {{"x", map_of(cfg, d_x, ld_x), true}, {"gamma", channels_of(cfg, d_gamma), false}, {"beta", channels_of(cfg, d_beta), false}},
+                     {{"y", map_of(cfg, d_y, ld_y), true},
+                      {"mean", stats_of(cfg, d_mean), false},
+                      {"rstd", stats_of(cfg, d_rstd), false},
+                      {"the checkpoint's codes", codes_of(keep, rows, cfg->c), false},
+                      {"the checkpoint's scales", scales_of(keep, rows, cfg->c), false},
+                      {"the workspace", Region(need ? d_workspace : nullptr, (long)need), false}}));
   GnArgs a = gn_args(cfg);
   a.x = d_x;
   a.ld_x = ld_x;
@@ -842,8 +840,20 @@ int alexnet_group_norm_backward(const alexnet_group_norm_t* cfg, const void* d_x
              ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
   if (kept) AX_TRY(check_checkpoint(kept, who));
   AX_TRY(check_scratch(who, d_workspace, workspace_bytes, need));
-  AX_TRY(check_overlap(who, cfg, d_dy, ld_dy, d_dx, ld_dx));
-  if (!kept) AX_TRY(check_overlap(who, cfg, d_x, ld_x, d_dx, ld_dx));
+  const long rows = (long)cfg->n * cfg->hw;
+  AX_TRY(check_apart(who,
+                     {{"x", map_of(cfg, d_x, ld_x), true},
+                      {"the checkpoint's codes", codes_of(kept, rows, cfg->c), false},
+                      {"the checkpoint's scales", scales_of(kept, rows, cfg->c), false},
+                      {"dy", map_of(cfg, d_dy, ld_dy), true},
+                      {"mean", stats_of(cfg, d_mean), false},
+                      {"rstd", stats_of(cfg, d_rstd), false},
+                      {"gamma", channels_of(cfg, d_gamma), false},
+                      {"beta", channels_of(cfg, d_beta), false}},
+                     {{"dx", map_of(cfg, d_dx, ld_dx), true},
+                      {"dgamma", channels_of(cfg, d_dgamma), false},
+                      {"dbeta", channels_of(cfg, d_dbeta), false},
+                      {"the workspace", Region(need ? d_workspace : nullptr, (long)need), false}}));
   GnArgs a = gn_args(cfg);
   a.x = d_x;
   a.ld_x = ld_x;
