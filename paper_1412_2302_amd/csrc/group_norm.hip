@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(1024) gn_channel_totals_kernel(GnArgs a) {
 }
 static int total_blocks(const GnArgs& a) { return a.dbeta || a.dgamma ? ceil_div(a.c, kTotalChannels) : 0; }
 
-// Its first workgroups, total_blocks of them, leave dbeta and dgamma meanwhile.  128 x 3025 x 96 fp32 from int8: 65 us, 5.2 TB/s.
+// Its first workgroups, total_blocks of them (none where they have a launch of their own), leave dbeta and dgamma meanwhile.  128 x 3025 x 96 fp32 from int8: 65 us, 5.2 TB/s.
 template <typename T, int V, int SRC>
 __global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a, int total_blocks) {
   __shared__ union {
@@ -700,6 +700,11 @@ static int gn_forward(GnArgs a, int keep, hipStream_t st) {
   return ALEXNET_OK;
 }
 
+static int channel_totals_launch(const GnArgs& a, int totals, hipStream_t st) {
+  KernelScope ks("gn_grad_totals", 0, 0, st);
+  GN_LAUNCH(gn_channel_totals_kernel, totals, 1024, st, a);
+  return ALEXNET_OK;
+}
 template <typename T, int V, int SRC>
 static int gn_backward(GnArgs a, hipStream_t st) {
   split(a, V, false);
@@ -720,8 +725,12 @@ static int gn_backward(GnArgs a, hipStream_t st) {
       hipLaunchKernelGGL(gn_grad_means_kernel<256>, dim3((unsigned)(a.n * a.groups)), dim3(256), 0, st, a, width);
     AX_LAUNCH_CHECK();
   }
+  int totals = total_blocks(a);
+  if (blocks + totals >= 1 << 24) {  // together more than the 2^32 threads of a grid
+    AX_TRY(channel_totals_launch(a, totals, st));
+    totals = 0;
+  }
   KernelScope ks("gn_grad_apply", 0, in + values * sizeof(T), st);
-  const int totals = total_blocks(a);
   hipLaunchKernelGGL((gn_grad_apply_kernel<T, V, SRC>), dim3((unsigned)(blocks + totals)), dim3(256), 0, st, a, totals);
   AX_LAUNCH_CHECK();
   return ALEXNET_OK;
@@ -744,10 +753,7 @@ static int gn_backward_src(GnArgs a, int type, hipStream_t st) {
     a.chunks = a.col_blocks = 1;
     AX_TRY(launch_gn_slab_backward(a, p, type, SRC, st));
     const int totals = total_blocks(a);
-    if (a.n == 1 || !totals) return ALEXNET_OK;
-    KernelScope ks("gn_grad_totals", 0, 0, st);
-    GN_LAUNCH(gn_channel_totals_kernel, totals, 1024, st, a);
-    return ALEXNET_OK;
+    return a.n == 1 || !totals ? ALEXNET_OK : channel_totals_launch(a, totals, st);
   }
   constexpr int V = kBackwardVec;
   return a.c >= V && (a.c % V == 0 || (a.dy != a.out && a.x != a.out)) ? gn_backward<T, V, SRC>(a, st) : gn_backward<T, 1, SRC>(a, st);
