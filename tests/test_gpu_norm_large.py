@@ -42,3 +42,51 @@ def test_as_many_workgroups_as_a_grid_holds(lib):
         assert bool(((dx[i, 0].double() - want).abs() <= off).all())
     del x, dy, dx, sums, ends
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("code", [None, torch.int8, torch.float8_e4m3fn], ids=str)
+def test_gradient_sums_past_31_bits_of_elements(lib, code):
+    """Two pictures of 2^25 + 3 pixels.  dy and x rise along the pixels and from picture to picture, so that a chunk left out
+    or taken twice moves a sum by some 2^-11 of its terms.  A term passes at most 1311 additions of a thread, 25 rows,
+    64 chunks of a thread and five more: under 2048."""
+    n, hw, c, groups = 2, (1 << 25) + 3, 40, 4
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    ramp = torch.linspace(0, 1, hw, device="cuda")[None, :, None] + torch.tensor([0.0, 0.5], device="cuda")[:, None, None]
+    x = torch.randn((n, hw, c), device="cuda", generator=gen).add_(ramp, alpha=2.0)
+    dy = torch.randn((n, hw, c), device="cuda", generator=gen).add_(ramp + 1.0)
+    gamma = torch.randn(c, device="cuda", generator=gen) * 0.2 + 1
+    _, mean, rstd, kept = lib.group_norm_forward(x, gamma, None, groups, 1e-5, "none", checkpoint=code)
+    wide_m, wide_r = (t.double().repeat_interleave(c // groups, 1)[:, None] for t in (mean, rstd))
+    sums = torch.zeros((n, 4, c), device="cuda", dtype=torch.float64)  # of dy, of dy hat, and of their magnitudes
+
+    def hats(a, b):
+        part = x[:, a:b] if kept is None else lib.checkpoint_unpack(
+            lib.Checkpoint(kept.codes[:, a:b].contiguous(), kept.scales[:, a:b].contiguous()))
+        return (part.double() - wide_m) * wide_r
+
+    step = 1 << 21
+    for a in range(0, hw, step):
+        d, hat = dy[:, a:a + step].double(), hats(a, min(hw, a + step))
+        sums += torch.stack([d.sum(1), (d * hat).sum(1), d.abs().sum(1), (d * hat).abs().sum(1)], 1)
+        del d, hat
+    # the first, the last and some pixels between, before dx takes the place of dy
+    spots = [(0, 500), (hw // 2, hw // 2 + 500), (hw - 500, hw)]
+    some = [(dy[:, a:b].double(), hats(a, b)) for a, b in spots]
+    dx, dgamma, dbeta = lib.group_norm_backward(x if kept is None else kept, dy, mean, rstd, gamma, None, "none", out=dy)
+    k = 2048 * R.EPS32
+    total = sums.sum(0)
+    assert bool(((dbeta.double() - total[0]).abs() <= k * total[2]).all())
+    assert bool(((dgamma.double() - total[1]).abs() <= (k + 3 * R.EPS32) * total[3]).all())
+    g = gamma.double()
+
+    def group_mean(t):
+        return (t.view(n, groups, -1).sum(2) / (hw * (c // groups))).repeat_interleave(c // groups, 1)[:, None]
+
+    a, b = group_mean(g * sums[:, 0]), group_mean(g * sums[:, 1])
+    off_a, off_b = k * group_mean(g.abs() * sums[:, 2]), (k + 3 * R.EPS32) * group_mean(g.abs() * sums[:, 3])
+    for (lo, hi), (d, hat) in zip(spots, some):
+        want = wide_r * (g * d - a - hat * b)
+        off = wide_r * (off_a + hat.abs() * off_b + 4 * R.EPS32 * ((g * d).abs() + a.abs() + 2 * (hat * b).abs()))
+        assert bool(((dx[:, lo:hi].double() - want).abs() <= off + want.abs() * R.HALF_STEP[torch.float32] * 1.01).all())
+    del x, dy, dx, kept, some
+    torch.cuda.empty_cache()
