@@ -383,10 +383,12 @@ int alexnet_checkpoint_unpack(const alexnet_checkpoint_t* in, int64_t rows, int3
  * pixels) from the checkpoint of its input x [rows][in]:
  *   dw [out][in] = dy^T x, db [out] = sum of dy over the rows (d_db may be null)
  * with dy [rows][out] of `type` at row stride ld_dy, products of the unpacked
- * values, float32 sums and results.  No operand is rounded: x is exact in
- * bfloat16 and dy is multiplied as one (BF16), two (FP16) or three (FP32)
- * bfloat16 terms; only what lies under 2^-133, the smallest bfloat16 number, is
- * left off a float32 dy.  rows may be 0 (the gradients are then zero). */
+ * values, float32 sums and results.  Both operands are exact as bfloat16 terms,
+ * of which dy takes one (BF16), two (FP16) or three (FP32), but for what lies
+ * under 2^-133, the smallest bfloat16 number: that is left off a float32 dy, and
+ * E4M3 values in blocks of scale 0 to 2 (none of them past 448 * 2^-125) are
+ * rounded to the nearest multiple of it.  rows may be 0 (the gradients are then
+ * zero). */
 int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes);
 int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const void* d_dy, int64_t ld_dy, int32_t type,
                                           int64_t rows, int32_t in, int32_t out, float* d_dw, float* d_db,

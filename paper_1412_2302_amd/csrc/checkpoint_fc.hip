@@ -3,7 +3,8 @@
 //
 // Multiplied on the bf16 matrix instructions without rounding an operand: x is a code of at most eight significant bits times a
 // power of two, which bf16 holds, and dy goes in as its leading eight bits, the next eight and the last eight (fp32; two terms
-// hold fp16, one bf16).  Sums stay fp32.
+// hold fp16, one bf16).  Sums stay fp32.  What lies under bf16's 2^-133 is the exception: dy leaves it off, and e4m3 values of
+// the scales 0 to 2 are rounded to a multiple of it by the instruction that widens them.
 //
 // Both operands have the summed index outermost, and the matrix instruction wants eight consecutive rows of one column in a
 // lane.  A thread therefore loads a patch of eight rows by NA (NB) columns, and while it widens and splits the values in

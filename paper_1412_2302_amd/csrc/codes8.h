@@ -4,8 +4,8 @@
 // value = code * 2^(scale - 127).  The scale is the smallest power of two (2^-126 and up) that holds the block's largest
 // magnitude: 127 steps in int8, 448 in e4m3 (four exponent bits, three of fraction).  A power of two because it makes both
 // directions exact but for the one rounding to nearest even of the code, and because code * 2^e has at most eight significant
-// bits: bf16 holds it exactly, so the matrix instructions take a checkpoint without rounding it a second time.  A block with
-// an infinity or a NaN gets scale code 255 and reads back as NaN: a diverged layer stays visible.
+// bits: bf16 holds it exactly, so the matrix instructions take a checkpoint without rounding it a second time (but for e4m3
+// under the scales 0 to 2, whose fractions reach down to 2^-136 and bf16's to 2^-133).  A block with an infinity or a NaN gets scale code 255 and reads back as NaN: a diverged layer stays visible.
 #pragma once
 #include <initializer_list>
 
