@@ -18,17 +18,13 @@
 //
 // 256 x 9216 x 4096 fp32: 65 us, three terms at 890 TFLOP/s, bound by the matrix instructions with what feeds them;
 // 43264 x 384 x 384 bf16 from e4m3: 35 us and 5 for the slices, bound by the conversion, which every tile repeats.
-#include <algorithm>
 #include <utility>
 
 #include "codes8.h"
+#include "fc_plan.h"
 #include "kernels.h"
 
 namespace ax {
-
-constexpr int kStep = 32;         // rows of a stage
-constexpr int kSliceRows = 4096;  // of a workgroup at most: a longer running sum loses more to rounding than one split up
-constexpr int kMaxSlices = 1024;
 
 struct FcArgs {
   const uint8_t *codes, *scales;
@@ -45,6 +41,7 @@ template <typename T>
 constexpr int terms() {
   return sizeof(T) == 4 ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;
 }
+static int terms_of(int type) { return type == ALEXNET_TYPE_FP32 ? 3 : type == ALEXNET_TYPE_FP16 ? 2 : 1; }
 // the upper halves of two numbers as one word: bf16 by leaving off what follows
 __device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
   return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
@@ -443,52 +440,6 @@ static int fc_zero(float* dw, size_t n, float* db, int out, hipStream_t st) {
   return db ? launch_fill(db, out, 0.f, st) : ALEXNET_OK;
 }
 
-struct FcPlan {
-  int na, nb;  // the tile is 64 na x 64 nb
-  int gm, gn, slices, steps;
-  size_t slab, ws;  // floats of a slice's dw; bytes of scratch
-};
-// The tile and the number of slices that a model of the measured times makes cheapest.  A step of a workgroup that has a
-// compute unit to itself takes kAloneUs microseconds, one among as many as fit kStepUs of the unit's time; slices are written
-// and read once more each.  256 x 9216 x 4096 fp32 (few rows, large dw): 128 x 256 tiles 60 us, 64 x 128 ones 84, two slices 180;
-// 43264 x 384 x 384 bf16: 128 x 256 tiles in 86 slices 36 us, in 43 slices 54, 64 x 128 ones in 56 slices 38, in 12 slices 78,
-// 64 x 64 ones in 64 slices 53; 100000 x 96 x 64 fp32: 64 x 128 tiles in 512 slices 20, 64 x 64 ones in 64 slices 41.
-static FcPlan fc_plan(long rows, int in, int out, int type) {
-  static const double kStepUs[3][3] = {{0.19, 0.25, 0.32}, {0.21, 0.32, 0.44}, {0.46, 0.78, 1.1}};  // [tile][terms - 1]
-  static const double kAloneUs[3][3] = {{0.3, 0.4, 0.48}, {0.5, 0.56, 0.62}, {0.8, 1.1, 1.33}};
-  static const int kFit[3] = {4, 4, 2};  // workgroups on a compute unit
-  FcPlan best = {};
-  double least = 1e300;
-  const int terms = type == ALEXNET_TYPE_FP32 ? 3 : type == ALEXNET_TYPE_FP16 ? 2 : 1;
-  const long steps = (rows + kStep - 1) / kStep;
-  const double bytes = 4.0 * in * out;
-  for (int shape = 0; shape < 3; ++shape) {
-    FcPlan p = {};
-    p.na = shape == 2 ? 2 : 1;
-    p.nb = 1 << shape;
-    if (out < p.na || in < p.nb) continue;
-    p.gm = ceil_div(out, 64 * p.na);
-    p.gn = ceil_div(in, 64 * p.nb);
-    const double tiles = (double)p.gm * p.gn, us = kStepUs[shape][terms - 1], alone = kAloneUs[shape][terms - 1];
-    const int fit = kFit[shape];
-    for (long s = std::max<long>(1, (rows + kSliceRows - 1) / kSliceRows); s <= std::min<long>(steps, kMaxSlices); s += 1 + s / 8) {
-      p.steps = (int)((steps + s - 1) / s);
-      p.slices = (int)((steps + p.steps - 1) / p.steps);
-      if (tiles * p.slices >= 1 << 24) continue;  // past the threads of a grid
-      const double units = tiles * p.slices / 256, full = std::floor(units / fit), rest = std::ceil(units - full * fit);
-      const double each = full * std::max(alone, us * fit) + (rest > 0 ? std::max(alone, us * rest) : 0.0);
-      const double cost = p.steps * each + p.slices * bytes / 8.8e6 + (p.slices > 1 ? 4.3 + p.slices * bytes / 6.4e6 : 0.0);
-      if (cost < least) {
-        least = cost;
-        best = p;
-      }
-    }
-  }
-  best.slab = ((size_t)in * out + 63) & ~(size_t)63;
-  best.ws = best.slices > 1 ? align256(best.slices * (best.slab + out) * sizeof(float)) : 0;
-  return best;
-}
-
 template <typename T, int CODE>
 static int fc_launch(const FcArgs& a, const FcPlan& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.gm * p.gn * p.slices)), block(256);
@@ -523,7 +474,7 @@ extern "C" {
 int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes) {
   AX_TRY(fc_check("alexnet_checkpoint_fc_query", rows, in, out, type));
   AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_checkpoint_fc_query: null argument");
-  const FcPlan p = fc_plan(rows, in, out, type);
+  const FcPlan p = fc_plan(rows, in, out, terms_of(type));
   AX_REQUIRE(rows == 0 || p.slices, ALEXNET_ESHAPE, "alexnet_checkpoint_fc_query: %ld rows of %d by %d are more than one launch covers",
              (long)rows, in, out);
   *workspace_bytes = p.ws;
@@ -542,7 +493,7 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
   AX_REQUIRE(d_dy, ALEXNET_EINVAL, "%s: null argument", who);
   AX_TRY(check_checkpoint(x, who));
   AX_REQUIRE(ld_dy >= out, ALEXNET_ESHAPE, "%s: row stride %ld is under %d columns", who, (long)ld_dy, out);
-  const FcPlan p = fc_plan(rows, in, out, type);
+  const FcPlan p = fc_plan(rows, in, out, terms_of(type));
   AX_REQUIRE(p.slices, ALEXNET_ESHAPE, "%s: %ld rows of %d by %d are more than one launch covers", who, (long)rows, in, out);
   if (p.ws) {
     AX_REQUIRE(workspace_bytes >= p.ws && d_workspace, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who,
