@@ -615,12 +615,8 @@ static GnArgs gn_args(const alexnet_group_norm_t* cfg) {
   return a;
 }
 static bool empty(const alexnet_group_norm_t* cfg) { return cfg->n == 0 || cfg->hw == 0; }
-static SlabPlan forward_plan(const GnArgs& a, size_t size, bool keep) {
-  return slab_plan(a.n, a.hw, a.c, a.groups, 16 / (int)size, kForwardRegs, kForwardRegs, keep, 1, 12, 128 / (int)size, 32 / (int)size);
-}
-static SlabPlan backward_plan(const GnArgs& a, size_t size) {
-  return slab_plan(a.n, a.hw, a.c, a.groups, kBackwardVec, kBackwardRegs, kBackwardRegs1024, false, 2, 16, 32, 32 / (int)size);
-}
+static SlabPlan forward_plan(const GnArgs& a, size_t size, bool keep) { return forward_plan(a.n, a.hw, a.c, a.groups, (int)size, keep); }
+static SlabPlan backward_plan(const GnArgs& a, size_t size) { return backward_plan(a.n, a.hw, a.c, a.groups, (int)size); }
 // Scratch: sums per chunk and channel, then the groups' statistics; for chunks the larger of the two ways to cut rows into
 // threads (one value a thread: tiny or in-place odd rows).
 static size_t stat_bytes(const GnArgs& a) { return align256((size_t)a.n * a.groups * 2 * sizeof(float)); }

@@ -68,4 +68,14 @@ inline SlabPlan slab_plan(int n, int hw, int c, int groups, int V, int max_regs,
   return best.groups && ((long)best.groups * cpg >= 16 || !large.groups) ? best : large;
 }
 
+// The plans of the two passes over elements of `size` bytes.  Pixels of a thread at most: 1024 threads have 128 registers each.
+// Backward a thread keeps four channels of any type: with eight 16-bit ones what it knows per channel would take half its registers.
+constexpr int kForwardRegs = 16, kBackwardRegs = 8, kBackwardRegs1024 = 6, kBackwardVec = 4;
+inline SlabPlan forward_plan(int n, int hw, int c, int groups, int size, bool keep) {
+  return slab_plan(n, hw, c, groups, 16 / size, kForwardRegs, kForwardRegs, keep, 1, 12, 128 / size, 32 / size);
+}
+inline SlabPlan backward_plan(int n, int hw, int c, int groups, int size) {
+  return slab_plan(n, hw, c, groups, kBackwardVec, kBackwardRegs, kBackwardRegs1024, false, 2, 16, 32, 32 / size);
+}
+
 }  // namespace ax
