@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(256) gn_moments_kernel(GnArgs a) {
         }
         const float d = bm - m[i];
         m[i] = __builtin_fmaf(d, w, m[i]);
-        q[i] += __builtin_fmaf(d * d, wq, bq);
+        q[i] += __builtin_fmaf(d * wq, d, bq);  // in this order: wq is 0 at first, and d the mean itself, whose square may be infinite
       }
       cnt += nu;
     }

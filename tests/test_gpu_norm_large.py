@@ -90,3 +90,54 @@ def test_gradient_sums_past_31_bits_of_elements(lib, code):
         assert bool(((dx[:, lo:hi].double() - want).abs() <= off + want.abs() * R.HALF_STEP[torch.float32] * 1.01).all())
     del x, dy, dx, kept, some
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("size", [(2, 300, 64, 4), (2, 5000, 64, 4), (1, 9000, 300, 2)], ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_the_largest_and_smallest_values_that_sums_hold(lib, size, dtype):
+    """Squares that add up to 2^125 to 2^126 in a group, values that add up to 2^126, and values next to nothing beside eps."""
+    n, hw, c, groups = size
+    count = hw * c // groups
+    gen = torch.Generator(device="cuda").manual_seed(hw)
+    sign = torch.randint(0, 2, (n, hw, c), device="cuda", generator=gen).double() * 2 - 1
+    spread = 2.0 ** 62.5 / count ** 0.5 * sign * (1 + 0.1 * torch.rand((n, hw, c), device="cuda", generator=gen))
+    level = 2.0 ** 126 / count * torch.ones_like(spread)
+    tiny = 2.0 ** -100 * sign
+    for v, eps in ((spread, 1e-5), (level, 1e-5), (tiny, 1e-5), (tiny, 1e-37)):
+        x = v.to(dtype)
+        y, mean, rstd, kept = lib.group_norm_forward(x, None, None, groups, eps, "none", checkpoint=torch.int8)
+        xd = x.double().view(n, hw, groups, c // groups)
+        m = xd.mean((1, 3))
+        r = (((xd - m[:, None, :, None]) ** 2).mean((1, 3)) + eps) ** -0.5
+        tol_m = R.DEPTH * R.EPS32 * xd.abs().mean((1, 3)) + 1e-38
+        if v is level:  # all values alike: the deviations are the mean's own rounding
+            assert bool(((mean.double() - m).abs() <= tol_m).all()) and bool(torch.isfinite(y).all())
+            continue
+        tol_r = R.DEPTH * R.EPS32 + (tol_m * r) ** 2
+        assert bool(((mean.double() - m).abs() <= tol_m).all()) and bool(((rstd.double() - r).abs() <= tol_r * r).all())
+        want = (xd - m[:, None, :, None]) * r[:, None, :, None]
+        off = tol_m[:, None, :, None] * r[:, None, :, None] + want.abs() * (tol_r[:, None, :, None] + 3 * R.EPS32)
+        off = off + want.abs() * R.HALF_STEP[dtype] * 1.01 + R.TINY[dtype]
+        assert bool(((y.double().view(xd.shape) - want).abs() <= off).all())
+        back = lib.checkpoint_unpack(kept, torch.float32)
+        most = torch.nn.functional.pad(x.float().abs(), (0, -c % 32)).view(n, hw, -1, 32).amax(3).repeat_interleave(32, 2)[..., :c]
+        assert bool(((back - x.float()).abs() <= most / 127).all())
+
+
+@pytest.mark.parametrize("size", [(2, 300, 64, 4), (2, 5000, 64, 4), (1, 9000, 300, 2), (3, 9000, 256, 256)], ids=str)
+def test_a_mean_whose_square_no_float_holds(lib, size):
+    """Only squares of deviations count: values of 2^64.5 with deviations of 2^54, whose squares add up to 2^126 at most."""
+    n, hw, c, groups = size
+    gen = torch.Generator(device="cuda").manual_seed(hw)
+    x = (2.0 ** 64.5 + 2.0 ** 54 / (hw * c // groups / 2.0 ** 17 + 1) ** 0.5
+         * torch.randn((n, hw, c), device="cuda", generator=gen, dtype=torch.float64)).float()
+    xd = x.double().view(n, hw, groups, c // groups)
+    m = xd.mean((1, 3))
+    r = (((xd - m[:, None, :, None]) ** 2).mean((1, 3)) + 1e-5) ** -0.5
+    y, mean, rstd, _ = lib.group_norm_forward(x, None, None, groups)
+    tol_m = R.DEPTH * R.EPS32 * xd.abs().mean((1, 3))
+    tol_r = R.DEPTH * R.EPS32 + (tol_m * r) ** 2
+    assert bool(((mean.double() - m).abs() <= tol_m).all()) and bool(((rstd.double() - r).abs() <= tol_r * r).all())
+    want = (xd - m[:, None, :, None]) * r[:, None, :, None]
+    off = tol_m[:, None, :, None] * r[:, None, :, None] + want.abs() * (tol_r[:, None, :, None] + 4 * R.EPS32) + R.EPS32
+    assert bool(((y.double().view(xd.shape) - want).abs() <= off).all())
