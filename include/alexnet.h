@@ -364,7 +364,8 @@ int alexnet_softmax_xent_static(const float* d_logits, const int32_t* d_labels, 
  * block's largest magnitude is at most 127 (448) and rounds each value to the
  * nearest code (ties to even): off by at most half a step, which is
  * 2^(s - 128) for INT8.  A block with an infinity or a NaN is packed as s = 255
- * and reads back as NaN throughout.  One call takes 2^35 values and 2^29 rows. */
+ * and reads back as NaN throughout.  One call takes up to 2^35 values, 2^28 rows and
+ * 2^20 columns; what a launch cannot cover is refused. */
 #define ALEXNET_CODE_INT8 0
 #define ALEXNET_CODE_E4M3 1
 typedef struct {
@@ -388,7 +389,10 @@ int alexnet_checkpoint_unpack(const alexnet_checkpoint_t* in, int64_t rows, int3
  * under 2^-133, the smallest bfloat16 number: that is left off a float32 dy, and
  * E4M3 values in blocks of scale 0 to 2 (none of them past 448 * 2^-125) are
  * rounded to the nearest multiple of it.  rows may be 0 (the gradients are then
- * zero). */
+ * zero); at most 2^22 rows, 2^20 columns of either operand and 2^33 weights, and
+ * what one launch cannot cover is refused.
+ * This is the weight gradient alone: alexnet_fc_backward, which gives the data
+ * gradient, takes its input in full and computes dw from that as well. */
 int alexnet_checkpoint_fc_query(int64_t rows, int32_t in, int32_t out, int32_t type, size_t* workspace_bytes);
 int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const void* d_dy, int64_t ld_dy, int32_t type,
                                           int64_t rows, int32_t in, int32_t out, float* d_dw, float* d_db,
@@ -401,7 +405,10 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
  * ld_* are pixel strides in elements (>= c): a call can work on a slice of the
  * channels of a wider tensor; pictures follow each other (hw * ld_*).  y may be
  * x, and dx may be dy or x (same pointer and stride).
- * Squares are float32: where deviations from the mean pass 10^19, v is infinite.
+ * Sums are float32: m is infinite where a group's values add up past 3.4 * 10^38,
+ * v where the squares of their deviations do.  A group with an infinity or a NaN
+ * has NaN for y, and statistics that are not finite.  At most 2^20 channels, 2^28
+ * pixels of a map and 2^21 groups in all pictures.
  * n and hw may be 0: nothing is read then, the statistics are m = 0 and
  * r = 1/sqrt(eps), the parameter gradients 0. */
 typedef struct {
