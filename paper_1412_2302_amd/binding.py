@@ -596,7 +596,9 @@ def nhwc_to_nchw(x: torch.Tensor) -> torch.Tensor:
 
 # ---- group normalisation and 8-bit activation checkpoints ----
 # Channel-last tensors [n]...[c] of float32, bfloat16 or float16.  A channel slice of a wider tensor is taken as it is (pixels
-# at one stride).  Outputs and scratch are allocated on the stream that the call runs on, so calls share nothing.
+# at one stride).  Outputs and scratch are allocated on the stream that the call runs on, so calls share nothing.  A call on another
+# `stream` than the current one waits for nothing: whoever passes one orders it behind the work that makes the inputs.  As everywhere
+# in this module nothing is recorded for autograd: a gradient is its own call.
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
@@ -635,9 +637,12 @@ class Checkpoint:
     def _arg(self) -> CheckpointArg:
         return CheckpointArg(self.codes.data_ptr(), self.scales.data_ptr(), _CODES[self.codes.dtype])
 
-    def _need(self, what: str):
-        if not self.codes.is_cuda:
-            raise ValueError(f"{what}: expected a device tensor, got a checkpoint on {self.codes.device}")
+    @staticmethod
+    def _need(kept, what: str):
+        if not isinstance(kept, Checkpoint):
+            raise TypeError(f"{what}: expected a Checkpoint, got {type(kept).__name__}")
+        if not kept.codes.is_cuda:
+            raise ValueError(f"{what}: expected a device tensor, got a checkpoint on {kept.codes.device}")
 
 
 def _rows_stride(t, what: str) -> int:
@@ -771,13 +776,15 @@ def group_norm_backward(x, dy: torch.Tensor, mean: torch.Tensor, rstd: torch.Ten
     kept = p_x = None
     ld_x = 0
     if isinstance(x, Checkpoint):
+        Checkpoint._need(x, what)
         kept, source = x._arg(), x.codes
-        x._need(what)
     else:
         ld_x, p_x, source = _rows_stride(x, "group_norm_backward: x"), x.data_ptr(), x
     if source.shape != shape or source.device != device or (kept is None and x.dtype != dy.dtype):
         raise ValueError(f"{what}: x {list(source.shape)} and dy {list(shape)} differ in shape, type or device")
     n, c = shape[0], shape[-1]
+    if not isinstance(mean, torch.Tensor) or not isinstance(rstd, torch.Tensor):
+        raise TypeError(f"{what}: mean and rstd: expected torch.Tensors, got {type(mean).__name__} and {type(rstd).__name__}")
     if mean.dim() != 2 or mean.shape[0] != n or mean.shape[1] < 1:
         raise ValueError(f"{what}: mean: expected [{n}][groups], got {list(mean.shape)}")
     groups = mean.shape[1]
@@ -808,10 +815,10 @@ def checkpoint_pack(x: torch.Tensor, dtype: torch.dtype = torch.int8, stream=Non
 def checkpoint_unpack(kept: Checkpoint, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
     """The values of a checkpoint as float32, bfloat16 or float16."""
+    Checkpoint._need(kept, "checkpoint_unpack")
     codes = kept.codes
     if dtype not in _TYPES:
         raise ValueError(f"checkpoint_unpack: expected float32, bfloat16 or float16, got {dtype}")
-    kept._need("checkpoint_unpack")
     if not _here(codes, stream):
         return _there(codes, stream, (kept, out), lambda: checkpoint_unpack(kept, dtype, out))
     x, ld = _result(out, codes.shape, dtype, codes.device, "checkpoint_unpack: out")
@@ -832,9 +839,9 @@ def checkpoint_fc_backward_weight(kept: Checkpoint, dy: torch.Tensor, dw: Option
     """(dw [out][in], db [out]) in float32 of a dense layer, or of a 1 x 1 convolution over pixels, whose input [rows]...[in]
     was kept as a Checkpoint, from dy [rows]...[out].  dw, db: where they go."""
     what = "checkpoint_fc_backward_weight"
+    Checkpoint._need(kept, what)
     codes = kept.codes
     ld = _rows_stride(dy, "checkpoint_fc_backward_weight: dy")
-    kept._need(what)
     if not _here(dy, stream):
         return _there(dy, stream, (kept, dy, dw, db), lambda: checkpoint_fc_backward_weight(kept, dy, dw, db))
     device = dy.device
