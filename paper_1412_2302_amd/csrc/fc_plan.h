@@ -20,8 +20,8 @@ struct FcPlan {
 // The tile and the number of slices that a model of the measured times makes cheapest.  A step of a workgroup that has a
 // compute unit to itself takes kAloneUs microseconds, one among as many as fit kStepUs of the unit's time; slices are written
 // and read once more each.  256 x 9216 x 4096 fp32 (few rows, large dw): 128 x 256 tiles 60 us, 64 x 128 ones 84, two slices 180;
-// 43264 x 384 x 384 bf16: 128 x 256 tiles in 86 slices 36 us, in 43 slices 54, 64 x 128 ones in 56 slices 38, in 12 slices 78,
-// 64 x 64 ones in 64 slices 53; 100000 x 96 x 64 fp32: 64 x 128 tiles in 512 slices 20, 64 x 64 ones in 64 slices 41.
+// 43264 x 384 x 384 bf16: 128 x 256 tiles in 86 slices 36 us, in 43 slices 54, 64 x 128 ones in 56 slices 38, in 39 slices, which
+// the model takes by a tenth of a microsecond, 40, in 12 slices 78, 64 x 64 ones in 64 slices 53; 100000 x 96 x 64 fp32: 64 x 128 tiles in 512 slices 20, 64 x 64 ones in 64 slices 41.
 inline FcPlan fc_plan(long rows, int in, int out, int terms) {
   static const double kStepUs[3][3] = {{0.19, 0.25, 0.32}, {0.21, 0.32, 0.44}, {0.46, 0.78, 1.1}};  // [tile][terms - 1]
   static const double kAloneUs[3][3] = {{0.3, 0.4, 0.48}, {0.5, 0.56, 0.62}, {0.8, 1.1, 1.33}};

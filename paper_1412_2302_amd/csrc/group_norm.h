@@ -85,7 +85,9 @@ __device__ __forceinline__ void with_act(int act, F f) {
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
   if (ACT == ALEXNET_ACT_RELU) return z < 0.f ? 0.f : z;  // a NaN stays one
-  if (ACT == ALEXNET_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));  // one ulp each
+  // The reciprocal is off by an ulp; the exponential rounds its argument, which puts its result off by |z| roundings, as much
+  // as the rounding of z itself does.
+  if (ACT == ALEXNET_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
   return z;
 }
 

@@ -33,8 +33,10 @@ __device__ __forceinline__ Slab slab(const GnArgs& a, int V) {
 }
 
 // Sums of every channel of the slab over the pixels of the workgroup, N values per channel and thread in, lds[k * stride +
-// channel] out; stride: threads * V.  Channels lie side by side, so neither the stores nor the sums' reads meet in a bank;
-// first every thread adds up the rows r = part, part + parts, ... of one channel, then one thread its channel's parts.
+// channel] out; stride: threads * V.  First every thread adds up the rows r = part, part + parts, ... of one channel, then one
+// thread its channel's parts.  Channels lie side by side, so the sums' reads meet in no bank; the stores do, V lanes of a wave in
+// each (one value at a time, V words apart, as a thread may leave out its first ones): 1.85e6 cycles over the 4.4e5 LDS
+// instructions of the forward pass over 256 x 729 x 256 bf16, 1.57e6 over 1.1e6 backward fp32.
 template <int V, int N>
 __device__ __forceinline__ void channel_sums(const GnArgs& a, const Slab& s, Vec v, const float (*x)[V], float* lds) {
   const int w = s.width, t = threadIdx.x, threads = blockDim.x, stride = threads * V;
