@@ -405,10 +405,10 @@ int alexnet_checkpoint_fc_backward_weight(const alexnet_checkpoint_t* x, const v
  * ld_* are pixel strides in elements (>= c): a call can work on a slice of the
  * channels of a wider tensor; pictures follow each other (hw * ld_*).  y may be
  * x, and dx may be dy or x (same pointer and stride).
- * Sums are float32: m is infinite where a group's values add up past 3.4 * 10^38,
- * v where the squares of their deviations do.  A group with an infinity or a NaN
- * has NaN for y, and statistics that are not finite.  At most 2^20 channels, 2^28
- * pixels of a map and 2^21 groups in all pictures.
+ * Sums are float32: m is not finite where a group's values add up past
+ * 3.4 * 10^38, nor v where the squares of their deviations do.  A group with an
+ * infinity or a NaN has NaN for y, and no finite m.  At most 2^20 channels, 2^28
+ * pixels of a map, and in all pictures together 2^21 groups and 2^32 channels.
  * n and hw may be 0: nothing is read then, the statistics are m = 0 and
  * r = 1/sqrt(eps), the parameter gradients 0. */
 typedef struct {

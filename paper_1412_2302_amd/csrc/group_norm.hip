@@ -499,7 +499,8 @@ __global__ void __launch_bounds__(1024) gn_channel_totals_kernel(GnArgs a) {
 }
 static int total_blocks(const GnArgs& a) { return a.dbeta || a.dgamma ? ceil_div(a.c, kTotalChannels) : 0; }
 
-// Its first workgroups, total_blocks of them (none where they have a launch of their own), leave dbeta and dgamma meanwhile.  128 x 3025 x 96 fp32 from int8: 65 us, 5.2 TB/s.
+// Its first workgroups, total_blocks of them (none where they have a launch of their own), leave dbeta and dgamma meanwhile.
+// 128 x 3025 x 96 fp32 from int8: 65 us, 5.2 TB/s.
 template <typename T, int V, int SRC>
 __global__ void __launch_bounds__(256) gn_grad_apply_kernel(GnArgs a, int total_blocks) {
   __shared__ union {
