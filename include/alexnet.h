@@ -446,6 +446,97 @@ int alexnet_group_norm_backward(const alexnet_group_norm_t* cfg, const void* d_x
                                 void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, void* d_workspace,
                                 size_t workspace_bytes, void* stream);
 
+/* --- dense layers in 8-bit floating point, root-mean-square normalisation, gradient clipping ---
+ * What a residual net of dense layers (of 1x1 convolutions: rows are pixels)
+ * trains and answers with, next to the operators above and under their rules:
+ * no handle, no state, calls may overlap in time and may be captured; TYPE is that of
+ * activations and gradients; pointers are aligned to their element unless
+ * stated; what a call writes overlaps nothing that it reads or else writes,
+ * or it is refused, but for a result in the very place of an input where the call says so.
+ *
+ * An operand [rows][cols] of a product, in 8 bits.  With nb = ceil(cols / 128):
+ *   d_codes [rows][128 nb]: an 8-bit float a value (E4M3 as above; E5M2: five
+ *     exponent and two fraction bits), zeros behind the columns; 16-byte aligned;
+ *   d_scales: a byte s for every 128 consecutive columns of a row (square = 0),
+ *     as [nb][rows up to a multiple of 4], zeros behind the rows, 4-byte aligned;
+ *     or for every 128 rows of 128 columns (square = 1), as [nb][ceil(rows / 128)].
+ *   value = code * 2^(s - 127)
+ * Packing takes the smallest scale from 2^-126 up under which the block's
+ * largest magnitude is at most 448 (57344 for E5M2) and rounds each value to the
+ * nearest code (ties to even).  A block with an infinity or a NaN is packed as
+ * s = 255 and stands for NaN throughout.  At most 2^28 rows, 2^28 columns and 2^36 codes. */
+#define ALEXNET_CODE_E5M2 2
+#define ALEXNET_BLOCK8 128
+typedef struct {
+  void* d_codes;
+  void* d_scales;
+  int32_t code;   /* ALEXNET_CODE_E4M3 or ALEXNET_CODE_E5M2 */
+  int32_t square; /* a scale for 128 rows by 128 columns, not for each row's */
+} alexnet_blocks8_t;
+
+/* x [rows][cols] as an operand (rows), its transpose as one (columns), or both
+ * from one reading of x; either may be null.  A product sums over the columns of both its operands,
+ * so a layer's forward pass takes x and w as they are, the gradient of x the transpose
+ * of w, and that of w the transposes of dy and x.  Both are of the same code and kind; square blocks are
+ * the same values either way. */
+int alexnet_block8_pack(const void* d_x, int64_t ld_x, int32_t type, int64_t rows, int64_t cols,
+                        const alexnet_blocks8_t* out_rows, const alexnet_blocks8_t* out_columns, void* stream);
+/* Values are rounded once to `type` (past its range: infinity). */
+int alexnet_block8_unpack(const alexnet_blocks8_t* in, int64_t rows, int64_t cols, void* d_x, int64_t ld_x,
+                          int32_t type, void* stream);
+/* y [m][n] = a b^T of a [m][k] and b [n][k], rounded once to `type`.  In FP32
+ * products are exact and sums float32 (values past float32's range, which packing
+ * makes of some just under it, count as infinities).  For BF16 and FP16 eight products at
+ * a time are added with 13 bits under the largest of them, those sums in float32:
+ * off by at most 7 * 2^-13 of what each eight's largest add up to, 1.5e-5 of a result of
+ * normal numbers.  Results repeat bit for bit.  k = 0 gives
+ * zeros.  Codes and scales may be any bytes.  At most 2^28 rows of either, 2^22
+ * columns and 2^32 results, and what one launch cannot cover is refused. */
+int alexnet_block8_product_query(int64_t m, int64_t n, int64_t k, int32_t type, size_t* workspace_bytes);
+int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* b, int64_t m, int64_t n, int64_t k,
+                           void* d_y, int64_t ld_y, int32_t type, void* d_workspace, size_t workspace_bytes,
+                           void* stream);
+
+/* Root-mean-square normalisation of every row, with a residual in front of it:
+ *   s = x + residual, rounded to TYPE; r = 1/sqrt(mean(s^2) + eps); y = s r gamma
+ * d_residual and d_sum (where s goes) are both given, or both null: s is x then.
+ * y goes to d_y, rounded once to TYPE, or to `blocks` (not square) as an operand of a
+ * product; the other of the two is null.  d_gamma [cols] may be null (1), as may d_rstd [rows], which
+ * receives r.  ld_* are row strides in elements (>= cols).  y and sum may each take the place of x or
+ * residual (same pointer and stride).  Sums are float32: r is 0, and y with it, where the squares of a row add up past
+ * 3.4 * 10^38.  A row with an infinity or a NaN has NaN somewhere in y, and as blocks no finite value in
+ * the blocks that it has them in.  At most 2^24 rows and 2^20 columns; rows may be 0. */
+int alexnet_rms_norm_forward(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, int32_t type,
+                             int64_t rows, int64_t cols, float eps, const float* d_gamma, void* d_sum, int64_t ld_sum,
+                             void* d_y, int64_t ld_y, const alexnet_blocks8_t* blocks, float* d_rstd, void* stream);
+/* Gradients from s (the forward call's sum, or x where there was no residual), r
+ * and gamma, from dy and dsum, the gradient that s has from elsewhere (may be null):
+ *   dx = dsum + r (dy gamma - s r mean(dy gamma s r)),  dgamma = sum over rows of dy s r
+ * dx is the gradient of x and of the residual alike, and may take the place of sum, dy
+ * or dsum.  Of y in blocks dy is the gradient of the values that they stand for.  d_dgamma may be null.  rows may
+ * be 0: dgamma is then 0. */
+int alexnet_rms_norm_query(int64_t rows, int64_t cols, int32_t type, size_t* backward_bytes);
+int alexnet_rms_norm_backward(const void* d_sum, int64_t ld_sum, const void* d_dy, int64_t ld_dy, const void* d_dsum,
+                              int64_t ld_dsum, int32_t type, int64_t rows, int64_t cols, const float* d_rstd,
+                              const float* d_gamma, void* d_dx, int64_t ld_dx, float* d_dgamma, void* d_workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* The norm of `count` gradients together, and clipping to it:
+ *   norm = sqrt(sum over all tensors and values of g^2),
+ *   out = g * min(1, max_norm / norm), rounded once to the tensor's type
+ * The tables are HOST arrays, read before the call returns; tensor i has sizes[i]
+ * contiguous values of types[i] at grads[i] (anything where sizes[i] = 0).  outs null: in place.
+ * Sums are float64, in a fixed order, so that no finite float32 gradient is too large or small for them.  d_norm
+ * (float32, may be null in clip_gradients) receives the norm.  Where the norm is
+ * an infinity or a NaN, or not over max_norm, gradients stay as they are.
+ * At most 2^20 tensors and 2^40 values. */
+int alexnet_clip_query(int32_t count, const int64_t* sizes, size_t* workspace_bytes);
+int alexnet_gradient_norm(int32_t count, const void* const* grads, const int64_t* sizes, const int32_t* types,
+                          float* d_norm, void* d_workspace, size_t workspace_bytes, void* stream);
+int alexnet_clip_gradients(int32_t count, const void* const* grads, void* const* outs, const int64_t* sizes,
+                           const int32_t* types, float max_norm, float* d_norm, void* d_workspace,
+                           size_t workspace_bytes, void* stream);
+
 /* --- per-kernel timing (measurement aid; not part of the training path) ---
  * Between alexnet_profile_begin and alexnet_profile_end every kernel the
  * calling thread launches through this library is bracketed by two HIP events

@@ -120,6 +120,26 @@ _SIGS.update({
     "alexnet_checkpoint_fc_query": [_i64, _i32, _i32, _i32, C.POINTER(_sz)],
     "alexnet_checkpoint_fc_backward_weight": [_kp, _vp, _i64, _i32, _i64, _i32, _i32, _vp, _vp, _vp, _sz, _vp],
 })
+
+
+class Blocks8Arg(C.Structure):
+    _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("code", C.c_int32), ("square", C.c_int32)]
+
+
+_bp, _f32 = C.POINTER(Blocks8Arg), C.c_float
+_SIGS.update({
+    "alexnet_block8_pack": [_vp, _i64, _i32, _i64, _i64, _bp, _bp, _vp],
+    "alexnet_block8_unpack": [_bp, _i64, _i64, _vp, _i64, _i32, _vp],
+    "alexnet_block8_product_query": [_i64, _i64, _i64, _i32, C.POINTER(_sz)],
+    "alexnet_block8_product": [_bp, _bp, _i64, _i64, _i64, _vp, _i64, _i32, _vp, _sz, _vp],
+    "alexnet_rms_norm_query": [_i64, _i64, _i32, C.POINTER(_sz)],
+    "alexnet_rms_norm_forward": [_vp, _i64, _vp, _i64, _i32, _i64, _i64, _f32, _vp, _vp, _i64, _vp, _i64, _bp, _vp, _vp],
+    "alexnet_rms_norm_backward": [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _sz,
+                                  _vp],
+    "alexnet_clip_query": [_i32, _vp, C.POINTER(_sz)],
+    "alexnet_gradient_norm": [_i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "alexnet_clip_gradients": [_i32, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _sz, _vp],
+})
 _SIGS["alexnet_profile_begin"] = []
 _SIGS["alexnet_profile_end"] = [C.POINTER(ProfEntry), _i32, C.POINTER(_i32)]
 for _name, _args in _SIGS.items():
@@ -699,7 +719,7 @@ def _there(t: torch.Tensor, stream, inputs, call):
         outputs = result if isinstance(result, tuple) else (result,)
         for group, user in ((inputs, stream), (outputs, caller)):
             for x in group:
-                for part in (x.codes, x.scales) if isinstance(x, Checkpoint) else (x,):
+                for part in (x.codes, x.scales) if isinstance(x, (Checkpoint, Blocks8)) else (x,):
                     if part is not None:
                         part.record_stream(user)
     return result
@@ -859,3 +879,258 @@ def checkpoint_fc_backward_weight(kept: Checkpoint, dy: torch.Tensor, dw: Option
                                                       db.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes,
                                                       _raw_stream(device.index)))
     return dw, db
+
+
+# ---- dense layers in 8-bit floating point, root-mean-square normalisation, gradient clipping ----
+# As above: no handle, outputs and scratch on the call's stream, nothing recorded for autograd.
+_CODES8 = {torch.float8_e4m3fn: 1, torch.float8_e5m2: 2}
+BLOCK8 = 128  # columns (of square blocks also rows) that share a scale
+
+
+class Blocks8:
+    """A matrix [rows][cols] in 8 bits, as an operand of block8_product: codes (float8_e4m3fn or float8_e5m2) [rows][cols up to a
+    multiple of 128], scales (uint8) [ceil(cols / 128)][rows up to a multiple of 4], or, of square blocks of 128 x 128, [ceil(cols
+    / 128)][ceil(rows / 128)]; value = code * 2^(scale - 127).  The codes behind the columns are zeros."""
+
+    __slots__ = ("codes", "scales", "cols", "square")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, square: bool = False):
+        if codes.dtype not in _CODES8 or scales.dtype != torch.uint8:
+            raise ValueError(f"Blocks8: codes are float8_e4m3fn or float8_e5m2 and scales uint8, got {codes.dtype} and {scales.dtype}")
+        if codes.dim() != 2 or tuple(codes.shape) + tuple(scales.shape) != Blocks8._sizes(codes.shape[0], cols, square):
+            raise ValueError(f"Blocks8: codes {list(codes.shape)} and scales {list(scales.shape)} are not those of {cols} columns"
+                             f"{' in square blocks' if square else ''}")
+        if not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device:
+            raise ValueError("Blocks8: codes and scales must be contiguous, on one device")
+        self.codes, self.scales, self.cols, self.square = codes, scales, cols, bool(square)
+
+    @staticmethod
+    def _sizes(rows: int, cols: int, square: bool):
+        blocks = -(-cols // BLOCK8)
+        return rows, blocks * BLOCK8, blocks, -(-rows // BLOCK8) if square else -(-rows // 4) * 4
+
+    @staticmethod
+    def _empty(rows: int, cols: int, dtype: torch.dtype, square: bool, device) -> "Blocks8":
+        rows, pitch, blocks, scales = Blocks8._sizes(rows, cols, square)
+        made = Blocks8.__new__(Blocks8)
+        made.codes = torch.empty((rows, pitch), dtype=dtype, device=device)
+        made.scales = torch.empty((blocks, scales), dtype=torch.uint8, device=device)
+        made.cols, made.square = cols, square
+        return made
+
+    @property
+    def shape(self):
+        return torch.Size((self.codes.shape[0], self.cols))
+
+    def _arg(self) -> Blocks8Arg:
+        return Blocks8Arg(self.codes.data_ptr(), self.scales.data_ptr(), _CODES8[self.codes.dtype], self.square)
+
+    @staticmethod
+    def _need(blocks, what: str):
+        if not isinstance(blocks, Blocks8):
+            raise TypeError(f"{what}: expected Blocks8, got {type(blocks).__name__}")
+        if not blocks.codes.is_cuda:
+            raise ValueError(f"{what}: expected a device tensor, got Blocks8 on {blocks.codes.device}")
+
+
+def _code8(dtype: torch.dtype, what: str):
+    if dtype not in _CODES8:
+        raise ValueError(f"{what}: codes are float8_e4m3fn or float8_e5m2, got {dtype}")
+
+
+def block8_pack(x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, square: bool = False, along: str = "rows", stream=None):
+    """x [rows]...[cols], taken as a matrix, as an operand of products: along "rows" as it is, along "columns" its transpose, along
+    "both" the two of them from one reading.  A scale for 128 values along the operand's rows, or, square, for 128 x 128 of them."""
+    ld = _rows_stride(x, "block8_pack: x")
+    _code8(dtype, "block8_pack")
+    if along not in ("rows", "columns", "both"):
+        raise ValueError(f'block8_pack: along is "rows", "columns" or "both", got {along!r}')
+    if not _here(x, stream):
+        return _there(x, stream, (x,), lambda: block8_pack(x, dtype, square, along))
+    rows, cols, device = x.shape[:-1].numel(), x.shape[-1], x.device
+    by_rows = Blocks8._empty(rows, cols, dtype, square, device) if along != "columns" else None
+    by_columns = Blocks8._empty(cols, rows, dtype, square, device) if along != "rows" else None
+    _check(_lib.alexnet_block8_pack(x.data_ptr(), ld, _TYPES[x.dtype], rows, cols, None if by_rows is None else by_rows._arg(),
+                                    None if by_columns is None else by_columns._arg(), _raw_stream(device.index)))
+    return by_columns if by_rows is None else by_rows if by_columns is None else (by_rows, by_columns)
+
+
+def block8_unpack(blocks: Blocks8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values [rows][cols] of an operand as float32, bfloat16 or float16."""
+    Blocks8._need(blocks, "block8_unpack")
+    codes = blocks.codes
+    if dtype not in _TYPES:
+        raise ValueError(f"block8_unpack: expected float32, bfloat16 or float16, got {dtype}")
+    if not _here(codes, stream):
+        return _there(codes, stream, (blocks, out), lambda: block8_unpack(blocks, dtype, out))
+    x, ld = _result(out, blocks.shape, dtype, codes.device, "block8_unpack: out")
+    _check(_lib.alexnet_block8_unpack(blocks._arg(), codes.shape[0], blocks.cols, x.data_ptr(), ld, _TYPES[dtype],
+                                      _raw_stream(codes.get_device())))
+    return x
+
+
+@functools.lru_cache(maxsize=256)
+def _block8_product_ws(m: int, n: int, k: int, kind: int) -> int:
+    ws = _sz()
+    _check(_lib.alexnet_block8_product_query(m, n, k, kind, C.byref(ws)))
+    return ws.value
+
+
+def block8_product(a: Blocks8, b: Blocks8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """y [m][n] = a b^T of a [m][k] and b [n][k] in float32, bfloat16 or float16.  With w [out][in] a dense layer's forward pass is
+    block8_product(x, w), the gradient of x block8_product(dy, w along columns), that of w block8_product(dy along columns, x
+    along columns).  out: where y goes."""
+    Blocks8._need(a, "block8_product: a")
+    Blocks8._need(b, "block8_product: b")
+    codes = a.codes
+    if a.cols != b.cols or codes.device != b.codes.device:
+        raise ValueError(f"block8_product: a {list(a.shape)} on {codes.device} and b {list(b.shape)} on {b.codes.device} differ in "
+                         "their columns or device")
+    if dtype not in _TYPES:
+        raise ValueError(f"block8_product: expected float32, bfloat16 or float16, got {dtype}")
+    if not _here(codes, stream):
+        return _there(codes, stream, (a, b, out), lambda: block8_product(a, b, dtype, out))
+    m, n, k, kind, device = codes.shape[0], b.codes.shape[0], a.cols, _TYPES[dtype], codes.device
+    y, ld = _result(out, torch.Size((m, n)), dtype, device, "block8_product: out")
+    ws_bytes = _block8_product_ws(m, n, k, kind)
+    ws = _scratch(ws_bytes, device)
+    _check(_lib.alexnet_block8_product(a._arg(), b._arg(), m, n, k, y.data_ptr(), ld, kind, None if ws is None else ws.data_ptr(),
+                                       ws_bytes, _raw_stream(device.index)))
+    return y
+
+
+def rms_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                     blocks: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                     out_sum: Optional[torch.Tensor] = None, stream=None):
+    """y = s / sqrt(mean(s^2) + eps) * gamma over the last dimension of s = x + residual: (y, s, rstd [rows]).  Without a residual s
+    is x.  blocks: the type of the codes (torch.float8_e4m3fn, torch.float8_e5m2) to have y as Blocks8, else y is of x's type.  out,
+    out_sum: where y and s go (each may be x or residual)."""
+    what = "rms_norm_forward"
+    ld_x = _rows_stride(x, "rms_norm_forward: x")
+    if blocks is not None:
+        _code8(blocks, what)
+        if out is not None:
+            raise ValueError(f"{what}: y goes to Blocks8 or to out, not to both")
+    if out_sum is not None and residual is None:
+        raise ValueError(f"{what}: without a residual the sum is x, out_sum is not written")
+    if not _here(x, stream):
+        return _there(x, stream, (x, gamma, residual, out, out_sum),
+                      lambda: rms_norm_forward(x, gamma, residual, eps, blocks, out, out_sum))
+    shape, device = x.shape, x.device
+    rows, cols = shape[:-1].numel(), shape[-1]
+    p_gamma = _vector(gamma, cols, x, "rms_norm_forward: gamma")
+    s, ld_s, p_s, p_residual, ld_residual = x, 0, None, None, 0
+    if residual is not None:
+        ld_residual = _rows_stride(residual, "rms_norm_forward: residual")
+        if residual.shape != shape or residual.dtype != x.dtype or residual.device != device:
+            raise ValueError(f"{what}: x {list(shape)} and residual {list(residual.shape)} differ in shape, type or device")
+        s, ld_s = _result(out_sum, shape, x.dtype, device, "rms_norm_forward: out_sum")
+        p_s, p_residual = s.data_ptr(), residual.data_ptr()
+    if blocks is None:
+        y, ld_y = _result(out, shape, x.dtype, device, "rms_norm_forward: out")
+        p_y, arg = y.data_ptr(), None
+    else:
+        y, ld_y, p_y = Blocks8._empty(rows, cols, blocks, False, device), 0, None
+        arg = y._arg()
+    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    _check(_lib.alexnet_rms_norm_forward(x.data_ptr(), ld_x, p_residual, ld_residual, _TYPES[x.dtype], rows, cols, eps, p_gamma, p_s,
+                                         ld_s, p_y, ld_y, arg, rstd.data_ptr(), _raw_stream(device.index)))
+    return y, s, rstd
+
+
+@functools.lru_cache(maxsize=256)
+def _rms_norm_ws(rows: int, cols: int, kind: int) -> int:
+    ws = _sz()
+    _check(_lib.alexnet_rms_norm_query(rows, cols, kind, C.byref(ws)))
+    return ws.value
+
+
+def rms_norm_backward(s: torch.Tensor, dy: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
+                      dsum: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dgamma) of rms_norm_forward from its s and rstd, from dy and from dsum, the gradient that s has from elsewhere; dx is the
+    gradient of x and of the residual alike.  out: where dx goes (may be s, dy or dsum)."""
+    what = "rms_norm_backward"
+    ld_s, ld_dy = _rows_stride(s, "rms_norm_backward: s"), _rows_stride(dy, "rms_norm_backward: dy")
+    if not _here(dy, stream):
+        return _there(dy, stream, (s, dy, rstd, gamma, dsum, out), lambda: rms_norm_backward(s, dy, rstd, gamma, dsum, out))
+    shape, device = dy.shape, dy.device
+    if s.shape != shape or s.dtype != dy.dtype or s.device != device:
+        raise ValueError(f"{what}: s {list(s.shape)} and dy {list(shape)} differ in shape, type or device")
+    rows, cols, kind = shape[:-1].numel(), shape[-1], _TYPES[dy.dtype]
+    if rstd is None:
+        raise TypeError(f"{what}: rstd: expected a torch.Tensor, got NoneType")
+    p_rstd, p_gamma = _vector(rstd, rows, dy, "rms_norm_backward: rstd"), _vector(gamma, cols, dy, "rms_norm_backward: gamma")
+    p_dsum, ld_dsum = None, 0
+    if dsum is not None:
+        ld_dsum = _rows_stride(dsum, "rms_norm_backward: dsum")
+        if dsum.shape != shape or dsum.dtype != dy.dtype or dsum.device != device:
+            raise ValueError(f"{what}: dsum {list(dsum.shape)} and dy {list(shape)} differ in shape, type or device")
+        p_dsum = dsum.data_ptr()
+    dx, ld_dx = _result(out, shape, dy.dtype, device, "rms_norm_backward: out")
+    dgamma = torch.empty(cols, dtype=torch.float32, device=device)
+    ws_bytes = _rms_norm_ws(rows, cols, kind)
+    ws = _scratch(ws_bytes, device)
+    _check(_lib.alexnet_rms_norm_backward(s.data_ptr(), ld_s, dy.data_ptr(), ld_dy, p_dsum, ld_dsum, kind, rows, cols, p_rstd, p_gamma,
+                                          dx.data_ptr(), ld_dx, dgamma.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes,
+                                          _raw_stream(device.index)))
+    return dx, dgamma
+
+
+def _gradients(grads, what: str):
+    """Checked gradients, as (list, device, host tables of pointers, sizes and types)."""
+    grads = list(grads)
+    for g in grads:
+        if not isinstance(g, torch.Tensor):
+            raise TypeError(f"{what}: expected torch.Tensors, got {type(g).__name__}")
+        if not g.is_cuda or g.dtype not in _TYPES or not g.is_contiguous() or g.device != grads[0].device:
+            raise ValueError(f"{what}: expected contiguous float32, bfloat16 or float16 tensors on one device, got {g.dtype} "
+                             f"{list(g.shape)} of strides {g.stride()} on {g.device}")
+    if not grads:
+        raise ValueError(f"{what}: no gradients")
+    n = len(grads)
+    return grads, (_vp * n)(*map(torch.Tensor.data_ptr, grads)), (_i64 * n)(*map(torch.Tensor.numel, grads)), (
+        _i32 * n)(*[_TYPES[g.dtype] for g in grads])
+
+
+def _clip_ws(sizes) -> int:
+    ws = _sz()
+    _check(_lib.alexnet_clip_query(len(sizes), sizes, C.byref(ws)))
+    return ws.value
+
+
+def gradient_norm(grads, stream=None) -> torch.Tensor:
+    """The 2-norm over all values of all tensors (float32, bfloat16 or float16, mixed if wanted), as a float32 tensor of one element
+    on their device."""
+    grads, pointers, sizes, types = _gradients(grads, "gradient_norm")
+    first = grads[0]
+    if not _here(first, stream):
+        return _there(first, stream, grads, lambda: gradient_norm(grads))
+    norm = torch.empty((), dtype=torch.float32, device=first.device)
+    ws_bytes = _clip_ws(sizes)
+    ws = _scratch(ws_bytes, first.device)
+    _check(_lib.alexnet_gradient_norm(len(grads), pointers, sizes, types, norm.data_ptr(), ws.data_ptr(), ws_bytes,
+                                      _raw_stream(first.get_device())))
+    return norm
+
+
+def clip_gradients(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
+    """Scales all tensors by max_norm / norm if their gradient_norm is over max_norm, and returns that norm.  out: tensors of the same
+    sizes and types that receive the result (each may be its own gradient); otherwise that happens in place.  Where the norm is an
+    infinity or a NaN nothing is scaled."""
+    what = "clip_gradients"
+    grads, pointers, sizes, types = _gradients(grads, what)
+    results = None
+    if out is not None:
+        out, results, out_sizes, out_types = _gradients(out, "clip_gradients: out")
+        if len(out) != len(grads) or out_sizes[:] != sizes[:] or out_types[:] != types[:] or out[0].device != grads[0].device:
+            raise ValueError(f"{what}: out differs from the gradients in number, sizes, types or device")
+    first = grads[0]
+    if not _here(first, stream):
+        return _there(first, stream, grads + (out or []), lambda: clip_gradients(grads, max_norm, out))
+    norm = torch.empty((), dtype=torch.float32, device=first.device)
+    ws_bytes = _clip_ws(sizes)
+    ws = _scratch(ws_bytes, first.device)
+    _check(_lib.alexnet_clip_gradients(len(grads), pointers, results, sizes, types, max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes,
+                                       _raw_stream(first.get_device())))
+    return norm

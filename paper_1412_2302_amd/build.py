@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libalexnet_hip.so")
 SOURCES = ["alexnet.hip", "conv_gemm.hip", "wave_gemm.hip", "first_layer.hip", "first_weight.hip", "weight_direct.hip", "patch_conv.hip", "ops.hip", "winograd.hip", "loader.hip",
-           "group_norm.hip", "group_norm_resident.hip", "checkpoint.hip", "checkpoint_fc.hip"]
+           "group_norm.hip", "group_norm_resident.hip", "checkpoint.hip", "checkpoint_fc.hip",
+           "block8.hip", "block8_product.hip", "rms_norm.hip", "rms_norm_bwd.hip", "clip.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc", "-Wall", "-Wno-unused-function",
     # packed fp32 VALU ops are kept off

@@ -1,0 +1,432 @@
+// y [m][n] = a b^T of two operands in 8-bit floating point with power-of-two scales per block of 128 (blocks8.h):
+//   y[i][j] = sum over blocks B of 2^(sa[B][i] + sb[B][j] - 254) * sum over k in B of code_a[i][k] * code_b[j][k]
+//
+// Two kinds of arithmetic, by the type of y.
+//   16 bits: the 8-bit matrix instruction, which takes 32 (64, for 32 x 32 results) of the sum with a scale byte for each lane's row,
+//     so that scales cost the load of a word per block.  It adds eight products at a time with 13 bits under the largest of the
+//     eight (measured; the sums of those eights go on in float32), 1.5e-5 of a result of normal numbers and a hundredth of what
+//     rounding it to bf16 costs, a twentieth to fp16: a choice for twice the rate.
+//   32 bits: codes are widened to bf16 with their scales, which is exact, and go through the bf16 instruction, whose sums are
+//     float32 throughout: 6e-8 of a result.
+//
+// Tiles.  A workgroup of four waves owns BM x BN of y; operands go from memory to LDS directly (buffer_load ... lds), a block of 128 at a time:
+// a row of a stage is the 128 bytes of one row's block, eight 16-byte units, unit (row, slot) holding slot ^ (row & 7), so that
+// a fragment read of eight rows touches all banks and a load instruction brings eight whole lines.  Rows are dealt out in
+// turn to the tiles of a wave: row t of every TM goes to tile t.  That gives a lane's TM (TN) rows their scales as one word, which the instruction
+// picks its byte from, and makes a lane's TN results neighbours in y.
+#include <algorithm>
+
+#include "blocks8.h"
+#include "kernels.h"
+#include "product_plan.h"
+
+namespace ax {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+
+struct ProductArgs {
+  const uint8_t *a, *b, *sa, *sb;
+  long pitch, spa, spb;  // bytes of a row of codes; of a block's scales
+  long m, n, ld;
+  int nb, a_square, b_square;
+  void* y;
+  float* part;  // slices
+  long slab;
+  int type, tiles_m, tiles_n, slices, steps;
+};
+
+__device__ __forceinline__ Rsrc rsrc_of(const uint8_t* p, long bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)min(bytes, 0x7fffffffL), 0x00020000);
+}
+
+// N neighbouring results of a row, of which `has` lie inside it
+template <int N>
+__device__ __forceinline__ void store_results(const ProductArgs& p, int slice, long row, long col, const float* v) {
+  const long has = p.n - col;
+  if (has <= 0) return;
+  auto put = [&](auto* q) {
+    typedef typename std::remove_pointer<decltype(q)>::type T;
+    q += col;
+    if (has >= N) {
+      Pack<T, N>::store(q, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i < has) q[i] = (T)v[i];
+    }
+  };
+  if (p.part)
+    put(p.part + slice * p.slab + row * p.n);
+  else if (p.type == ALEXNET_TYPE_FP32)
+    put((float*)p.y + row * p.ld);
+  else if (p.type == ALEXNET_TYPE_BF16)
+    put((__bf16*)p.y + row * p.ld);
+  else
+    put((_Float16*)p.y + row * p.ld);
+}
+
+// Eight codes of a lane as bf16, with their scale.  FMT: 0 E4M3, 1 E5M2, as the 8-bit instruction numbers them.
+template <int FMT>
+__device__ __forceinline__ v8bf widen8(int lo, int hi, float scale) {
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  v8bf r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int w = i < 2 ? lo : hi;
+    v2bf p;
+    if constexpr (FMT == 0)
+      p = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+    else
+      p = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, false);
+    r[2 * i] = p[0];
+    r[2 * i + 1] = p[1];
+  }
+  return r;
+}
+
+// ---- tiles ------------------------------------------------------------------------
+__device__ __forceinline__ void stage_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ void load_unit(const Rsrc& r, Word4* to, int off, int from) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, off, from, 0, 0);
+}
+// a block's scales, from those of row0 on
+__device__ __forceinline__ Rsrc scales_of(const uint8_t* s, long pitch, int square, long row0, int block) {
+  const long start = square ? row0 / kBlock8 : row0;
+  return rsrc_of(s + block * pitch + start, max(pitch - start, 0L));
+}
+// scales of TM (at most four) neighbouring rows: a byte each
+template <int TM>
+__device__ __forceinline__ uint32_t load_scales(const Rsrc& r, int off, bool square) {
+  if (square) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(r, off, 0, 0) * 0x01010101u;
+  return TM == 4 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0) : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
+}
+
+template <int FA, int FB, bool WIDE, int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ void __launch_bounds__(64 * WAVES_M * WAVES_N, BM == 256 ? 1 : 2) block8_tile_kernel(ProductArgs p) {
+  constexpr int kWaves = WAVES_M * WAVES_N, TM = BM / (32 * WAVES_M), TN = BN / (32 * WAVES_N);  // a wave's tiles of 32 x 32
+  constexpr int kLoadsA = BM / (8 * kWaves), kLoadsB = BN / (8 * kWaves);                        // of a lane and step
+  __shared__ __attribute__((aligned(16))) Word4 stage0[(BM + BN) * 8];
+  __shared__ __attribute__((aligned(16))) Word4 stage1[(BM + BN) * 8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WAVES_M, wn = wave / WAVES_M;
+  // neighbouring tiles to one of the eight dies
+  const uint32_t total = gridDim.x, L = blockIdx.x, q8 = total >> 3, r8 = total & 7, xcd = L & 7;
+  const uint32_t tile = xcd * q8 + min(xcd, r8) + (L >> 3);
+  const int slice = tile / (p.tiles_m * p.tiles_n), in_slice = tile - slice * (p.tiles_m * p.tiles_n);
+  const int tm = in_slice / p.tiles_n, tn = in_slice - tm * p.tiles_n;
+  const long m0 = (long)tm * BM, n0 = (long)tn * BN;
+  const int first = slice * p.steps, steps = min(p.steps, p.nb - first);
+
+  // rows past the end lie outside of the buffers and read as zeros
+  const Rsrc ra = rsrc_of(p.a + m0 * p.pitch, min((long)BM, p.m - m0) * p.pitch);
+  const Rsrc rb = rsrc_of(p.b + n0 * p.pitch, min((long)BN, p.n - n0) * p.pitch);
+  int off_a[kLoadsA], off_b[kLoadsB];
+  auto offset = [&](int i, int deal) {
+    const int at = (i * kWaves + wave) * 8 + (lane >> 3);  // row of the stage
+    const int row = at / (32 * deal) * (32 * deal) + deal * (at & 31) + at / 32 % deal;
+    return row * (int)p.pitch + 16 * ((lane & 7) ^ (lane >> 3));
+  };
+#pragma unroll
+  for (int i = 0; i < kLoadsA; ++i) off_a[i] = offset(i, TM);
+#pragma unroll
+  for (int i = 0; i < kLoadsB; ++i) off_b[i] = offset(i, TN);
+  const long srow = m0 + wm * 32 * TM, scol = n0 + wn * 32 * TN;
+  const int a_at = p.a_square ? 0 : TM * (lane & 31), b_at = p.b_square ? 0 : TN * (lane & 31);
+  uint32_t sa, sb, sa_next, sb_next;
+  auto load = [&](Word4* st, int step) {
+    const int k = (first + step) * kBlock8;
+#pragma unroll
+    for (int i = 0; i < kLoadsA; ++i)
+      load_unit(ra, st + (i * kWaves + wave) * 64, off_a[i], k);
+#pragma unroll
+    for (int i = 0; i < kLoadsB; ++i)
+      load_unit(rb, st + BM * 8 + (i * kWaves + wave) * 64, off_b[i], k);
+    sa_next = load_scales<TM>(scales_of(p.sa, p.spa, p.a_square, srow, first + step), a_at, p.a_square);
+    sb_next = load_scales<TN>(scales_of(p.sb, p.spb, p.b_square, scol, first + step), b_at, p.b_square);
+  };
+
+  v16f acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  const int row = lane & 31, half = lane >> 5;
+  auto fragment = [&](const Word4* st, int at, int kk) {
+    const int u = 4 * kk + 2 * half;
+    const Word4 lo = st[(at + row) * 8 + (u ^ (row & 7))], hi = st[(at + row) * 8 + ((u + 1) ^ (row & 7))];
+    return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+  auto multiply = [&](const Word4* st) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      if (BM == 256) __builtin_amdgcn_sched_barrier(0);  // fragments of both halves are more than the registers hold
+      v8i a[TM], b[TN];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) a[i] = fragment(st, wm * 32 * TM + 32 * i, kk);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[j] = fragment(st, BM + wn * 32 * TN + 32 * j, kk);
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {  // any eight of a lane's codes: both operands take the same
+          v8bf wa[TM], wb[TN];
+#pragma unroll
+          for (int i = 0; i < TM; ++i) wa[i] = widen8<FA>(a[i][2 * q], a[i][2 * q + 1], code_scale(sa >> 8 * i & 255));
+#pragma unroll
+          for (int j = 0; j < TN; ++j) wb[j] = widen8<FB>(b[j][2 * q], b[j][2 * q + 1], code_scale(sb >> 8 * j & 255));
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
+        }
+        continue;
+      }
+#define AX_TILE(I, J)                 \
+  if constexpr (I < TM && J < TN)     \
+  acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[I], b[J], acc[I][J], FA, FB, I, (int)sa, J, (int)sb)
+#define AX_TILES(I) \
+  AX_TILE(I, 0);    \
+  AX_TILE(I, 1)
+      AX_TILES(0);
+      AX_TILES(1);
+      AX_TILES(2);
+      AX_TILES(3);
+#undef AX_TILES
+#undef AX_TILE
+    }
+  };
+  load(stage0, 0);
+  for (int t = 0; t < steps; t += 2) {
+    stage_barrier();
+    sa = sa_next;
+    sb = sb_next;
+    if (t + 1 < steps) load(stage1, t + 1);
+    multiply(stage0);
+    if (t + 1 >= steps) break;
+    stage_barrier();
+    sa = sa_next;
+    sb = sb_next;
+    if (t + 2 < steps) load(stage0, t + 2);
+    multiply(stage1);
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const long y = m0 + wm * 32 * TM + TM * (8 * (r / 4) + 4 * half + r % 4) + i;
+      float v[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) v[j] = acc[i][j][r];
+      if (y < p.m) store_results<TN>(p, slice, y, n0 + wn * 32 * TN + TN * row, v);
+    }
+}
+
+// ---- few rows ---------------------------------------------------------------------
+// What counts is how many loads of b are on their way: a workgroup has 16 of its rows and all of a's, its eight waves a block of the sum in turn,
+// both operands straight to registers; the waves' sums meet in LDS.
+constexpr int kRowWaves = 8;
+template <int FA, int FB, bool WIDE, int MT>
+__global__ void __launch_bounds__(64 * kRowWaves) block8_rows_kernel(ProductArgs p) {
+  __shared__ v4f sums[kRowWaves][MT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int tn = blockIdx.x / p.tiles_m, tm = blockIdx.x - tn * p.tiles_m;
+  const long m0 = (long)tm * 16 * MT, n0 = (long)tn * 16;
+  const int row = lane & 15, part = lane >> 4;
+  const long b_row = min(n0 + row, p.n - 1);
+  const uint8_t* const b = p.b + b_row * p.pitch + 32 * part;
+  const uint8_t* const sb = p.sb + (p.b_square ? b_row / kBlock8 : b_row);
+  const uint8_t *a[MT], *sa[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const long r = min(m0 + 16 * i + row, p.m - 1);
+    a[i] = p.a + r * p.pitch + 32 * part;
+    sa[i] = p.sa + (p.a_square ? r / kBlock8 : r);
+  }
+  v4f acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = v4f{0.f, 0.f, 0.f, 0.f};
+  auto fragment = [](const uint8_t* q) { return *reinterpret_cast<const v8i*>(q); };
+  for (int kb = wave; kb < p.nb; kb += kRowWaves) {
+    const v8i fb = fragment(b + (long)kb * kBlock8);
+    const int s = sb[kb * p.spb];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const v8i fa = fragment(a[i] + (long)kb * kBlock8);
+      const int t = sa[i][kb * p.spa];
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FA>(fa[2 * q], fa[2 * q + 1], code_scale(t)),
+                                                          widen8<FB>(fb[2 * q], fb[2 * q + 1], code_scale(s)), acc[i], 0, 0, 0);
+      } else {
+        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[i], FA, FB, 0, t, 0, s);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+  __syncthreads();
+  if (wave >= MT) return;
+  v4f v = sums[0][wave][lane];
+#pragma unroll
+  for (int w = 1; w < kRowWaves; ++w) v += sums[w][wave][lane];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const long y = m0 + 16 * wave + 4 * part + r;
+    const float f[1] = {v[r]};
+    if (y < p.m) store_results<1>(p, 0, y, n0 + row, f);
+  }
+}
+
+// y = the sum of the slices
+template <typename T>
+__global__ void __launch_bounds__(256) block8_sum_kernel(const float* __restrict__ part, long slab, int slices, long m, long n, T* y, long ld) {
+  const long vecs = (n + 7) / 8, i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= m * vecs) return;
+  const long row = i / vecs, col = (i - row * vecs) * 8;
+  const float* const q = part + row * n + col;
+  float v[8];
+  load8(q, n - col, v);
+  for (int s = 1; s < slices; ++s) {
+    float w[8];
+    load8(q + s * slab, n - col, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  }
+  store8(y + row * ld + col, n - col, v);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) block8_zero_kernel(T* y, long m, long n, long ld) {
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < m * n; i += (long)gridDim.x * 256) y[i / n * ld + i % n] = (T)0.f;
+}
+
+template <int FA, int FB, bool WIDE>
+static int product_launch(const ProductArgs& a, const ProductPlan& p, hipStream_t st) {
+  const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.slices));
+  if (p.kind == PRODUCT_256)
+    hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 256, 256, 2, 4>), grid, dim3(512), 0, st, a);
+  else if (p.kind == PRODUCT_128)
+    hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 128, 128, 2, 2>), grid, dim3(256), 0, st, a);
+  else if (p.mt == 1)
+    hipLaunchKernelGGL((block8_rows_kernel<FA, FB, WIDE, 1>), grid, dim3(64 * kRowWaves), 0, st, a);
+  else if (p.mt == 2)
+    hipLaunchKernelGGL((block8_rows_kernel<FA, FB, WIDE, 2>), grid, dim3(64 * kRowWaves), 0, st, a);
+  else
+    hipLaunchKernelGGL((block8_rows_kernel<FA, FB, WIDE, 4>), grid, dim3(64 * kRowWaves), 0, st, a);
+  AX_LAUNCH_CHECK();
+  return ALEXNET_OK;
+}
+template <int FA, int FB>
+static int product_launch_type(const ProductArgs& a, const ProductPlan& p, hipStream_t st) {
+  return a.type == ALEXNET_TYPE_FP32 ? product_launch<FA, FB, true>(a, p, st) : product_launch<FA, FB, false>(a, p, st);
+}
+template <typename T>
+static int product_sum(const ProductArgs& a, hipStream_t st) {
+  KernelScope ks("block8_product_sum", 0, (double)a.m * a.n * (4.0 * a.slices + sizeof(T)), st);
+  hipLaunchKernelGGL(block8_sum_kernel<T>, dim3((unsigned)((a.m * ((a.n + 7) / 8) + 255) / 256)), dim3(256), 0, st, a.part, a.slab, a.slices, a.m, a.n,
+                     (T*)a.y, a.ld);
+  AX_LAUNCH_CHECK();
+  return ALEXNET_OK;
+}
+template <typename T>
+static int product_zero(void* y, long m, long n, long ld, hipStream_t st) {
+  hipLaunchKernelGGL(block8_zero_kernel<T>, dim3((unsigned)std::min((m * n + 255) / 256, 1L << 16)), dim3(256), 0, st, (T*)y, m, n, ld);
+  AX_LAUNCH_CHECK();
+  return ALEXNET_OK;
+}
+
+static int check_product(const char* who, long m, long n, long k, int type) {
+  AX_REQUIRE(type_ok(type), ALEXNET_EINVAL, "%s: unknown type %d", who, type);
+  AX_REQUIRE(m >= 0 && m <= 1L << 28 && n >= 0 && n <= 1L << 28 && k >= 0 && k <= 1L << 22 && m * n <= 1L << 32 &&
+                 blocks_sizes_ok(m, k) && blocks_sizes_ok(n, k),
+             ALEXNET_ESHAPE, "%s: bad sizes, %ld by %ld over %ld (at most 2^28 rows of an operand, 2^22 columns, 2^32 results)", who, m, n, k);
+  AX_REQUIRE(m == 0 || n == 0 || product_plan(m, n, k).fits, ALEXNET_ESHAPE, "%s: %ld by %ld over %ld are more than one launch covers", who, m, n, k);
+  return ALEXNET_OK;
+}
+
+}  // namespace ax
+
+using namespace ax;
+
+extern "C" {
+
+int alexnet_block8_product_query(int64_t m, int64_t n, int64_t k, int32_t type, size_t* workspace_bytes) {
+  AX_TRY(check_product("alexnet_block8_product_query", m, n, k, type));
+  AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_block8_product_query: null argument");
+  *workspace_bytes = m && n ? product_plan(m, n, k).ws : 0;
+  return ALEXNET_OK;
+}
+
+int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* b, int64_t m, int64_t n, int64_t k, void* d_y, int64_t ld_y,
+                           int32_t type, void* d_workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "alexnet_block8_product";
+  AX_TRY(check_product(who, m, n, k, type));
+  if (m == 0 || n == 0) return ALEXNET_OK;
+  AX_REQUIRE(d_y, ALEXNET_EINVAL, "%s: null argument", who);
+  AX_REQUIRE(ld_y >= n && ld_y <= 1L << 40, ALEXNET_ESHAPE, "%s: row stride %ld of %ld columns", who, (long)ld_y, (long)n);
+  AX_REQUIRE((uintptr_t)d_y % type_size(type) == 0, ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
+  hipStream_t st = (hipStream_t)stream;
+  if (k == 0)
+    return type == ALEXNET_TYPE_FP32   ? product_zero<float>(d_y, m, n, ld_y, st)
+           : type == ALEXNET_TYPE_BF16 ? product_zero<__bf16>(d_y, m, n, ld_y, st)
+                                       : product_zero<_Float16>(d_y, m, n, ld_y, st);
+  AX_TRY(check_blocks(a, "a", who));
+  AX_TRY(check_blocks(b, "b", who));
+  const ProductPlan p = product_plan(m, n, k);
+  AX_TRY(check_scratch(who, d_workspace, workspace_bytes, p.ws));
+  const long size = (long)type_size(type);
+  AX_TRY(check_apart(who,
+                     {{"a's codes", blocks_codes(a, m, k), false},
+                      {"a's scales", blocks_scales(a, m, k), false},
+                      {"b's codes", blocks_codes(b, n, k), false},
+                      {"b's scales", blocks_scales(b, n, k), false}},
+                     {{"y", Region(d_y, m, ld_y * size, n * size), false}, {"the workspace", Region(p.ws ? d_workspace : nullptr, (long)p.ws), false}}));
+  ProductArgs g = {};
+  g.a = (const uint8_t*)a->d_codes;
+  g.b = (const uint8_t*)b->d_codes;
+  g.sa = (const uint8_t*)a->d_scales;
+  g.sb = (const uint8_t*)b->d_scales;
+  g.pitch = codes_pitch(k);
+  g.spa = scales_pitch(m, a->square);
+  g.spb = scales_pitch(n, b->square);
+  g.m = m;
+  g.n = n;
+  g.ld = ld_y;
+  g.nb = (int)blocks_along(k);
+  g.a_square = a->square;
+  g.b_square = b->square;
+  g.y = d_y;
+  g.part = p.slices > 1 ? (float*)d_workspace : nullptr;
+  g.slab = (long)p.slab;
+  g.type = type;
+  g.tiles_m = p.tiles_m;
+  g.tiles_n = p.tiles_n;
+  g.slices = p.slices;
+  g.steps = p.steps;
+  {
+    KernelScope ks("block8_product", 2.0 * m * n * k, (double)(m + n) * k + (double)m * n * size, st);
+    const bool b4 = b->code == ALEXNET_CODE_E4M3;
+    AX_TRY(a->code == ALEXNET_CODE_E4M3 ? (b4 ? product_launch_type<0, 0>(g, p, st) : product_launch_type<0, 1>(g, p, st))
+                                        : (b4 ? product_launch_type<1, 0>(g, p, st) : product_launch_type<1, 1>(g, p, st)));
+  }
+  if (p.slices == 1) return ALEXNET_OK;
+  return type == ALEXNET_TYPE_FP32   ? product_sum<float>(g, st)
+         : type == ALEXNET_TYPE_BF16 ? product_sum<__bf16>(g, st)
+                                     : product_sum<_Float16>(g, st);
+}
+
+}  // extern "C"

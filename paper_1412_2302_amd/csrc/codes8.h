@@ -51,6 +51,12 @@ inline int check_apart(const char* who, std::initializer_list<Buffer> reads, std
   }
   return ALEXNET_OK;
 }
+inline int check_scratch(const char* who, const void* ws, size_t bytes, size_t need) {
+  if (!need) return ALEXNET_OK;
+  AX_REQUIRE(ws && bytes >= need, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, ws ? bytes : (size_t)0, need);
+  AX_REQUIRE((uintptr_t)ws % 256 == 0, ALEXNET_EALIGN, "%s: workspace is not 256-byte aligned", who);
+  return ALEXNET_OK;
+}
 inline Region codes_of(const alexnet_checkpoint_t* k, long rows, long cols) { return Region(k ? k->d_codes : nullptr, rows * cols); }
 inline Region scales_of(const alexnet_checkpoint_t* k, long rows, long cols) {
   return Region(k ? k->d_scales : nullptr, rows * ceil_div(cols, kCodeBlock));
@@ -120,7 +126,8 @@ __device__ __forceinline__ void codes_to_float4(uint32_t w, float s, float* v) {
     v[3] = ((float)(w >> 24) - 128.f) * s;
   } else {
     typedef float f2 __attribute__((ext_vector_type(2)));
-    const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    const f2 lo = CODE == ALEXNET_CODE_E5M2 ? __builtin_amdgcn_cvt_pk_f32_bf8((int)w, false) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+    const f2 hi = CODE == ALEXNET_CODE_E5M2 ? __builtin_amdgcn_cvt_pk_f32_bf8((int)w, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     v[0] = lo[0] * s;
     v[1] = lo[1] * s;
     v[2] = hi[0] * s;
@@ -159,11 +166,11 @@ __device__ __forceinline__ uint32_t block_max_bits(const float* v) {
 }
 
 // the scale code of a block whose largest magnitude has these bits: a fraction over that of 127 = 1.984375 * 2^6 (448 =
-// 1.75 * 2^8) carries into the exponent
+// 1.75 * 2^8, 57344 = 1.75 * 2^15) carries into the exponent
 template <int CODE>
 __device__ __forceinline__ uint32_t scale_code(uint32_t m) {
   const uint32_t top = CODE == ALEXNET_CODE_INT8 ? 0x7e0000u : 0x600000u;
-  const int e = (int)((m + (0x7fffffu - top)) >> 23) - (CODE == ALEXNET_CODE_INT8 ? 6 : 8);
+  const int e = (int)((m + (0x7fffffu - top)) >> 23) - (CODE == ALEXNET_CODE_INT8 ? 6 : CODE == ALEXNET_CODE_E4M3 ? 8 : 15);
   return m >= 0x7f800000u ? 255u : (uint32_t)max(e, 1);
 }
 
@@ -178,6 +185,10 @@ __device__ __forceinline__ uint32_t floats_to_codes4(const float* v, float inv) 
     return lo | hi << 16;
   }
   int w = 0;
+  if (CODE == ALEXNET_CODE_E5M2) {
+    w = __builtin_amdgcn_cvt_pk_bf8_f32(v[0] * inv, v[1] * inv, w, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(v[2] * inv, v[3] * inv, w, true);
+  }
   w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, w, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, w, true);
   return (uint32_t)w;

@@ -647,12 +647,6 @@ static void gn_scratch(GnArgs& a, void* ws, size_t bytes) {
   a.part = (float*)ws;
   a.stat = (float*)((char*)ws + (bytes >= stat_bytes(a) ? bytes - stat_bytes(a) : 0));
 }
-static int check_scratch(const char* who, const void* ws, size_t bytes, size_t need) {
-  if (!need) return ALEXNET_OK;
-  AX_REQUIRE(ws && bytes >= need, ALEXNET_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, ws ? bytes : (size_t)0, need);
-  AX_REQUIRE((uintptr_t)ws % 256 == 0, ALEXNET_EALIGN, "%s: workspace is not 256-byte aligned", who);
-  return ALEXNET_OK;
-}
 
 // a map of the call, and what a call holds per picture and group, or per channel
 static Region map_of(const alexnet_group_norm_t* cfg, const void* p, long ld) {
