@@ -9,12 +9,13 @@
 //   32 bits: codes are widened to bf16 with their scales, which is exact, and go through the bf16 instruction, whose sums are
 //     float32 throughout: 6e-8 of a result.
 //
-// Tiles.  A workgroup of four waves owns BM x BN of y; operands go from memory to LDS directly (buffer_load ... lds), a block of 128 at a time:
-// a row of a stage is the 128 bytes of one row's block, eight 16-byte units, unit (row, slot) holding slot ^ (row & 7), so that
-// a fragment read of eight rows touches all banks and a load instruction brings eight whole lines.  Rows are dealt out in
-// turn to the tiles of a wave: row t of every TM goes to tile t.  That gives a lane's TM (TN) rows their scales as one word, which the instruction
-// picks its byte from, and makes a lane's TN results neighbours in y.
+// Tiles.  Operands go from memory to LDS directly (buffer_load ... lds), a block of 128 at a time: a row of a stage is the 128 bytes
+// of one row's block, eight 16-byte units, unit (row, slot) holding slot ^ (row & 7), so that a fragment read of eight rows
+// touches all banks and a load instruction brings eight whole lines.  Rows are dealt out in turn to the tiles of a wave: with TM of
+// them row r goes to tile r % TM.  That gives a lane the scales of four tiles as one word, which the instruction picks its byte
+// from, and makes a lane's TN results neighbours in y.
 #include <algorithm>
+#include <utility>
 
 #include "blocks8.h"
 #include "kernels.h"
@@ -39,9 +40,11 @@ struct ProductArgs {
   int type, tiles_m, tiles_n, slices, steps;
 };
 
-__device__ __forceinline__ Rsrc rsrc_of(const uint8_t* p, long bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)min(bytes, 0x7fffffffL), 0x00020000);
+__device__ __forceinline__ Rsrc rsrc_of(const uint8_t* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, bytes, 0x00020000);
 }
+// A number that is the same for all lanes, for the compiler to see
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // N neighbouring results of a row, of which `has` lie inside it
 template <int N>
@@ -101,136 +104,192 @@ __device__ __forceinline__ void stage_barrier() {
 __device__ __forceinline__ void load_unit(const Rsrc& r, Word4* to, int off, int from) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, off, from, 0, 0);
 }
-// a block's scales, from those of row0 on
-__device__ __forceinline__ Rsrc scales_of(const uint8_t* s, long pitch, int square, long row0, int block) {
-  const long start = square ? row0 / kBlock8 : row0;
-  return rsrc_of(s + block * pitch + start, max(pitch - start, 0L));
-}
-// scales of TM (at most four) neighbouring rows: a byte each
-template <int TM>
-__device__ __forceinline__ uint32_t load_scales(const Rsrc& r, int off, bool square) {
-  if (square) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(r, off, 0, 0) * 0x01010101u;
-  return TM == 4 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0) : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
+// The scales of four neighbouring rows, a byte each, from s on, `left` bytes of which are a block's: of rows, the word at a lane's
+// `off`; of squares, one byte for all.  One of the two comes from an empty buffer, as zeros.  Put together only when they are used: until
+// then nothing waits for them.
+struct FourScales {
+  uint32_t rows, one;
+  __device__ __forceinline__ uint32_t word() const { return rows | one * 0x01010101u; }
+};
+__device__ __forceinline__ FourScales load_scales(const uint8_t* s, int left, int square, int off) {
+  return FourScales{(uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc_of(s, square ? 0 : left), off, 0, 0),
+                    (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rsrc_of(s, square ? left : 0), 0, 0, 0)};
 }
 
-template <int FA, int FB, bool WIDE, int BM, int BN, int WAVES_M, int WAVES_N>
-__global__ void __launch_bounds__(64 * WAVES_M * WAVES_N, BM == 256 ? 1 : 2) block8_tile_kernel(ProductArgs p) {
-  constexpr int kWaves = WAVES_M * WAVES_N, TM = BM / (32 * WAVES_M), TN = BN / (32 * WAVES_N);  // a wave's tiles of 32 x 32
-  constexpr int kLoadsA = BM / (8 * kWaves), kLoadsB = BN / (8 * kWaves);                        // of a lane and step
-  __shared__ __attribute__((aligned(16))) Word4 stage0[(BM + BN) * 8];
-  __shared__ __attribute__((aligned(16))) Word4 stage1[(BM + BN) * 8];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave % WAVES_M, wn = wave / WAVES_M;
+// f(0), f(1), ... with the numbers as constants
+template <typename F, int... I>
+__device__ __forceinline__ void for_each_index(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+
+// SIDE x SIDE of y, by waves of 16 TM x 16 TN.  The blocks of the sum take turns in two stages.  In a step a wave holds its fragments
+// of b and goes through those of a, each read two rows of products ahead; before the last two rows
+//   the workgroup meets: this stage has been read, the other one has arrived; the stage's next block is sent for,
+// and each fragment of b is read again, from the other stage, as soon as the last two products with it have begun.  So a block has
+// the whole of a step to arrive and no product waits for LDS.  Blocks past the end come from an empty buffer, as zeros that nothing
+// multiplies.
+//
+// 16 x 16 results, not 32 x 32: the larger instruction does the same work a clock, but the compiler gives its results registers of
+// their own beside those of its accumulator, which spills.
+template <int FA, int FB, bool WIDE, int SIDE>
+__global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel(ProductArgs p) {
+  constexpr int kWaves = SIDE / 32, TM = SIDE / 32, TN = 4, kLoads = 4;  // tiles of a wave; loads of a lane, operand and step
+  constexpr auto kAcross = std::make_integer_sequence<int, TN>();
+  __shared__ __attribute__((aligned(16))) Word4 stage0[2 * SIDE * 8];
+  __shared__ __attribute__((aligned(16))) Word4 stage1[2 * SIDE * 8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int wm = wave & 1, wn = wave >> 1;
   // neighbouring tiles to one of the eight dies
   const uint32_t total = gridDim.x, L = blockIdx.x, q8 = total >> 3, r8 = total & 7, xcd = L & 7;
-  const uint32_t tile = xcd * q8 + min(xcd, r8) + (L >> 3);
-  const int slice = tile / (p.tiles_m * p.tiles_n), in_slice = tile - slice * (p.tiles_m * p.tiles_n);
-  const int tm = in_slice / p.tiles_n, tn = in_slice - tm * p.tiles_n;
-  const long m0 = (long)tm * BM, n0 = (long)tn * BN;
+  const int tile = (int)(xcd * q8 + min(xcd, r8) + (L >> 3));
+  const int slice = uniform(tile / (p.tiles_m * p.tiles_n)), in_slice = tile - slice * (p.tiles_m * p.tiles_n);
+  const int tm = uniform(in_slice / p.tiles_n), tn = in_slice - tm * p.tiles_n;
+  const long m0 = (long)tm * SIDE, n0 = (long)tn * SIDE;
   const int first = slice * p.steps, steps = min(p.steps, p.nb - first);
 
   // rows past the end lie outside of the buffers and read as zeros
-  const Rsrc ra = rsrc_of(p.a + m0 * p.pitch, min((long)BM, p.m - m0) * p.pitch);
-  const Rsrc rb = rsrc_of(p.b + n0 * p.pitch, min((long)BN, p.n - n0) * p.pitch);
-  int off_a[kLoadsA], off_b[kLoadsB];
+  const uint8_t *const pa = p.a + m0 * p.pitch, *const pb = p.b + n0 * p.pitch;
+  const int rows_a = uniform((int)min((long)SIDE, p.m - m0)), rows_b = uniform((int)min((long)SIDE, p.n - n0));
+  const int bytes_a = rows_a * (int)p.pitch, bytes_b = rows_b * (int)p.pitch;
+  int off_a[kLoads], off_b[kLoads];
   auto offset = [&](int i, int deal) {
     const int at = (i * kWaves + wave) * 8 + (lane >> 3);  // row of the stage
-    const int row = at / (32 * deal) * (32 * deal) + deal * (at & 31) + at / 32 % deal;
+    const int row = at / (16 * deal) * (16 * deal) + deal * (at & 15) + at / 16 % deal;
     return row * (int)p.pitch + 16 * ((lane & 7) ^ (lane >> 3));
   };
 #pragma unroll
-  for (int i = 0; i < kLoadsA; ++i) off_a[i] = offset(i, TM);
-#pragma unroll
-  for (int i = 0; i < kLoadsB; ++i) off_b[i] = offset(i, TN);
-  const long srow = m0 + wm * 32 * TM, scol = n0 + wn * 32 * TN;
-  const int a_at = p.a_square ? 0 : TM * (lane & 31), b_at = p.b_square ? 0 : TN * (lane & 31);
-  uint32_t sa, sb, sa_next, sb_next;
+  for (int i = 0; i < kLoads; ++i) {
+    off_a[i] = offset(i, TM);
+    off_b[i] = offset(i, TN);
+  }
   auto load = [&](Word4* st, int step) {
-    const int k = (first + step) * kBlock8;
+    const int k = uniform((first + step) * kBlock8);
+    const Rsrc ra = rsrc_of(pa, uniform(step < steps ? bytes_a : 0)), rb = rsrc_of(pb, uniform(step < steps ? bytes_b : 0));
 #pragma unroll
-    for (int i = 0; i < kLoadsA; ++i)
-      load_unit(ra, st + (i * kWaves + wave) * 64, off_a[i], k);
+    for (int i = 0; i < kLoads; ++i) load_unit(ra, st + (i * kWaves + wave) * 64, off_a[i], k);
 #pragma unroll
-    for (int i = 0; i < kLoadsB; ++i)
-      load_unit(rb, st + BM * 8 + (i * kWaves + wave) * 64, off_b[i], k);
-    sa_next = load_scales<TM>(scales_of(p.sa, p.spa, p.a_square, srow, first + step), a_at, p.a_square);
-    sb_next = load_scales<TN>(scales_of(p.sb, p.spb, p.b_square, scol, first + step), b_at, p.b_square);
+    for (int i = 0; i < kLoads; ++i) load_unit(rb, st + SIDE * 8 + (i * kWaves + wave) * 64, off_b[i], k);
+  };
+  // of the wave's rows
+  const long srow = m0 + wm * 16 * TM, scol = n0 + wn * 16 * TN, start_a = p.a_square ? srow / kBlock8 : srow, start_b = p.b_square ? scol / kBlock8 : scol;
+  const int left_a = uniform((int)max(0L, min(p.spa - start_a, 16L * TM))), left_b = uniform((int)max(0L, min(p.spb - start_b, 16L * TN)));
+  struct Scales {
+    FourScales a[TM / 4], b;
+  };
+  auto scales = [&](int step) {
+    const long block = min(first + step, p.nb - 1);
+    Scales s;
+#pragma unroll
+    for (int i = 0; i < TM / 4; ++i) s.a[i] = load_scales(p.sa + block * p.spa + start_a, left_a, p.a_square, TM * (lane & 15) + 4 * i);
+    s.b = load_scales(p.sb + block * p.spb + start_b, left_b, p.b_square, TN * (lane & 15));
+    return s;
   };
 
-  v16f acc[TM][TN];
+  v4f acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  const int row = lane & 31, half = lane >> 5;
-  auto fragment = [&](const Word4* st, int at, int kk) {
-    const int u = 4 * kk + 2 * half;
-    const Word4 lo = st[(at + row) * 8 + (u ^ (row & 7))], hi = st[(at + row) * 8 + ((u + 1) ^ (row & 7))];
+    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  const int row = lane & 15, part = lane >> 4;
+  auto fragment = [&](const Word4* st, int at) {
+    const Word4 lo = st[(at + row) * 8 + (2 * part ^ (row & 7))], hi = st[(at + row) * 8 + ((2 * part + 1) ^ (row & 7))];
     return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   };
-  auto multiply = [&](const Word4* st) {
+  auto fragment_a = [&](const Word4* st, int i) { return fragment(st, (wm * TM + i) * 16); };
+  auto fragment_b = [&](const Word4* st, int j) { return fragment(st, SIDE + (wn * TN + j) * 16); };
+  v8i a[4], b[TN];  // a: row i of products in a[i % 4]
+  struct Wide {
+    v8bf q[4];
+  };
+  auto step = [&](Word4* st, const Word4* other, int t, const Scales& s, Scales& s_next) {
+    uint32_t sa[TM / 4];
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      if (BM == 256) __builtin_amdgcn_sched_barrier(0);  // fragments of both halves are more than the registers hold
-      v8i a[TM], b[TN];
+    for (int i = 0; i < TM / 4; ++i) sa[i] = s.a[i].word();
+    const uint32_t sb = s.b.word();
+    s_next = scales(t + 1);
+    Wide wb[WIDE ? TN : 1];
+    if constexpr (WIDE) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) a[i] = fragment(st, wm * 32 * TM + 32 * i, kk);
+      for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) b[j] = fragment(st, BM + wn * 32 * TN + 32 * j, kk);
+        for (int q = 0; q < 4; ++q) wb[j].q[q] = widen8<FB>(b[j][2 * q], b[j][2 * q + 1], code_scale(sb >> 8 * j & 255));
+    }
+    auto widen_a = [&](int i) {
+      Wide w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w.q[q] = widen8<FA>(a[i % 4][2 * q], a[i % 4][2 * q + 1], code_scale(sa[i / 4] >> 8 * (i % 4) & 255));
+      return w;
+    };
+    auto one = [&](auto i, auto j, const Wide& wa) {
+      constexpr int I = decltype(i)::value, J = decltype(j)::value;
       if constexpr (WIDE) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {  // any eight of a lane's codes: both operands take the same
-          v8bf wa[TM], wb[TN];
-#pragma unroll
-          for (int i = 0; i < TM; ++i) wa[i] = widen8<FA>(a[i][2 * q], a[i][2 * q + 1], code_scale(sa >> 8 * i & 255));
-#pragma unroll
-          for (int j = 0; j < TN; ++j) wb[j] = widen8<FB>(b[j][2 * q], b[j][2 * q + 1], code_scale(sb >> 8 * j & 255));
-#pragma unroll
-          for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
-        }
-        continue;
+        for (int q = 0; q < 4; ++q)  // any eight of a lane's codes: both operands take the same
+          acc[I][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa.q[q], wb[J].q[q], acc[I][J], 0, 0, 0);
+      } else {
+        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[I % 4], b[J], acc[I][J], FA, FB, I % 4, (int)sa[I / 4], J, (int)sb);
       }
-#define AX_TILE(I, J)                 \
-  if constexpr (I < TM && J < TN)     \
-  acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[I], b[J], acc[I][J], FA, FB, I, (int)sa, J, (int)sb)
-#define AX_TILES(I) \
-  AX_TILE(I, 0);    \
-  AX_TILE(I, 1)
-      AX_TILES(0);
-      AX_TILES(1);
-      AX_TILES(2);
-      AX_TILES(3);
-#undef AX_TILES
-#undef AX_TILE
+    };
+    for_each_index([&](auto i) {
+      constexpr int I = decltype(i)::value;
+      a[(I + 2) % 4] = fragment_a(st, I + 2);
+      Wide wa;
+      if constexpr (WIDE) wa = widen_a(I);
+      for_each_index([&](auto j) { one(i, j, wa); }, kAcross);
+    }, std::make_integer_sequence<int, TM - 2>());
+    if constexpr (!WIDE) {
+#pragma unroll
+      for (int i = 0; i < TM - 2; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);
+      }
     }
+    stage_barrier();
+    load(st, t + 2);
+    Wide w0, w1;
+    if constexpr (WIDE) w0 = widen_a(TM - 2), w1 = widen_a(TM - 1);
+    a[0] = fragment_a(other, 0);
+    a[1] = fragment_a(other, 1);
+    for_each_index([&](auto j) {
+      one(std::integral_constant<int, TM - 2>(), j, w0);
+      one(std::integral_constant<int, TM - 1>(), j, w1);
+      b[decltype(j)::value] = fragment_b(other, decltype(j)::value);
+    }, kAcross);
+    if constexpr (!WIDE) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
+  Scales s0, s1;
   load(stage0, 0);
-  for (int t = 0; t < steps; t += 2) {
-    stage_barrier();
-    sa = sa_next;
-    sb = sb_next;
-    if (t + 1 < steps) load(stage1, t + 1);
-    multiply(stage0);
-    if (t + 1 >= steps) break;
-    stage_barrier();
-    sa = sa_next;
-    sb = sb_next;
-    if (t + 2 < steps) load(stage0, t + 2);
-    multiply(stage1);
+  s0 = scales(0);
+  stage_barrier();
+  load(stage1, 1);
+  a[0] = fragment_a(stage0, 0);
+  a[1] = fragment_a(stage0, 1);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) b[j] = fragment_b(stage0, j);
+  int t = 0;
+  for (; t + 1 < steps; t += 2) {  // one way out: with two the accumulators take twice the registers
+    step(stage0, stage1, t, s0, s1);
+    step(stage1, stage0, t + 1, s1, s0);
   }
+  if (t < steps) step(stage0, stage1, t, s0, s1);
+  __builtin_amdgcn_s_waitcnt(0x0070);  // nothing is on its way to LDS when the workgroup ends
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const long y = m0 + wm * 32 * TM + TM * (8 * (r / 4) + 4 * half + r % 4) + i;
+    for (int r = 0; r < 4; ++r) {
+      const long y = m0 + wm * 16 * TM + TM * (4 * part + r) + i;
       float v[TN];
 #pragma unroll
       for (int j = 0; j < TN; ++j) v[j] = acc[i][j][r];
-      if (y < p.m) store_results<TN>(p, slice, y, n0 + wn * 32 * TN + TN * row, v);
+      if (y < p.m) store_results<TN>(p, slice, y, n0 + wn * 16 * TN + TN * row, v);
     }
 }
 
@@ -317,10 +376,14 @@ __global__ void __launch_bounds__(256) block8_zero_kernel(T* y, long m, long n, 
 template <int FA, int FB, bool WIDE>
 static int product_launch(const ProductArgs& a, const ProductPlan& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.slices));
-  if (p.kind == PRODUCT_256)
-    hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 256, 256, 2, 4>), grid, dim3(512), 0, st, a);
-  else if (p.kind == PRODUCT_128)
-    hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 128, 128, 2, 2>), grid, dim3(256), 0, st, a);
+  if constexpr (!WIDE)
+    if (p.kind == PRODUCT_256) {
+      hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 256>), grid, dim3(512), 0, st, a);
+      AX_LAUNCH_CHECK();
+      return ALEXNET_OK;
+    }
+  if (p.kind == PRODUCT_128)
+    hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 128>), grid, dim3(256), 0, st, a);
   else if (p.mt == 1)
     hipLaunchKernelGGL((block8_rows_kernel<FA, FB, WIDE, 1>), grid, dim3(64 * kRowWaves), 0, st, a);
   else if (p.mt == 2)
@@ -354,7 +417,7 @@ static int check_product(const char* who, long m, long n, long k, int type) {
   AX_REQUIRE(m >= 0 && m <= 1L << 28 && n >= 0 && n <= 1L << 28 && k >= 0 && k <= 1L << 22 && m * n <= 1L << 32 &&
                  blocks_sizes_ok(m, k) && blocks_sizes_ok(n, k),
              ALEXNET_ESHAPE, "%s: bad sizes, %ld by %ld over %ld (at most 2^28 rows of an operand, 2^22 columns, 2^32 results)", who, m, n, k);
-  AX_REQUIRE(m == 0 || n == 0 || product_plan(m, n, k).fits, ALEXNET_ESHAPE, "%s: %ld by %ld over %ld are more than one launch covers", who, m, n, k);
+  AX_REQUIRE(m == 0 || n == 0 || product_plan(m, n, k, type == ALEXNET_TYPE_FP32).fits, ALEXNET_ESHAPE, "%s: %ld by %ld over %ld are more than one launch covers", who, m, n, k);
   return ALEXNET_OK;
 }
 
@@ -367,7 +430,7 @@ extern "C" {
 int alexnet_block8_product_query(int64_t m, int64_t n, int64_t k, int32_t type, size_t* workspace_bytes) {
   AX_TRY(check_product("alexnet_block8_product_query", m, n, k, type));
   AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_block8_product_query: null argument");
-  *workspace_bytes = m && n ? product_plan(m, n, k).ws : 0;
+  *workspace_bytes = m && n ? product_plan(m, n, k, type == ALEXNET_TYPE_FP32).ws : 0;
   return ALEXNET_OK;
 }
 
@@ -386,7 +449,7 @@ int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* 
                                        : product_zero<_Float16>(d_y, m, n, ld_y, st);
   AX_TRY(check_blocks(a, "a", who));
   AX_TRY(check_blocks(b, "b", who));
-  const ProductPlan p = product_plan(m, n, k);
+  const ProductPlan p = product_plan(m, n, k, type == ALEXNET_TYPE_FP32);
   AX_TRY(check_scratch(who, d_workspace, workspace_bytes, p.ws));
   const long size = (long)type_size(type);
   AX_TRY(check_apart(who,

@@ -17,7 +17,7 @@ struct ProductPlan {
   bool fits;          // a launch covers it
 };
 
-inline ProductPlan product_plan(long m, long n, long k) {
+inline ProductPlan product_plan(long m, long n, long k, bool wide) {
   ProductPlan p = {};
   const long nb = std::max(1L, (k + 127) / 128);  // no columns: nothing is launched
   auto tiles = [](long size, long tile) { return (size + tile - 1) / tile; };
@@ -31,7 +31,7 @@ inline ProductPlan product_plan(long m, long n, long k) {
     p.tiles_n = (int)tiles(n, 16);
     grid = (long)p.tiles_m * p.tiles_n;
   } else {
-    const bool large = tiles(m, 256) * tiles(n, 256) >= 256;
+    const bool large = !wide && tiles(m, 256) * tiles(n, 256) >= 256;
     const long side = large ? 256 : 128;
     p.kind = large ? PRODUCT_256 : PRODUCT_128;
     p.tiles_m = (int)tiles(m, side);
