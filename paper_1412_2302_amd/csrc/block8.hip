@@ -27,9 +27,23 @@ __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
   const int t = threadIdx.x, tr = t >> 4, tc = t & 15, wave = t >> 6;
   const long rb = blockIdx.x / a.across, cb = blockIdx.x - rb * a.across;
   const long row0 = rb * kBlock8 + 8 * tr, col0 = cb * kBlock8 + 8 * tc;
+  // all eight loads on their way at once: rows past the end repeat the last one, and are zeros afterwards
+  Eight<T> raw[8];
+  if (col0 + 8 <= a.cols) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i].r = Pack<T, 8>::load((const T*)a.x + min(row0 + i, a.rows - 1) * a.ld + col0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i].load((const T*)a.x + min(row0 + i, a.rows - 1) * a.ld + col0, a.cols - col0);
+  }
   float v[8][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load8((const T*)a.x + (row0 + i) * a.ld + col0, row0 + i < a.rows ? a.cols - col0 : 0, v[i]);
+  for (int i = 0; i < 8; ++i) {
+    raw[i].widen(v[i]);
+    if (row0 + i >= a.rows)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+  }
 
   uint32_t of_row[8], of_col[8];
 #pragma unroll

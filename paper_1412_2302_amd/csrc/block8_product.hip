@@ -92,15 +92,15 @@ __device__ __forceinline__ v8bf widen8(int lo, int hi, float scale) {
 }
 
 // ---- tiles ------------------------------------------------------------------------
-__device__ __forceinline__ void stage_barrier() {
+// every LDS read of this wave is done; then the workgroup meets
+__device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
-
 __device__ __forceinline__ void load_unit(const Rsrc& r, Word4* to, int off, int from) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, off, from, 0, 0);
 }
@@ -135,6 +135,7 @@ template <int FA, int FB, bool WIDE, int SIDE>
 __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel(ProductArgs p) {
   constexpr int kWaves = SIDE / 32, TM = SIDE / 32, TN = 4, kLoads = 4;  // tiles of a wave; loads of a lane, operand and step
   constexpr auto kAcross = std::make_integer_sequence<int, TN>();
+  constexpr int kTail = TM / 2, kAhead = (TM - 2 + TM - kTail - 1) / (TM - kTail);  // rows of products behind the meeting; fragments read in a row before it
   __shared__ __attribute__((aligned(16))) Word4 stage0[2 * SIDE * 8];
   __shared__ __attribute__((aligned(16))) Word4 stage1[2 * SIDE * 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -143,7 +144,9 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
   const uint32_t total = gridDim.x, L = blockIdx.x, q8 = total >> 3, r8 = total & 7, xcd = L & 7;
   const int tile = (int)(xcd * q8 + min(xcd, r8) + (L >> 3));
   const int slice = uniform(tile / (p.tiles_m * p.tiles_n)), in_slice = tile - slice * (p.tiles_m * p.tiles_n);
-  const int tm = uniform(in_slice / p.tiles_n), tn = in_slice - tm * p.tiles_n;
+  // eight rows of tiles go across together: what the compute units of a die work on at a time shares most of its operands
+  const int band = uniform(in_slice / (8 * p.tiles_n)), high = min(8, p.tiles_m - 8 * band), in_band = in_slice - band * 8 * p.tiles_n;
+  const int tn = uniform(in_band / high), tm = 8 * band + in_band - tn * high;
   const long m0 = (long)tm * SIDE, n0 = (long)tn * SIDE;
   const int first = slice * p.steps, steps = min(p.steps, p.nb - first);
 
@@ -151,24 +154,25 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
   const uint8_t *const pa = p.a + m0 * p.pitch, *const pb = p.b + n0 * p.pitch;
   const int rows_a = uniform((int)min((long)SIDE, p.m - m0)), rows_b = uniform((int)min((long)SIDE, p.n - n0));
   const int bytes_a = rows_a * (int)p.pitch, bytes_b = rows_b * (int)p.pitch;
-  int off_a[kLoads], off_b[kLoads];
-  auto offset = [&](int i, int deal) {
-    const int at = (i * kWaves + wave) * 8 + (lane >> 3);  // row of the stage
-    const int row = at / (16 * deal) * (16 * deal) + deal * (at & 15) + at / 16 % deal;
-    return row * (int)p.pitch + 16 * ((lane & 7) ^ (lane >> 3));
-  };
+  // Load i of a lane brings 16 bytes of row (i * kWaves + wave) * 8 + lane / 8 of a stage.  The matrix's row is that of load 0 and a number
+  // of rows that is the same for all lanes.
+  const int at0 = wave * 8 + (lane >> 3), unit = 16 * ((lane & 7) ^ (lane >> 3));
+  auto dealt = [](int at, int deal) { return at / (16 * deal) * (16 * deal) + deal * (at & 15) + at / 16 % deal; };
+  int off_a = dealt(at0, TM) * (int)p.pitch + unit, off_b = dealt(at0, TN) * (int)p.pitch + unit;
+  int more_a[kLoads], more_b[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    off_a[i] = offset(i, TM);
-    off_b[i] = offset(i, TN);
+    more_a[i] = uniform((dealt((i * kWaves + wave) * 8, TM) - dealt(wave * 8, TM)) * (int)p.pitch);
+    more_b[i] = uniform((dealt((i * kWaves + wave) * 8, TN) - dealt(wave * 8, TN)) * (int)p.pitch);
   }
   auto load = [&](Word4* st, int step) {
     const int k = uniform((first + step) * kBlock8);
+    asm volatile("" : "+v"(off_a), "+v"(off_b));  // the sums below are made again each time: eight registers less
     const Rsrc ra = rsrc_of(pa, uniform(step < steps ? bytes_a : 0)), rb = rsrc_of(pb, uniform(step < steps ? bytes_b : 0));
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_unit(ra, st + (i * kWaves + wave) * 64, off_a[i], k);
+    for (int i = 0; i < kLoads; ++i) load_unit(ra, st + (i * kWaves + wave) * 64, off_a + more_a[i], k);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_unit(rb, st + SIDE * 8 + (i * kWaves + wave) * 64, off_b[i], k);
+    for (int i = 0; i < kLoads; ++i) load_unit(rb, st + SIDE * 8 + (i * kWaves + wave) * 64, off_b + more_b[i], k);
   };
   // of the wave's rows
   const long srow = m0 + wm * 16 * TM, scol = n0 + wn * 16 * TN, start_a = p.a_square ? srow / kBlock8 : srow, start_b = p.b_square ? scol / kBlock8 : scol;
@@ -185,28 +189,40 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
     return s;
   };
 
+  // Loads arrive in the order that they were sent in, and a step's scales are sent behind its codes: where the scales are used the
+  // compiler waits for both.
+  auto arrived = [](const Scales& s) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < TM / 4; ++i) asm volatile("" ::"v"(s.a[i].rows), "v"(s.a[i].one));
+    asm volatile("" ::"v"(s.b.rows), "v"(s.b.one) : "memory");
+  };
+
   v4f acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  // A lane's 32 codes of a row are units `part` and part + 4, for both operands; with two neighbouring ones the sixteen lanes that
+  // LDS serves at a time meet in its banks (8 clocks a read instead of 4).
   const int row = lane & 15, part = lane >> 4;
   auto fragment = [&](const Word4* st, int at) {
-    const Word4 lo = st[(at + row) * 8 + (2 * part ^ (row & 7))], hi = st[(at + row) * 8 + ((2 * part + 1) ^ (row & 7))];
+    const Word4 lo = st[(at + row) * 8 + (part ^ (row & 7))], hi = st[(at + row) * 8 + (part ^ 4 ^ (row & 7))];
     return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   };
   auto fragment_a = [&](const Word4* st, int i) { return fragment(st, (wm * TM + i) * 16); };
   auto fragment_b = [&](const Word4* st, int j) { return fragment(st, SIDE + (wn * TN + j) * 16); };
-  v8i a[4], b[TN];  // a: row i of products in a[i % 4]
+  v8i a[TM], b[TN];
   struct Wide {
     v8bf q[4];
   };
-  auto step = [&](Word4* st, const Word4* other, int t, const Scales& s, Scales& s_next) {
+  // step t, in `st`, with its scales; the next stage, and where the scales of its step go
+  auto step = [&](Word4* st, int t, const Scales& s, const Word4* other, Scales& s_other) {
     uint32_t sa[TM / 4];
 #pragma unroll
     for (int i = 0; i < TM / 4; ++i) sa[i] = s.a[i].word();
     const uint32_t sb = s.b.word();
-    s_next = scales(t + 1);
+    s_other = scales(t + 1);
     Wide wb[WIDE ? TN : 1];
     if constexpr (WIDE) {
 #pragma unroll
@@ -217,7 +233,7 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
     auto widen_a = [&](int i) {
       Wide w;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w.q[q] = widen8<FA>(a[i % 4][2 * q], a[i % 4][2 * q + 1], code_scale(sa[i / 4] >> 8 * (i % 4) & 255));
+      for (int q = 0; q < 4; ++q) w.q[q] = widen8<FA>(a[i][2 * q], a[i][2 * q + 1], code_scale(sa[i / 4] >> 8 * (i % 4) & 255));
       return w;
     };
     auto one = [&](auto i, auto j, const Wide& wa) {
@@ -227,39 +243,50 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
         for (int q = 0; q < 4; ++q)  // any eight of a lane's codes: both operands take the same
           acc[I][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa.q[q], wb[J].q[q], acc[I][J], 0, 0, 0);
       } else {
-        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[I % 4], b[J], acc[I][J], FA, FB, I % 4, (int)sa[I / 4], J, (int)sb);
+        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[I], b[J], acc[I][J], FA, FB, I % 4, (int)sa[I / 4], J, (int)sb);
       }
+    };
+    auto row_of = [&](auto i) {
+      Wide wa;
+      if constexpr (WIDE) wa = widen_a(decltype(i)::value);
+      for_each_index([&](auto j) { one(i, j, wa); }, kAcross);
     };
     for_each_index([&](auto i) {
       constexpr int I = decltype(i)::value;
-      a[(I + 2) % 4] = fragment_a(st, I + 2);
-      Wide wa;
-      if constexpr (WIDE) wa = widen_a(I);
-      for_each_index([&](auto j) { one(i, j, wa); }, kAcross);
-    }, std::make_integer_sequence<int, TM - 2>());
+#pragma unroll
+      for (int k = 2 + I * kAhead; k < min(TM, 2 + (I + 1) * kAhead); ++k) a[k] = fragment_a(st, k);
+      row_of(i);
+    }, std::make_integer_sequence<int, TM - kTail>());
     if constexpr (!WIDE) {
 #pragma unroll
-      for (int i = 0; i < TM - 2; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      for (int i = 0; i < TM - kTail; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);
       }
     }
-    stage_barrier();
+    arrived(s_other);
+    meet();
     load(st, t + 2);
-    Wide w0, w1;
-    if constexpr (WIDE) w0 = widen_a(TM - 2), w1 = widen_a(TM - 1);
+    Wide wa[WIDE ? kTail : 1];
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < kTail; ++i) wa[i] = widen_a(TM - kTail + i);
+    }
     a[0] = fragment_a(other, 0);
     a[1] = fragment_a(other, 1);
     for_each_index([&](auto j) {
-      one(std::integral_constant<int, TM - 2>(), j, w0);
-      one(std::integral_constant<int, TM - 1>(), j, w1);
+      for_each_index([&](auto i) { one(std::integral_constant<int, TM - kTail + decltype(i)::value>(), j, wa[WIDE ? decltype(i)::value : 0]); },
+                     std::make_integer_sequence<int, kTail>());
       b[decltype(j)::value] = fragment_b(other, decltype(j)::value);
     }, kAcross);
     if constexpr (!WIDE) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kTail / 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kTail / 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       }
     }
@@ -268,7 +295,8 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
   Scales s0, s1;
   load(stage0, 0);
   s0 = scales(0);
-  stage_barrier();
+  arrived(s0);
+  meet();
   load(stage1, 1);
   a[0] = fragment_a(stage0, 0);
   a[1] = fragment_a(stage0, 1);
@@ -276,10 +304,10 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
   for (int j = 0; j < TN; ++j) b[j] = fragment_b(stage0, j);
   int t = 0;
   for (; t + 1 < steps; t += 2) {  // one way out: with two the accumulators take twice the registers
-    step(stage0, stage1, t, s0, s1);
-    step(stage1, stage0, t + 1, s1, s0);
+    step(stage0, t, s0, stage1, s1);
+    step(stage1, t + 1, s1, stage0, s0);
   }
-  if (t < steps) step(stage0, stage1, t, s0, s1);
+  if (t < steps) step(stage0, t, s0, stage1, s1);
   __builtin_amdgcn_s_waitcnt(0x0070);  // nothing is on its way to LDS when the workgroup ends
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -294,44 +322,49 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
 }
 
 // ---- few rows ---------------------------------------------------------------------
-// What counts is how many loads of b are on their way: a workgroup has 16 of its rows and all of a's, its eight waves a block of the sum in turn,
-// both operands straight to registers; the waves' sums meet in LDS.
+// Few rows, or few products: what counts is to have many waves and no way through LDS.  A workgroup has 16 of b's rows and 16 MT of a's,
+// its eight waves the blocks of the sum in turn, both operands straight to registers; the waves' sums meet in LDS.  As in the
+// tiles a lane's 32 codes are two units 64 bytes apart, so that a load's lanes cover whole half lines.  Four blocks sent for at a time
+// instead of one: 1 x 9216 x 4096 7.6 -> 9.6 us, 64 x 4096 x 4096 12.2 -> 12.4.
 constexpr int kRowWaves = 8;
 template <int FA, int FB, bool WIDE, int MT>
 __global__ void __launch_bounds__(64 * kRowWaves) block8_rows_kernel(ProductArgs p) {
   __shared__ v4f sums[kRowWaves][MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int tn = blockIdx.x / p.tiles_m, tm = blockIdx.x - tn * p.tiles_m;
   const long m0 = (long)tm * 16 * MT, n0 = (long)tn * 16;
   const int row = lane & 15, part = lane >> 4;
   const long b_row = min(n0 + row, p.n - 1);
-  const uint8_t* const b = p.b + b_row * p.pitch + 32 * part;
+  const uint8_t* const b = p.b + b_row * p.pitch + 16 * part;
   const uint8_t* const sb = p.sb + (p.b_square ? b_row / kBlock8 : b_row);
   const uint8_t *a[MT], *sa[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const long r = min(m0 + 16 * i + row, p.m - 1);
-    a[i] = p.a + r * p.pitch + 32 * part;
+    a[i] = p.a + r * p.pitch + 16 * part;
     sa[i] = p.sa + (p.a_square ? r / kBlock8 : r);
   }
   v4f acc[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = v4f{0.f, 0.f, 0.f, 0.f};
-  auto fragment = [](const uint8_t* q) { return *reinterpret_cast<const v8i*>(q); };
-  for (int kb = wave; kb < p.nb; kb += kRowWaves) {
-    const v8i fb = fragment(b + (long)kb * kBlock8);
-    const int s = sb[kb * p.spb];
+  auto fragment = [](const uint8_t* q) {
+    const Word4 lo = *reinterpret_cast<const Word4*>(q), hi = *reinterpret_cast<const Word4*>(q + 64);
+    return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+  for (long kb = wave; kb < p.nb; kb += kRowWaves) {
+    const v8i fb = fragment(b + kb * kBlock8);
+    const int t = sb[kb * p.spb];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const v8i fa = fragment(a[i] + (long)kb * kBlock8);
-      const int t = sa[i][kb * p.spa];
+      const v8i fa = fragment(a[i] + kb * kBlock8);
+      const int s = sa[i][kb * p.spa];
       if constexpr (WIDE) {
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FA>(fa[2 * q], fa[2 * q + 1], code_scale(t)),
-                                                          widen8<FB>(fb[2 * q], fb[2 * q + 1], code_scale(s)), acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FA>(fa[2 * q], fa[2 * q + 1], code_scale(s)),
+                                                          widen8<FB>(fb[2 * q], fb[2 * q + 1], code_scale(t)), acc[i], 0, 0, 0);
       } else {
-        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[i], FA, FB, 0, t, 0, s);
+        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[i], FA, FB, 0, s, 0, t);
       }
     }
   }
@@ -350,22 +383,42 @@ __global__ void __launch_bounds__(64 * kRowWaves) block8_rows_kernel(ProductArgs
   }
 }
 
-// y = the sum of the slices
-template <typename T>
+// y = the sum of the slices, four values a thread and TEAM threads to them: a thread adds up every TEAM-th slice, all of them on their way at
+// a time, and few values of many slices want larger teams
+template <typename T, int TEAM>
 __global__ void __launch_bounds__(256) block8_sum_kernel(const float* __restrict__ part, long slab, int slices, long m, long n, T* y, long ld) {
-  const long vecs = (n + 7) / 8, i = (long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= m * vecs) return;
-  const long row = i / vecs, col = (i - row * vecs) * 8;
+  constexpr int kQuads = 256 / TEAM;
+  __shared__ v4f share[TEAM > 1 ? 256 : 1];
+  const long vecs = (n + 3) / 4, i = (long)blockIdx.x * kQuads + threadIdx.x % kQuads, row = i / vecs, col = (i - row * vecs) * 4;
+  const int member = threadIdx.x / kQuads;
+  const bool on = i < m * vecs;
   const float* const q = part + row * n + col;
-  float v[8];
-  load8(q, n - col, v);
-  for (int s = 1; s < slices; ++s) {
-    float w[8];
-    load8(q + s * slab, n - col, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  const int has = (int)min(n - col, 4L);
+  v4f v = {0.f, 0.f, 0.f, 0.f};
+  if (on && has == 4) {
+#pragma unroll 8
+    for (int s = member; s < slices; s += TEAM) v += Pack<float, 4>::load(q + s * slab);
+  } else if (on) {
+    for (int e = 0; e < has; ++e)
+      for (int s = member; s < slices; s += TEAM) v[e] += q[s * slab + e];
   }
-  store8(y + row * ld + col, n - col, v);
+  if constexpr (TEAM > 1) {
+    share[threadIdx.x] = v;
+    __syncthreads();
+    if (member) return;
+#pragma unroll
+    for (int k = 1; k < TEAM; ++k) v += share[k * kQuads + threadIdx.x];
+  }
+  if (!on) return;
+  T* const out = y + row * ld + col;
+  const float f[4] = {v[0], v[1], v[2], v[3]};
+  if (has == 4) {
+    Pack<T, 4>::store(out, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < has) out[e] = (T)f[e];
+  }
 }
 
 template <typename T>
@@ -397,13 +450,17 @@ template <int FA, int FB>
 static int product_launch_type(const ProductArgs& a, const ProductPlan& p, hipStream_t st) {
   return a.type == ALEXNET_TYPE_FP32 ? product_launch<FA, FB, true>(a, p, st) : product_launch<FA, FB, false>(a, p, st);
 }
-template <typename T>
-static int product_sum(const ProductArgs& a, hipStream_t st) {
+template <typename T, int TEAM>
+static int product_sum_team(const ProductArgs& a, hipStream_t st) {
   KernelScope ks("block8_product_sum", 0, (double)a.m * a.n * (4.0 * a.slices + sizeof(T)), st);
-  hipLaunchKernelGGL(block8_sum_kernel<T>, dim3((unsigned)((a.m * ((a.n + 7) / 8) + 255) / 256)), dim3(256), 0, st, a.part, a.slab, a.slices, a.m, a.n,
-                     (T*)a.y, a.ld);
+  const long quads = a.m * ((a.n + 3) / 4), per = 256 / TEAM;
+  hipLaunchKernelGGL((block8_sum_kernel<T, TEAM>), dim3((unsigned)((quads + per - 1) / per)), dim3(256), 0, st, a.part, a.slab, a.slices, a.m, a.n, (T*)a.y, a.ld);
   AX_LAUNCH_CHECK();
   return ALEXNET_OK;
+}
+template <typename T>
+static int product_sum(const ProductArgs& a, hipStream_t st) {
+  return a.m * a.n < 1 << 18 && a.slices > 8 ? product_sum_team<T, 8>(a, st) : product_sum_team<T, 1>(a, st);
 }
 template <typename T>
 static int product_zero(void* y, long m, long n, long ld, hipStream_t st) {

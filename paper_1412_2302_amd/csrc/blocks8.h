@@ -35,30 +35,32 @@ inline Region blocks_scales(const alexnet_blocks8_t* b, long rows, long cols) {
 typedef uint32_t Word2 __attribute__((ext_vector_type(2)));
 typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
 
-// Eight neighbouring values of a row, of which `has` (any number) lie inside it; zeros in the place of the others.
+// Eight neighbouring values of a row, of which `has` (any number) lie inside it; zeros in the place of the others.  Raw as they come: a caller
+// that wants several loads on their way at a time widens them afterwards.
+template <typename T>
+struct Eight {
+  typedef typename Pack<T, 8>::Raw Raw;
+  Raw r;
+  __device__ __forceinline__ void load(const T* p, long has) {
+    if (has >= 8) {
+      r = Pack<T, 8>::load(p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = i < has ? p[i] : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ void widen(float* v) const { Pack<T, 8>::widen(r, v); }
+};
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, long has, float* v) {
-  if (has >= 8) {
-    if constexpr (sizeof(T) == 2) {
-      Pack<T, 8>::widen(Pack<T, 8>::load(p), v);
-    } else {
-      Pack<T, 4>::widen(Pack<T, 4>::load(p), v);
-      Pack<T, 4>::widen(Pack<T, 4>::load(p + 4), v + 4);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < has ? (float)p[i] : 0.f;
-  }
+  Eight<T> e;
+  e.load(p, has);
+  e.widen(v);
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, long has, const float* v) {
   if (has >= 8) {
-    if constexpr (sizeof(T) == 2) {
-      Pack<T, 8>::store(p, v);
-    } else {
-      Pack<T, 4>::store(p, v);
-      Pack<T, 4>::store(p + 4, v + 4);
-    }
+    Pack<T, 8>::store(p, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
