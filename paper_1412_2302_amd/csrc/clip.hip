@@ -55,6 +55,30 @@ __device__ __forceinline__ void over_chunks(const ClipArgs& a, int c0, int c1, b
   }
 }
 
+// f(values, of which so many are the tensor's, place) of a thread's eights of a chunk: of a whole one all loads are on their way at once
+template <typename T, typename F>
+__device__ __forceinline__ void over_eights(const T* in, long n, F f) {
+  constexpr int kEights = kClipChunk / 2048;
+  const int at = 8 * threadIdx.x;
+  if (n == kClipChunk) {
+    Eight<T> raw[kEights];
+#pragma unroll
+    for (int k = 0; k < kEights; ++k) raw[k].r = Pack<T, 8>::load(in + at + 2048 * k);
+#pragma unroll
+    for (int k = 0; k < kEights; ++k) {
+      float v[8];
+      raw[k].widen(v);
+      f(v, 8, at + 2048 * k);
+    }
+  } else {
+    for (int i = at; i < n; i += 2048) {
+      float v[8];
+      load8(in + i, n - i, v);
+      f(v, (int)min(n - i, 8L), i);
+    }
+  }
+}
+
 __device__ __forceinline__ double add_lanes(double v) {
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
@@ -73,12 +97,10 @@ __global__ void __launch_bounds__(256) clip_squares_kernel(ClipArgs a) {
   const int c0 = (long)a.chunks * blockIdx.x / gridDim.x, c1 = (long)a.chunks * (blockIdx.x + 1) / gridDim.x;
   double sum = 0.0;
   over_chunks(a, c0, c1, false, [&](const auto* in, auto*, long n) {
-    for (long i = 8 * threadIdx.x; i < n; i += 2048) {
-      float v[8];
-      load8(in + i, n - i, v);
+    over_eights(in, n, [&](const float* v, int, int) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)v[e], (double)v[e], sum);
-    }
+    });
   });
   sum = add_threads(sum, cross);
   if (threadIdx.x == 0) a.part[a.first_part + blockIdx.x] = sum;
@@ -107,13 +129,11 @@ __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a) {
   const int b = gridDim.x - 1 - blockIdx.x;
   const int c0 = (long)a.chunks * b / gridDim.x, c1 = (long)a.chunks * (b + 1) / gridDim.x;
   over_chunks(a, c0, c1, true, [&](const auto* in, auto* out, long n) {
-    for (long i = 8 * threadIdx.x; i < n; i += 2048) {
-      float v[8];
-      load8(in + i, n - i, v);
+    over_eights(in, n, [&](float* v, int has, int i) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (float)((double)v[e] * factor);
-      store8(out + i, n - i, v);
-    }
+      store8(out + i, has, v);
+    });
   });
 }
 

@@ -22,22 +22,21 @@ struct RmsArgs {
   float eps;
 };
 
-// What fits in registers: vectors of a row <= TEAM * NV
+// What fits in registers: vectors of a row <= TEAM * NV.  The backward pass holds a row's values three times over (with gamma and its
+// gradient), so its teams are larger: 4096 x 9216 bf16 104 us by 256 lanes of eight vectors, 67 by 512 of three.
 struct RmsPlan {
   int team, nv;  // nv 0: rows are read twice
 };
 inline RmsPlan rms_plan(long cols, bool backward) {
   const long v = (cols + 7) / 8;
-  return v <= 16     ? RmsPlan{16, 1}
-         : v <= 32   ? RmsPlan{16, 2}
-         : v <= 48   ? RmsPlan{16, 3}
-         : v <= 64   ? RmsPlan{64, 1}
-         : v <= 128  ? RmsPlan{64, 2}
-         : v <= 256  ? RmsPlan{64, 4}
+  if (v <= 48) return RmsPlan{16, v <= 16 ? 1 : v <= 32 ? 2 : 3};
+  if (v <= 128) return RmsPlan{64, v <= 64 ? 1 : 2};
+  if (backward)
+    return v <= 256 ? RmsPlan{256, 1} : v <= 512 ? RmsPlan{256, 2} : v <= 1024 ? RmsPlan{512, 2} : v <= 1536 ? RmsPlan{512, 3} : v <= 2048 ? RmsPlan{512, 4} : RmsPlan{1024, 0};
+  return v <= 256    ? RmsPlan{64, 4}
          : v <= 512  ? RmsPlan{256, 2}
          : v <= 1024 ? RmsPlan{256, 4}
          : v <= 2048 ? RmsPlan{256, 8}
-         : backward  ? RmsPlan{1024, 0}  // three arrays of a row's values are more than 1024 threads' registers hold
          : v <= 4096 ? RmsPlan{1024, 4}
          : v <= 8192 ? RmsPlan{1024, 8}
                      : RmsPlan{1024, 0};
@@ -70,8 +69,8 @@ __device__ __forceinline__ float team_sum(float v, float* cross) {
   return v;
 }
 
-// f with the plan's numbers as constants
-template <typename F>
+// f with a plan's numbers as constants
+template <bool BACKWARD, typename F>
 static int with_rms_plan(const RmsPlan& p, F f) {
 #define AX_PLAN(TEAM, NV) \
   if (p.team == TEAM && p.nv == NV) return f(std::integral_constant<int, TEAM>(), std::integral_constant<int, NV>())
@@ -80,12 +79,19 @@ static int with_rms_plan(const RmsPlan& p, F f) {
   AX_PLAN(16, 3);
   AX_PLAN(64, 1);
   AX_PLAN(64, 2);
-  AX_PLAN(64, 4);
   AX_PLAN(256, 2);
-  AX_PLAN(256, 4);
-  AX_PLAN(256, 8);
-  AX_PLAN(1024, 4);
-  AX_PLAN(1024, 8);
+  if constexpr (BACKWARD) {
+    AX_PLAN(256, 1);
+    AX_PLAN(512, 2);
+    AX_PLAN(512, 3);
+    AX_PLAN(512, 4);
+  } else {
+    AX_PLAN(64, 4);
+    AX_PLAN(256, 4);
+    AX_PLAN(256, 8);
+    AX_PLAN(1024, 4);
+    AX_PLAN(1024, 8);
+  }
   return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
 #undef AX_PLAN
 }

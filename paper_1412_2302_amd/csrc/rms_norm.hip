@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256) rms_norm_kernel(RmsAr
 
 template <typename T, int CODE>
 static int rms_forward(const RmsArgs& a, hipStream_t st) {
-  return with_rms_plan(rms_plan(8L * a.vecs, false), [&](auto team, auto nv) {
+  return with_rms_plan<false>(rms_plan(8L * a.vecs, false), [&](auto team, auto nv) {
     constexpr int kTeam = decltype(team)::value, kTeams = kTeam > 256 ? 1 : 256 / kTeam;
     hipLaunchKernelGGL((rms_norm_kernel<T, CODE, kTeam, decltype(nv)::value>), dim3((unsigned)((a.rows + kTeams - 1) / kTeams)),
                        dim3(kTeam > 256 ? kTeam : 256), 0, st, a);

@@ -33,18 +33,38 @@ __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256) rms_norm_bwd_kernel(R
   }
   const float scale = 1.f / (float)a.cols;
   int turn = 0;
-  for (long row = (long)blockIdx.x * kTeams + mine; row < a.rows; row += a.teams) {
-    const float rstd = a.rstd[row];
+  // The next row's loads are on their way while a row is worked on, where the registers hold both and leave room for other waves:
+  // 16384 x 4096 bf16 157 -> 104 us; float32 of two vectors and 16 bits of three gain nothing.
+  constexpr bool kAhead = NV * sizeof(T) <= 4;
+  struct Row {
+    Eight<T> s[NV], dy[NV], dsum[NV];
+    float rstd;
+  };
+  auto load = [&](Row& r, long row) {
+    r.rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = 8 * (t + i * TEAM), has = a.cols - col;
+      r.s[i].load((const T*)a.x + row * a.ld_x + col, has);
+      r.dy[i].load((const T*)a.dy + row * a.ld_dy + col, has);
+      if (a.dsum) r.dsum[i].load((const T*)a.dsum + row * a.ld_dsum + col, has);
+    }
+  };
+  Row now, next;
+  long row = (long)blockIdx.x * kTeams + mine;
+  if (kAhead && row < a.rows) load(now, row);
+  for (; row < a.rows; row += a.teams) {
+    if constexpr (!kAhead)
+      load(now, row);
+    else if (row + a.teams < a.rows)
+      load(next, row + a.teams);
+    const float rstd = now.rstd;
     float h[NV][8], g[NV][8];
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int col = 8 * (t + i * TEAM), has = a.cols - col;
-      load8((const T*)a.x + row * a.ld_x + col, has, h[i]);
-      load8((const T*)a.dy + row * a.ld_dy + col, has, g[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
+      now.s[i].widen(h[i]);
+      now.dy[i].widen(g[i]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         h[i][e] *= rstd;
@@ -52,6 +72,7 @@ __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256) rms_norm_bwd_kernel(R
         g[i][e] *= gamma[i][e];
         dot = __builtin_fmaf(g[i][e], h[i][e], dot);
       }
+    }
     dot = team_sum<TEAM>(dot, cross[turn]) * scale;
     turn ^= 1;
 #pragma unroll
@@ -61,11 +82,12 @@ __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256) rms_norm_bwd_kernel(R
       float d[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[e] = 0.f;
-      if (a.dsum) load8((const T*)a.dsum + row * a.ld_dsum + col, has, d);
+      if (a.dsum) now.dsum[i].widen(d);
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[e] = __builtin_fmaf(rstd, __builtin_fmaf(-h[i][e], dot, g[i][e]), d[e]);
       store8((T*)a.out + row * a.ld_out + col, has, d);
     }
+    if constexpr (kAhead) now = next;
   }
   if (!a.part) return;
 #pragma unroll
@@ -179,9 +201,9 @@ static int rms_backward(RmsArgs a, const RmsBwdPlan& b, void* ws, hipStream_t st
     AX_LAUNCH_CHECK();
     return ALEXNET_OK;
   }
-  return with_rms_plan(b.p, [&](auto team, auto nv) {
+  return with_rms_plan<true>(b.p, [&](auto team, auto nv) {
     constexpr int kTeam = decltype(team)::value, kNv = decltype(nv)::value;
-    if constexpr (kNv > 0 && kTeam * kNv <= 2048) {
+    if constexpr (kNv > 0) {
       hipLaunchKernelGGL((rms_norm_bwd_kernel<T, kTeam, kNv>), dim3((unsigned)b.grid), dim3(kTeam > 256 ? kTeam : 256), 0, st, a);
       AX_LAUNCH_CHECK();
     }
