@@ -119,6 +119,21 @@ __global__ void __launch_bounds__(256) clip_norm_kernel(ClipArgs a) {
   if (threadIdx.x == 0) *a.norm = (float)norm;
 }
 
+// A result that goes elsewhere passes the cache by, which keeps what of the gradients is in it (61 M float32 values: 146 -> 138 us).
+template <typename T>
+__device__ __forceinline__ void store_eight(const T* in, T* out, int has, const float* v) {
+  typedef typename Pack<T, 8>::Raw Raw;
+  typedef Raw Anywhere __attribute__((aligned(sizeof(T))));
+  if (in == out || has < 8) {
+    store8(out, has, v);
+    return;
+  }
+  Raw r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (T)v[e];  // nearest even
+  __builtin_nontemporal_store(r, reinterpret_cast<Anywhere*>(out));
+}
+
 __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a) {
   __shared__ double cross[4];
   const double norm = norm_of(a, cross);
@@ -132,7 +147,7 @@ __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a) {
     over_eights(in, n, [&](float* v, int has, int i) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (float)((double)v[e] * factor);
-      store8(out + i, has, v);
+      store_eight(in + i, out + i, has, v);
     });
   });
 }
