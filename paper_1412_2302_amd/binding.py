@@ -7,6 +7,7 @@ this module fails loudly when the library has not been built
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import os
@@ -1078,39 +1079,46 @@ def rms_norm_backward(s: torch.Tensor, dy: torch.Tensor, rstd: torch.Tensor, gam
 
 
 def _gradients(grads, what: str):
-    """Checked gradients, as (list, device, host tables of pointers, sizes and types)."""
+    """Checked gradients, as (list, their device's index, host tables of pointers, sizes and types).  Looked at by kind, not by
+    tensor: there may be many, and small."""
     grads = list(grads)
     for g in grads:
         if not isinstance(g, torch.Tensor):
             raise TypeError(f"{what}: expected torch.Tensors, got {type(g).__name__}")
-        if not g.is_cuda or g.dtype not in _TYPES or not g.is_contiguous() or g.device != grads[0].device:
-            raise ValueError(f"{what}: expected contiguous float32, bfloat16 or float16 tensors on one device, got {g.dtype} "
-                             f"{list(g.shape)} of strides {g.stride()} on {g.device}")
     if not grads:
         raise ValueError(f"{what}: no gradients")
-    n = len(grads)
-    return grads, (_vp * n)(*map(torch.Tensor.data_ptr, grads)), (_i64 * n)(*map(torch.Tensor.numel, grads)), (
-        _i32 * n)(*[_TYPES[g.dtype] for g in grads])
+    devices, types = list(map(torch.Tensor.get_device, grads)), [_TYPES.get(g.dtype, -1) for g in grads]
+    if devices.count(devices[0]) != len(grads) or devices[0] < 0 or -1 in types or not all(map(torch.Tensor.is_contiguous, grads)):
+        for g in grads:
+            if not g.is_cuda or g.dtype not in _TYPES or not g.is_contiguous() or g.device != grads[0].device:
+                raise ValueError(f"{what}: expected contiguous float32, bfloat16 or float16 tensors on one device, got {g.dtype} "
+                                 f"{list(g.shape)} of strides {g.stride()} on {g.device}")
+    return (grads, devices[0], array.array("Q", map(torch.Tensor.data_ptr, grads)), array.array("q", map(torch.Tensor.numel, grads)),
+            array.array("i", types))
+
+
+def _address(table) -> int:
+    return table.buffer_info()[0]
 
 
 def _clip_ws(sizes) -> int:
     ws = _sz()
-    _check(_lib.alexnet_clip_query(len(sizes), sizes, C.byref(ws)))
+    _check(_lib.alexnet_clip_query(len(sizes), _address(sizes), ws))
     return ws.value
 
 
 def gradient_norm(grads, stream=None) -> torch.Tensor:
     """The 2-norm over all values of all tensors (float32, bfloat16 or float16, mixed if wanted), as a float32 tensor of one element
     on their device."""
-    grads, pointers, sizes, types = _gradients(grads, "gradient_norm")
+    grads, index, pointers, sizes, types = _gradients(grads, "gradient_norm")
     first = grads[0]
     if not _here(first, stream):
         return _there(first, stream, grads, lambda: gradient_norm(grads))
     norm = torch.empty((), dtype=torch.float32, device=first.device)
     ws_bytes = _clip_ws(sizes)
     ws = _scratch(ws_bytes, first.device)
-    _check(_lib.alexnet_gradient_norm(len(grads), pointers, sizes, types, norm.data_ptr(), ws.data_ptr(), ws_bytes,
-                                      _raw_stream(first.get_device())))
+    _check(_lib.alexnet_gradient_norm(len(grads), _address(pointers), _address(sizes), _address(types), norm.data_ptr(), ws.data_ptr(),
+                                      ws_bytes, _raw_stream(index)))
     return norm
 
 
@@ -1119,11 +1127,11 @@ def clip_gradients(grads, max_norm: float, out=None, stream=None) -> torch.Tenso
     sizes and types that receive the result (each may be its own gradient); otherwise that happens in place.  Where the norm is an
     infinity or a NaN nothing is scaled."""
     what = "clip_gradients"
-    grads, pointers, sizes, types = _gradients(grads, what)
+    grads, index, pointers, sizes, types = _gradients(grads, what)
     results = None
     if out is not None:
-        out, results, out_sizes, out_types = _gradients(out, "clip_gradients: out")
-        if len(out) != len(grads) or out_sizes[:] != sizes[:] or out_types[:] != types[:] or out[0].device != grads[0].device:
+        out, out_index, results, out_sizes, out_types = _gradients(out, "clip_gradients: out")
+        if out_sizes != sizes or out_types != types or out_index != index:
             raise ValueError(f"{what}: out differs from the gradients in number, sizes, types or device")
     first = grads[0]
     if not _here(first, stream):
@@ -1131,6 +1139,6 @@ def clip_gradients(grads, max_norm: float, out=None, stream=None) -> torch.Tenso
     norm = torch.empty((), dtype=torch.float32, device=first.device)
     ws_bytes = _clip_ws(sizes)
     ws = _scratch(ws_bytes, first.device)
-    _check(_lib.alexnet_clip_gradients(len(grads), pointers, results, sizes, types, max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes,
-                                       _raw_stream(first.get_device())))
+    _check(_lib.alexnet_clip_gradients(len(grads), _address(pointers), None if results is None else _address(results), _address(sizes),
+                                       _address(types), max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes, _raw_stream(index)))
     return norm

@@ -474,7 +474,6 @@ static int check_product(const char* who, long m, long n, long k, int type) {
   AX_REQUIRE(m >= 0 && m <= 1L << 28 && n >= 0 && n <= 1L << 28 && k >= 0 && k <= 1L << 22 && m * n <= 1L << 32 &&
                  blocks_sizes_ok(m, k) && blocks_sizes_ok(n, k),
              ALEXNET_ESHAPE, "%s: bad sizes, %ld by %ld over %ld (at most 2^28 rows of an operand, 2^22 columns, 2^32 results)", who, m, n, k);
-  AX_REQUIRE(m == 0 || n == 0 || product_plan(m, n, k, type == ALEXNET_TYPE_FP32).fits, ALEXNET_ESHAPE, "%s: %ld by %ld over %ld are more than one launch covers", who, m, n, k);
   return ALEXNET_OK;
 }
 

@@ -14,11 +14,10 @@ struct ProductPlan {
   int tiles_m, tiles_n;
   int slices, steps;  // of the sum; blocks of 128 in a slice
   size_t slab, ws;    // floats of a slice's y; bytes of scratch
-  bool fits;          // a launch covers it
 };
 
 constexpr int kProductSlices = 64;
-constexpr long kProductGrid = 1L << 22;  // workgroups of a launch, of 512 threads at most
+constexpr long kProductGrid = 1L << 22;  // workgroups of a launch, of 512 threads at most; 2^32 results are at most 2^21 128-tiles and a few
 
 // What a model of the measured times makes cheapest, in microseconds.
 //   Rows: eight blocks take a compute unit by the rows that they read, not by their products; 64 x 4096 x 4096 12.2 (128-tiles in four slices 13.2), 129 x 1001 x 515 7.2 (14.0),
@@ -44,7 +43,6 @@ inline ProductPlan product_plan(long m, long n, long k, bool wide) {
     best.tiles_n = (int)tn;
     best.slices = (int)slices;
     best.steps = (int)tiles(nb, slices);
-    best.fits = true;
   };
   {
     const int mt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
