@@ -104,16 +104,14 @@ __device__ __forceinline__ void meet() {
 __device__ __forceinline__ void load_unit(const Rsrc& r, Word4* to, int off, int from) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, off, from, 0, 0);
 }
-// The scales of four neighbouring rows, a byte each, from s on, `left` bytes of which are a block's: of rows, the word at a lane's
-// `off`; of squares, one byte for all.  One of the two comes from an empty buffer, as zeros.  Put together only when they are used: until
-// then nothing waits for them.
+// The scales of four neighbouring rows, a byte each: of rows, the word at `off`; of squares, one byte for all.  One of the two buffers
+// is empty and gives zeros.  Put together only when they are used: until then nothing waits for them.
 struct FourScales {
   uint32_t rows, one;
   __device__ __forceinline__ uint32_t word() const { return rows | one * 0x01010101u; }
 };
-__device__ __forceinline__ FourScales load_scales(const uint8_t* s, int left, int square, int off) {
-  return FourScales{(uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc_of(s, square ? 0 : left), off, 0, 0),
-                    (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rsrc_of(s, square ? left : 0), 0, 0, 0)};
+__device__ __forceinline__ FourScales load_scales(const Rsrc& rows, const Rsrc& square, int off) {
+  return FourScales{(uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rows, off, 0, 0), (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(square, off, 0, 0)};
 }
 
 // f(0), f(1), ... with the numbers as constants
@@ -148,7 +146,7 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
   const int band = uniform(in_slice / (8 * p.tiles_n)), high = min(8, p.tiles_m - 8 * band), in_band = in_slice - band * 8 * p.tiles_n;
   const int tn = uniform(in_band / high), tm = 8 * band + in_band - tn * high;
   const long m0 = (long)tm * SIDE, n0 = (long)tn * SIDE;
-  const int first = slice * p.steps, steps = min(p.steps, p.nb - first);
+  const int first = uniform(slice * p.steps), steps = uniform(min(p.steps, p.nb - first));
 
   // rows past the end lie outside of the buffers and read as zeros
   const uint8_t *const pa = p.a + m0 * p.pitch, *const pb = p.b + n0 * p.pitch;
@@ -166,26 +164,34 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
     more_b[i] = uniform((dealt((i * kWaves + wave) * 8, TN) - dealt(wave * 8, TN)) * (int)p.pitch);
   }
   auto load = [&](Word4* st, int step) {
-    const int k = uniform((first + step) * kBlock8);
-    asm volatile("" : "+v"(off_a), "+v"(off_b));  // the sums below are made again each time: eight registers less
-    const Rsrc ra = rsrc_of(pa, uniform(step < steps ? bytes_a : 0)), rb = rsrc_of(pb, uniform(step < steps ? bytes_b : 0));
+    const int k = (first + step) * kBlock8;
+    if constexpr (SIDE == 256) asm volatile("" : "+v"(off_a), "+v"(off_b));  // the sums below are made again each time: eight registers less
+    const Rsrc ra = rsrc_of(pa, step < steps ? bytes_a : 0), rb = rsrc_of(pb, step < steps ? bytes_b : 0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_unit(ra, st + (i * kWaves + wave) * 64, off_a + more_a[i], k);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_unit(rb, st + SIDE * 8 + (i * kWaves + wave) * 64, off_b + more_b[i], k);
   };
-  // of the wave's rows
+  // From the wave's first row of the first block to the end of all: a lane past a block's rows gets scales of other ones, whose products
+  // are not stored, past the end zeros.
   const long srow = m0 + wm * 16 * TM, scol = n0 + wn * 16 * TN, start_a = p.a_square ? srow / kBlock8 : srow, start_b = p.b_square ? scol / kBlock8 : scol;
-  const int left_a = uniform((int)max(0L, min(p.spa - start_a, 16L * TM))), left_b = uniform((int)max(0L, min(p.spb - start_b, 16L * TN)));
+  const int left_a = uniform((int)max(0L, p.spa * p.nb - start_a)), left_b = uniform((int)max(0L, p.spb * p.nb - start_b));
+  const Rsrc rows_sa = rsrc_of(p.sa + start_a, p.a_square ? 0 : left_a), square_sa = rsrc_of(p.sa + start_a, p.a_square ? left_a : 0);
+  const Rsrc rows_sb = rsrc_of(p.sb + start_b, p.b_square ? 0 : left_b), square_sb = rsrc_of(p.sb + start_b, p.b_square ? left_b : 0);
+  const int spa = uniform((int)p.spa), spb = uniform((int)p.spb);
+  int s_off_a = first * spa + (p.a_square ? 0 : TM * (lane & 15)), s_off_b = first * spb + (p.b_square ? 0 : TN * (lane & 15));
   struct Scales {
     FourScales a[TM / 4], b;
   };
-  auto scales = [&](int step) {
-    const long block = min(first + step, p.nb - 1);
+  // of the next step, and on to the one after
+  auto scales = [&] {
     Scales s;
 #pragma unroll
-    for (int i = 0; i < TM / 4; ++i) s.a[i] = load_scales(p.sa + block * p.spa + start_a, left_a, p.a_square, TM * (lane & 15) + 4 * i);
-    s.b = load_scales(p.sb + block * p.spb + start_b, left_b, p.b_square, TN * (lane & 15));
+    for (int i = 0; i < TM / 4; ++i) s.a[i] = load_scales(rows_sa, square_sa, s_off_a + 4 * i);
+    if constexpr (TM == 8) s.a[1].one = s.a[0].one;  // of the same square
+    s.b = load_scales(rows_sb, square_sb, s_off_b);
+    s_off_a += spa;
+    s_off_b += spb;
     return s;
   };
 
@@ -222,7 +228,7 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
 #pragma unroll
     for (int i = 0; i < TM / 4; ++i) sa[i] = s.a[i].word();
     const uint32_t sb = s.b.word();
-    s_other = scales(t + 1);
+    s_other = scales();
     Wide wb[WIDE ? TN : 1];
     if constexpr (WIDE) {
 #pragma unroll
@@ -294,7 +300,7 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
   };
   Scales s0, s1;
   load(stage0, 0);
-  s0 = scales(0);
+  s0 = scales();
   arrived(s0);
   meet();
   load(stage1, 1);
