@@ -120,22 +120,25 @@ __device__ __forceinline__ void for_each_index(F f, std::integer_sequence<int, I
   (f(std::integral_constant<int, I>()), ...);
 }
 
-// SIDE x SIDE of y, by waves of 16 TM x 16 TN.  The blocks of the sum take turns in two stages.  In a step a wave holds its fragments
+// SIDE x SIDE of y, by waves of 16 TM x 16 TN.  The blocks of the sum take turns in STAGES stages (two, or, where a workgroup of 128 x
+// 128 has a compute unit to itself, four).  In a step a wave holds its fragments
 // of b and goes through those of a, each read two rows of products ahead; before the last two rows
 //   the workgroup meets: this stage has been read, the other one has arrived; the stage's next block is sent for,
 // and each fragment of b is read again, from the other stage, as soon as the last two products with it have begun.  So a block has
-// the whole of a step to arrive and no product waits for LDS.  Blocks past the end come from an empty buffer, as zeros that nothing
+// at least the whole of a step to arrive and no product waits for LDS.  Blocks past the end come from an empty buffer, as zeros that nothing
 // multiplies.
 //
 // 16 x 16 results, not 32 x 32: the larger instruction does the same work a clock, but the compiler gives its results registers of
 // their own beside those of its accumulator, which spills.
-template <int FA, int FB, bool WIDE, int SIDE>
-__global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel(ProductArgs p) {
+template <int FA, int FB, bool WIDE, int SIDE, int STAGES>
+__global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) block8_tile_kernel(ProductArgs p) {
   constexpr int kWaves = SIDE / 32, TM = SIDE / 32, TN = 4, kLoads = 4;  // tiles of a wave; loads of a lane, operand and step
   constexpr auto kAcross = std::make_integer_sequence<int, TN>();
   constexpr int kTail = TM / 2, kAhead = (TM - 2 + TM - kTail - 1) / (TM - kTail);  // rows of products behind the meeting; fragments read in a row before it
   __shared__ __attribute__((aligned(16))) Word4 stage0[2 * SIDE * 8];
   __shared__ __attribute__((aligned(16))) Word4 stage1[2 * SIDE * 8];
+  __shared__ __attribute__((aligned(16))) Word4 stage2[STAGES > 2 ? 2 * SIDE * 8 : 1];
+  __shared__ __attribute__((aligned(16))) Word4 stage3[STAGES > 2 ? 2 * SIDE * 8 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int wm = wave & 1, wn = wave >> 1;
   // neighbouring tiles to one of the eight dies
@@ -223,12 +226,12 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
     v8bf q[4];
   };
   // step t, in `st`, with its scales; the next stage, and where the scales of its step go
-  auto step = [&](Word4* st, int t, const Scales& s, const Word4* other, Scales& s_other) {
+  auto step = [&](Word4* st, int t, const Scales& s, const Word4* other, const Scales& s_other, Scales& s_last) {
     uint32_t sa[TM / 4];
 #pragma unroll
     for (int i = 0; i < TM / 4; ++i) sa[i] = s.a[i].word();
     const uint32_t sb = s.b.word();
-    s_other = scales();
+    s_last = scales();
     Wide wb[WIDE ? TN : 1];
     if constexpr (WIDE) {
 #pragma unroll
@@ -272,7 +275,7 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
     }
     arrived(s_other);
     meet();
-    load(st, t + 2);
+    load(st, t + STAGES);
     Wide wa[WIDE ? kTail : 1];
     if constexpr (WIDE) {
 #pragma unroll
@@ -298,22 +301,32 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256, 2) block8_tile_kernel
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  Scales s0, s1;
-  load(stage0, 0);
-  s0 = scales();
-  arrived(s0);
+  auto stage = [&](auto i) -> Word4* {
+    constexpr int I = decltype(i)::value % STAGES;
+    return I == 0 ? stage0 : I == 1 ? stage1 : I == 2 ? stage2 : stage3;
+  };
+  Scales s[STAGES];
+  for_each_index([&](auto i) {
+    load(stage(i), decltype(i)::value);
+    s[decltype(i)::value] = scales();
+  }, std::make_integer_sequence<int, STAGES - 1>());
+  arrived(s[0]);
   meet();
-  load(stage1, 1);
+  load(stage(std::integral_constant<int, STAGES - 1>()), STAGES - 1);
   a[0] = fragment_a(stage0, 0);
   a[1] = fragment_a(stage0, 1);
 #pragma unroll
   for (int j = 0; j < TN; ++j) b[j] = fragment_b(stage0, j);
+  auto turn = [&](auto i, int t) {
+    constexpr int I = decltype(i)::value;
+    step(stage(i), t + I, s[I], stage(std::integral_constant<int, I + 1>()), s[(I + 1) % STAGES], s[(I + STAGES - 1) % STAGES]);
+  };
   int t = 0;
-  for (; t + 1 < steps; t += 2) {  // one way out: with two the accumulators take twice the registers
-    step(stage0, t, s0, stage1, s1);
-    step(stage1, t + 1, s1, stage0, s0);
-  }
-  if (t < steps) step(stage0, t, s0, stage1, s1);
+  for (; t + STAGES <= steps; t += STAGES)  // one way out: with several the accumulators take twice the registers
+    for_each_index([&](auto i) { turn(i, t); }, std::make_integer_sequence<int, STAGES>());
+  for_each_index([&](auto i) {
+    if (t + decltype(i)::value < steps) turn(i, t);
+  }, std::make_integer_sequence<int, STAGES - 1>());
   __builtin_amdgcn_s_waitcnt(0x0070);  // nothing is on its way to LDS when the workgroup ends
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -436,13 +449,16 @@ template <int FA, int FB, bool WIDE>
 static int product_launch(const ProductArgs& a, const ProductPlan& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.slices));
   if constexpr (!WIDE)
-    if (p.kind == PRODUCT_256) {
-      hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 256>), grid, dim3(512), 0, st, a);
+    if (p.kind == PRODUCT_256 || p.deep) {
+      if (p.deep)
+        hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 128, 4>), grid, dim3(256), 0, st, a);
+      else
+        hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 256, 2>), grid, dim3(512), 0, st, a);
       AX_LAUNCH_CHECK();
       return ALEXNET_OK;
     }
   if (p.kind == PRODUCT_128)
-    hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 128>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 128, 2>), grid, dim3(256), 0, st, a);
   else if (p.mt == 1)
     hipLaunchKernelGGL((block8_rows_kernel<FA, FB, WIDE, 1>), grid, dim3(64 * kRowWaves), 0, st, a);
   else if (p.mt == 2)

@@ -10,7 +10,8 @@ enum { PRODUCT_ROWS = 0, PRODUCT_128 = 1, PRODUCT_256 = 2 };
 
 struct ProductPlan {
   int kind;
-  int mt;  // PRODUCT_ROWS: sixteens of rows of a workgroup
+  int mt;     // PRODUCT_ROWS: sixteens of rows of a workgroup
+  bool deep;  // PRODUCT_128: four stages, one workgroup to a compute unit
   int tiles_m, tiles_n;
   int slices, steps;  // of the sum; blocks of 128 in a slice
   size_t slab, ws;    // floats of a slice's y; bytes of scratch
@@ -23,7 +24,8 @@ constexpr long kProductGrid = 1L << 22;  // workgroups of a launch, of 512 threa
 //   Rows: eight blocks take a compute unit by the rows that they read, not by their products; 64 x 4096 x 4096 12.2 (128-tiles in four slices 13.2), 129 x 1001 x 515 7.2 (14.0),
 //   128 x 4096 x 4096 21.4 (15.2 in two slices).
 //   128-tiles: a step of a workgroup that has a compute unit to itself, and of two that share one; 2048 x 4096 x 4096 37 (256-tiles 50),
-//   43264 x 384 x 384 19 (26), 256 x 9216 x 4096 in four slices 24 (one 51, eight 25).
+//   43264 x 384 x 384 19 (26), 256 x 9216 x 4096 in four slices 24 (one 51, eight 25); with four stages, where a workgroup is alone,
+//   22, 256 x 4096 x 9216 26 -> 21, but 2048 x 4096 x 4096 37 -> 46.
 //   256-tiles, one to a compute unit: 16384 x 4096 x 4096 222 (128-tiles 266), 4096 x 4096 x 4096 65 (77).
 //   Slices are written and read once more each, in a second launch.
 // wide: the products are those of bf16, of which 256-tiles have more operands than registers.
@@ -32,13 +34,14 @@ inline ProductPlan product_plan(long m, long n, long k, bool wide) {
   auto tiles = [](long size, long tile) { return (size + tile - 1) / tile; };
   ProductPlan best = {};
   double least = 1e300;
-  auto consider = [&](int kind, int mt, long tm, long tn, long slices, double us) {
+  auto consider = [&](int kind, int mt, long tm, long tn, long slices, bool deep, double us) {
     if (tm > kProductGrid || tn > kProductGrid || tm * tn * slices > kProductGrid) return;
     if (slices > 1) us += 4 + slices * (0.3 + 4.0 * m * n / 4e6);
     if (us >= least) return;
     least = us;
     best.kind = kind;
     best.mt = mt;
+    best.deep = deep;
     best.tiles_m = (int)tm;
     best.tiles_n = (int)tn;
     best.slices = (int)slices;
@@ -47,18 +50,19 @@ inline ProductPlan product_plan(long m, long n, long k, bool wide) {
   {
     const int mt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
     const double busy = std::max(1.0, (double)tiles(m, 16 * mt) * tiles(n, 16) / 256), block = mt == 1 ? 0.33 : mt == 2 ? 0.85 : 2.05;
-    consider(PRODUCT_ROWS, mt, tiles(m, 16 * mt), tiles(n, 16), 1, 5 + tiles(nb, 8) * block * busy);
+    consider(PRODUCT_ROWS, mt, tiles(m, 16 * mt), tiles(n, 16), 1, false, 5 + tiles(nb, 8) * block * busy);
   }
   for (long want = 1; want <= std::min<long>(nb, kProductSlices); want += 1 + want / 8) {
     const long steps = tiles(nb, want), slices = tiles(nb, steps);
     {
       const double work = (double)tiles(m, 128) * tiles(n, 128) * slices, rest = work - 512 * (double)(long)(work / 512);
-      const double pair = steps * (wide ? 2.0 : 0.97) + 5, alone = steps * (wide ? 1.1 : 0.62) + 2.5;
-      consider(PRODUCT_128, 0, tiles(m, 128), tiles(n, 128), slices, 3 + (double)(long)(work / 512) * pair + (rest > 256 ? pair : rest > 0 ? alone : 0));
+      const bool deep = !wide && work <= 256 && steps >= 8;
+      const double pair = steps * (wide ? 2.0 : 0.97) + 5, alone = steps * (wide ? 1.1 : deep ? 0.5 : 0.62) + 2.5;
+      consider(PRODUCT_128, 0, tiles(m, 128), tiles(n, 128), slices, deep, 3 + (double)(long)(work / 512) * pair + (rest > 256 ? pair : rest > 0 ? alone : 0));
     }
     if (!wide) {
       const double work = (double)tiles(m, 256) * tiles(n, 256) * slices, rounds = (double)(long)((work + 255) / 256);
-      consider(PRODUCT_256, 0, tiles(m, 256), tiles(n, 256), slices, 3 + rounds * (steps * 1.35 + 10));
+      consider(PRODUCT_256, 0, tiles(m, 256), tiles(n, 256), slices, false, 3 + rounds * (steps * 1.35 + 10));
     }
   }
   best.slab = ((size_t)m * n + 63) & ~(size_t)63;
