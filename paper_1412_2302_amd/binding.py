@@ -700,9 +700,12 @@ _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_get
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
 def _here(t: torch.Tensor, stream) -> bool:
     """Whether a call on t runs on the current device and its current stream."""
-    return stream is None and t.get_device() == torch.cuda.current_device()
+    return stream is None and t.get_device() == _current_device()
 
 
 def _there(t: torch.Tensor, stream, inputs, call):
@@ -884,6 +887,7 @@ def checkpoint_fc_backward_weight(kept: Checkpoint, dy: torch.Tensor, dw: Option
 
 # ---- dense layers in 8-bit floating point, root-mean-square normalisation, gradient clipping ----
 # As above: no handle, outputs and scratch on the call's stream, nothing recorded for autograd.
+# Results are made from a tensor of the call (new_empty, empty_like): torch.empty takes twice as long, which small calls notice.
 _CODES8 = {torch.float8_e4m3fn: 1, torch.float8_e5m2: 2}
 BLOCK8 = 128  # columns (of square blocks also rows) that share a scale
 
@@ -911,11 +915,11 @@ class Blocks8:
         return rows, blocks * BLOCK8, blocks, -(-rows // BLOCK8) if square else -(-rows // 4) * 4
 
     @staticmethod
-    def _empty(rows: int, cols: int, dtype: torch.dtype, square: bool, device) -> "Blocks8":
+    def _empty(rows: int, cols: int, dtype: torch.dtype, square: bool, like: torch.Tensor) -> "Blocks8":
         rows, pitch, blocks, scales = Blocks8._sizes(rows, cols, square)
         made = Blocks8.__new__(Blocks8)
-        made.codes = torch.empty((rows, pitch), dtype=dtype, device=device)
-        made.scales = torch.empty((blocks, scales), dtype=torch.uint8, device=device)
+        made.codes = like.new_empty((rows, pitch), dtype=dtype)
+        made.scales = like.new_empty((blocks, scales), dtype=torch.uint8)
         made.cols, made.square = cols, square
         return made
 
@@ -934,6 +938,19 @@ class Blocks8:
             raise ValueError(f"{what}: expected a device tensor, got Blocks8 on {blocks.codes.device}")
 
 
+def _make(out, shape, dtype, like: torch.Tensor, what: str):
+    """out, if it is what is wanted, or a new tensor beside `like`; and its row stride."""
+    if out is not None:
+        return _result(out, shape, dtype, like.device, what)
+    if like.dtype == dtype and like.shape == shape and like.is_contiguous():
+        return torch.empty_like(like), shape[-1]
+    return like.new_empty(shape, dtype=dtype), shape[-1]
+
+
+def _scratch_for(nbytes: int, like: torch.Tensor):
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+
+
 def _code8(dtype: torch.dtype, what: str):
     if dtype not in _CODES8:
         raise ValueError(f"{what}: codes are float8_e4m3fn or float8_e5m2, got {dtype}")
@@ -949,8 +966,8 @@ def block8_pack(x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, squar
     if not _here(x, stream):
         return _there(x, stream, (x,), lambda: block8_pack(x, dtype, square, along))
     rows, cols, device = x.shape[:-1].numel(), x.shape[-1], x.device
-    by_rows = Blocks8._empty(rows, cols, dtype, square, device) if along != "columns" else None
-    by_columns = Blocks8._empty(cols, rows, dtype, square, device) if along != "rows" else None
+    by_rows = Blocks8._empty(rows, cols, dtype, square, x) if along != "columns" else None
+    by_columns = Blocks8._empty(cols, rows, dtype, square, x) if along != "rows" else None
     _check(_lib.alexnet_block8_pack(x.data_ptr(), ld, _TYPES[x.dtype], rows, cols, None if by_rows is None else by_rows._arg(),
                                     None if by_columns is None else by_columns._arg(), _raw_stream(device.index)))
     return by_columns if by_rows is None else by_rows if by_columns is None else (by_rows, by_columns)
@@ -964,7 +981,7 @@ def block8_unpack(blocks: Blocks8, dtype: torch.dtype = torch.float32, out: Opti
         raise ValueError(f"block8_unpack: expected float32, bfloat16 or float16, got {dtype}")
     if not _here(codes, stream):
         return _there(codes, stream, (blocks, out), lambda: block8_unpack(blocks, dtype, out))
-    x, ld = _result(out, blocks.shape, dtype, codes.device, "block8_unpack: out")
+    x, ld = _make(out, blocks.shape, dtype, codes, "block8_unpack: out")
     _check(_lib.alexnet_block8_unpack(blocks._arg(), codes.shape[0], blocks.cols, x.data_ptr(), ld, _TYPES[dtype],
                                       _raw_stream(codes.get_device())))
     return x
@@ -993,9 +1010,9 @@ def block8_product(a: Blocks8, b: Blocks8, dtype: torch.dtype = torch.bfloat16, 
     if not _here(codes, stream):
         return _there(codes, stream, (a, b, out), lambda: block8_product(a, b, dtype, out))
     m, n, k, kind, device = codes.shape[0], b.codes.shape[0], a.cols, _TYPES[dtype], codes.device
-    y, ld = _result(out, torch.Size((m, n)), dtype, device, "block8_product: out")
+    y, ld = _make(out, torch.Size((m, n)), dtype, codes, "block8_product: out")
     ws_bytes = _block8_product_ws(m, n, k, kind)
-    ws = _scratch(ws_bytes, device)
+    ws = _scratch_for(ws_bytes, codes)
     _check(_lib.alexnet_block8_product(a._arg(), b._arg(), m, n, k, y.data_ptr(), ld, kind, None if ws is None else ws.data_ptr(),
                                        ws_bytes, _raw_stream(device.index)))
     return y
@@ -1026,15 +1043,15 @@ def rms_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], residual: O
         ld_residual = _rows_stride(residual, "rms_norm_forward: residual")
         if residual.shape != shape or residual.dtype != x.dtype or residual.device != device:
             raise ValueError(f"{what}: x {list(shape)} and residual {list(residual.shape)} differ in shape, type or device")
-        s, ld_s = _result(out_sum, shape, x.dtype, device, "rms_norm_forward: out_sum")
+        s, ld_s = _make(out_sum, shape, x.dtype, x, "rms_norm_forward: out_sum")
         p_s, p_residual = s.data_ptr(), residual.data_ptr()
     if blocks is None:
-        y, ld_y = _result(out, shape, x.dtype, device, "rms_norm_forward: out")
+        y, ld_y = _make(out, shape, x.dtype, x, "rms_norm_forward: out")
         p_y, arg = y.data_ptr(), None
     else:
-        y, ld_y, p_y = Blocks8._empty(rows, cols, blocks, False, device), 0, None
+        y, ld_y, p_y = Blocks8._empty(rows, cols, blocks, False, x), 0, None
         arg = y._arg()
-    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    rstd = x.new_empty(rows, dtype=torch.float32)
     _check(_lib.alexnet_rms_norm_forward(x.data_ptr(), ld_x, p_residual, ld_residual, _TYPES[x.dtype], rows, cols, eps, p_gamma, p_s,
                                          ld_s, p_y, ld_y, arg, rstd.data_ptr(), _raw_stream(device.index)))
     return y, s, rstd
@@ -1068,10 +1085,10 @@ def rms_norm_backward(s: torch.Tensor, dy: torch.Tensor, rstd: torch.Tensor, gam
         if dsum.shape != shape or dsum.dtype != dy.dtype or dsum.device != device:
             raise ValueError(f"{what}: dsum {list(dsum.shape)} and dy {list(shape)} differ in shape, type or device")
         p_dsum = dsum.data_ptr()
-    dx, ld_dx = _result(out, shape, dy.dtype, device, "rms_norm_backward: out")
-    dgamma = torch.empty(cols, dtype=torch.float32, device=device)
+    dx, ld_dx = _make(out, shape, dy.dtype, dy, "rms_norm_backward: out")
+    dgamma = dy.new_empty(cols, dtype=torch.float32)
     ws_bytes = _rms_norm_ws(rows, cols, kind)
-    ws = _scratch(ws_bytes, device)
+    ws = _scratch_for(ws_bytes, dy)
     _check(_lib.alexnet_rms_norm_backward(s.data_ptr(), ld_s, dy.data_ptr(), ld_dy, p_dsum, ld_dsum, kind, rows, cols, p_rstd, p_gamma,
                                           dx.data_ptr(), ld_dx, dgamma.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes,
                                           _raw_stream(device.index)))
@@ -1114,9 +1131,9 @@ def gradient_norm(grads, stream=None) -> torch.Tensor:
     first = grads[0]
     if not _here(first, stream):
         return _there(first, stream, grads, lambda: gradient_norm(grads))
-    norm = torch.empty((), dtype=torch.float32, device=first.device)
+    norm = first.new_empty((), dtype=torch.float32)
     ws_bytes = _clip_ws(sizes)
-    ws = _scratch(ws_bytes, first.device)
+    ws = _scratch_for(ws_bytes, first)
     _check(_lib.alexnet_gradient_norm(len(grads), _address(pointers), _address(sizes), _address(types), norm.data_ptr(), ws.data_ptr(),
                                       ws_bytes, _raw_stream(index)))
     return norm
@@ -1136,9 +1153,9 @@ def clip_gradients(grads, max_norm: float, out=None, stream=None) -> torch.Tenso
     first = grads[0]
     if not _here(first, stream):
         return _there(first, stream, grads + (out or []), lambda: clip_gradients(grads, max_norm, out))
-    norm = torch.empty((), dtype=torch.float32, device=first.device)
+    norm = first.new_empty((), dtype=torch.float32)
     ws_bytes = _clip_ws(sizes)
-    ws = _scratch(ws_bytes, first.device)
+    ws = _scratch_for(ws_bytes, first)
     _check(_lib.alexnet_clip_gradients(len(grads), _address(pointers), None if results is None else _address(results), _address(sizes),
                                        _address(types), max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes, _raw_stream(index)))
     return norm
