@@ -128,8 +128,11 @@ __device__ __forceinline__ void for_each_index(F f, std::integer_sequence<int, I
 // at least the whole of a step to arrive and no product waits for LDS.  Blocks past the end come from an empty buffer, as zeros that nothing
 // multiplies.
 //
-// 16 x 16 results, not 32 x 32: the larger instruction does the same work a clock, but the compiler gives its results registers of
-// their own beside those of its accumulator, which spills.
+// 16384 x 4096 x 4096 220 to 250 us by the card (2.2 to 2.5 PFLOP/s; the library's product of plain codes 186 to 194), 8192 x 8192 x
+// 8192 385 to 440 (350 to 362): bound by the matrix instructions, which have the unit to themselves 55 % of the time at the
+// clock that their power leaves, and by what arrives late (with empty operands 166 us).  Tried and dropped: 32 x 32 results, which
+// do the same work a clock, 249 us instead of 224; workgroups that stay and send for their next tile's blocks before they store this
+// one's results, 223 instead of 219; eight waves to a 128 x 128 tile, 40 instead of 37 us for 2048 x 4096 x 4096.
 template <int FA, int FB, bool WIDE, int SIDE, int STAGES>
 __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) block8_tile_kernel(ProductArgs p) {
   constexpr int kWaves = SIDE / 32, TM = SIDE / 32, TN = 4, kLoads = 4;  // tiles of a wave; loads of a lane, operand and step
