@@ -109,13 +109,7 @@ def close(y, va, vb, dtype):
     assert y.dtype == dtype and (off <= tol).all(), (off / tol).max()
 
 
-# one row and up, odd sizes, k under, at and over a block; tiles of 128, cut along the sum or not, and of 256
-SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 2304), (2, 17, 129), (15, 3, 64), (16, 130, 1152), (17, 33, 1025), (32, 48, 256), (33, 100, 1280),
-         (63, 65, 127), (64, 16, 4096), (65, 7, 1000), (129, 515, 1001), (128, 128, 128), (200, 130, 5000), (300, 1000, 260), (1000, 65, 640),
-         (65, 4096, 130), (4000, 4097, 257), (16390, 1030, 129)]
-
-
-@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("m,n,k", R.PRODUCT_SIZES)
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_product(lib, m, n, k, dtype):
     which = m + n + k
@@ -124,7 +118,7 @@ def test_product(lib, m, n, k, dtype):
     close(lib.block8_product(a, b, dtype), va, vb, dtype)
 
 
-@pytest.mark.parametrize("m,n,k", SIZES + [(70, 66, 20000), (3, 5, 40000)])
+@pytest.mark.parametrize("m,n,k", R.PRODUCT_SIZES + [(70, 66, 20000), (3, 5, 40000)])
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_products_of_small_whole_numbers_are_exact(lib, m, n, k, dtype):
     """Sums that no arithmetic rounds: every value of the operands counts once, whatever the kernel."""
@@ -136,7 +130,7 @@ def test_products_of_small_whole_numbers_are_exact(lib, m, n, k, dtype):
         assert torch.equal(lib.block8_product(a, b, dtype).cpu(), y.to(dtype)), (code, square)
 
 
-@pytest.mark.parametrize("m,n,k", [(5, 40, 700), (40, 20, 300), (100, 300, 1300), (4100, 4100, 200)])
+@pytest.mark.parametrize("m,n,k", R.PRODUCT_KINDS)
 @pytest.mark.parametrize("ca", CODES, ids=str)
 @pytest.mark.parametrize("cb", CODES, ids=str)
 @pytest.mark.parametrize("sa", [False, True], ids=["rows", "square"])
@@ -147,7 +141,7 @@ def test_product_of_all_kinds(lib, m, n, k, ca, cb, sa, sb):
         close(lib.block8_product(a, b, dtype), va, vb, dtype)
 
 
-@pytest.mark.parametrize("m,n", [(3, 21), (50, 21), (130, 140), (4100, 4100)])
+@pytest.mark.parametrize("m,n", [(3, 21), (50, 21), (581, 2154), (4000, 4090)])
 def test_every_code_under_many_scales(lib, m, n):
     """Operands of any bytes, not of packing alone."""
     k = 384
@@ -165,7 +159,7 @@ def test_every_code_under_many_scales(lib, m, n):
         assert np.array_equal(f64(lib.block8_unpack(a)), va.astype(np.float32).astype(np.float64))
 
 
-@pytest.mark.parametrize("m,n,k", [(9, 20, 300), (130, 70, 3000), (4100, 4100, 128)])
+@pytest.mark.parametrize("m,n,k", [(9, 20, 300), (130, 70, 30000), (581, 2154, 184), (591, 897, 900), (4000, 4090, 128)])
 def test_product_writes_its_result_and_nothing_else(lib, m, n, k):
     a, b, va, vb = product_case(lib, m, n, k, torch.bfloat16, E4M3, E4M3, False, True)
     room = torch.full((m + 2, n + 11), 7.0, dtype=torch.bfloat16, device="cuda")
@@ -207,7 +201,7 @@ def test_a_layer_and_its_gradients(lib):
 
 def test_captured_and_replayed(lib):
     """Packing and products of every kind in one graph over static buffers, replayed with other inputs, eager work between."""
-    sizes = [(3, 200, 300), (130, 140, 2600), (4100, 4100, 130)]
+    sizes = [(3, 200, 300), (130, 140, 26000), (4000, 4090, 130)]
     xs = [matrix(m, k).cuda() for m, n, k in sizes]
     ws = [matrix(n, k).cuda() for m, n, k in sizes]
 
