@@ -902,7 +902,7 @@ class Blocks8:
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, square: bool = False):
         if codes.dtype not in _CODES8 or scales.dtype != torch.uint8:
             raise ValueError(f"Blocks8: codes are float8_e4m3fn or float8_e5m2 and scales uint8, got {codes.dtype} and {scales.dtype}")
-        if codes.dim() != 2 or tuple(codes.shape) + tuple(scales.shape) != Blocks8._sizes(codes.shape[0], cols, square):
+        if codes.dim() != 2 or cols < 0 or tuple(codes.shape) + tuple(scales.shape) != Blocks8._sizes(codes.shape[0], cols, square):
             raise ValueError(f"Blocks8: codes {list(codes.shape)} and scales {list(scales.shape)} are not those of {cols} columns"
                              f"{' in square blocks' if square else ''}")
         if not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device:

@@ -180,7 +180,7 @@ def test_blocks8_of_the_wrong_sizes(B):
     made = B.Blocks8(codes, scales, 200)
     assert made.shape == (5, 200) and not made.square
     assert B.Blocks8(codes, torch.zeros((2, 1), dtype=torch.uint8), 129, square=True).square
-    for bad in (lambda: B.Blocks8(codes, scales, 128), lambda: B.Blocks8(codes, scales, 257), lambda: B.Blocks8(codes, scales, 200, square=True),
+    for bad in (lambda: B.Blocks8(codes[:, :0], scales[:0], -5), lambda: B.Blocks8(codes, scales, 128), lambda: B.Blocks8(codes, scales, 257), lambda: B.Blocks8(codes, scales, 200, square=True),
                 lambda: B.Blocks8(codes.view(torch.uint8), scales, 200), lambda: B.Blocks8(codes, scales.int(), 200),
                 lambda: B.Blocks8(codes[:4], scales, 200), lambda: B.Blocks8(codes, scales[:, :5], 200), lambda: B.Blocks8(codes.view(5, 2, 128), scales, 200),
                 lambda: B.Blocks8(torch.zeros((256, 5), dtype=torch.uint8).t().view(E4M3), scales, 200)):
