@@ -4,6 +4,8 @@
 // + 7: a row's block is sixteen neighbouring lanes and a column's the same lanes of all waves, so both kinds of scales and of
 // codes come from one read.  Of the transpose a thread has eight codes of each of its columns as two words (the conversion takes
 // two values to a word, which here are two rows); they go through LDS to be stored as whole lines.
+// 4096 x 9216 float32 to square blocks both ways 50 us (4.5 TB/s), 43264 x 384 bf16 both ways 16 (4.1 TB/s), 256 x 9216 bf16 both ways, which is
+// 144 workgroups, 9: the eight loads of a thread on their way together, before that 13.
 #include <algorithm>
 
 #include "blocks8.h"
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
   }
 }
 
-// Eight codes a thread, four rows of a block of them
+// Eight codes a thread at a time.  43264 x 384 to bf16 10 us (4.8 TB/s): what comes from the cache and memory bounds it.
 struct Unpack8Args {
   const uint8_t *codes, *scales;
   void* x;
@@ -188,7 +190,7 @@ static int unpack8_type(const Unpack8Args& a, int code, hipStream_t st) {
   return ALEXNET_OK;
 }
 // what both directions ask of a matrix
-static int check_matrix(const char* who, const void* x, long ld, int type, long rows, long cols) {
+static int check_matrix(const char* who, const void* x, long ld, int type, long cols) {
   AX_REQUIRE(x, ALEXNET_EINVAL, "%s: null argument", who);
   AX_REQUIRE(ld >= cols && ld <= 1L << 40, ALEXNET_ESHAPE, "%s: row stride %ld of %ld columns", who, ld, cols);
   AX_REQUIRE((uintptr_t)x % type_size(type) == 0, ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
@@ -212,7 +214,7 @@ int alexnet_block8_pack(const void* d_x, int64_t ld_x, int32_t type, int64_t row
   AX_TRY(check_sizes(who, type, rows, cols));
   AX_REQUIRE(out_rows || out_columns, ALEXNET_EINVAL, "%s: nothing to write", who);
   if (rows == 0 || cols == 0) return ALEXNET_OK;
-  AX_TRY(check_matrix(who, d_x, ld_x, type, rows, cols));
+  AX_TRY(check_matrix(who, d_x, ld_x, type, cols));
   if (out_rows) AX_TRY(check_blocks(out_rows, "the rows", who));
   if (out_columns) AX_TRY(check_blocks(out_columns, "the columns", who));
   AX_REQUIRE(!out_rows || !out_columns || (out_rows->code == out_columns->code && out_rows->square == out_columns->square), ALEXNET_EINVAL,
@@ -253,7 +255,7 @@ int alexnet_block8_unpack(const alexnet_blocks8_t* in, int64_t rows, int64_t col
   const char* who = "alexnet_block8_unpack";
   AX_TRY(check_sizes(who, type, rows, cols));
   if (rows == 0 || cols == 0) return ALEXNET_OK;
-  AX_TRY(check_matrix(who, d_x, ld_x, type, rows, cols));
+  AX_TRY(check_matrix(who, d_x, ld_x, type, cols));
   AX_TRY(check_blocks(in, "the operand", who));
   const long size = (long)type_size(type);
   AX_TRY(check_apart(who, {{"the codes", blocks_codes(in, rows, cols), false}, {"the scales", blocks_scales(in, rows, cols), false}},

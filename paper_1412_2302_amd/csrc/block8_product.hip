@@ -2,8 +2,8 @@
 //   y[i][j] = sum over blocks B of 2^(sa[B][i] + sb[B][j] - 254) * sum over k in B of code_a[i][k] * code_b[j][k]
 //
 // Two kinds of arithmetic, by the type of y.
-//   16 bits: the 8-bit matrix instruction, which takes 32 (64, for 32 x 32 results) of the sum with a scale byte for each lane's row,
-//     so that scales cost the load of a word per block.  It adds eight products at a time with 13 bits under the largest of the
+//   16 bits: the 8-bit matrix instruction, which takes 128 of the sum, a lane's 32 with a scale byte of their own, so that
+//     scales cost the load of a word per block.  It adds eight products at a time with 13 bits under the largest of the
 //     eight (measured; the sums of those eights go on in float32), 1.5e-5 of a result of normal numbers and a hundredth of what
 //     rounding it to bf16 costs, a twentieth to fp16: a choice for twice the rate.
 //   32 bits: codes are widened to bf16 with their scales, which is exact, and go through the bf16 instruction, whose sums are
@@ -25,7 +25,6 @@ namespace ax {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 
@@ -170,7 +169,7 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu
     more_b[i] = uniform((dealt((i * kWaves + wave) * 8, TN) - dealt(wave * 8, TN)) * (int)p.pitch);
   }
   auto load = [&](Word4* st, int step) {
-    const int k = (first + step) * kBlock8;
+    const int k = step < steps ? (first + step) * kBlock8 : 0;  // nothing but the rows' offsets is held against a buffer's size
     if constexpr (SIDE == 256) asm volatile("" : "+v"(off_a), "+v"(off_b));  // the sums below are made again each time: eight registers less
     const Rsrc ra = rsrc_of(pa, step < steps ? bytes_a : 0), rb = rsrc_of(pb, step < steps ? bytes_b : 0);
 #pragma unroll
