@@ -5,9 +5,10 @@
 // lie is the launch's argument, which a captured graph keeps.  The first launch leaves a sum of squares per workgroup,
 // in float64: a square of a float32 is exact there and none is too large or too small.  Each workgroup of the second adds them all
 // up, in one order, and scales; it goes through the chunks backwards, as the last ones read are still in the cache.
-// Memory bounds both: 61 M float32 values 42 us (5.9 TB/s) and 95 (5.2 TB/s).  Of 16 small tensors the launches are what there is.
+// Memory bounds both: 61 M float32 values 41 us (5.9 TB/s) and, to other places, 73 (6.7 TB/s, of which the cache has some).  Of 16 small tensors the launches are what there is.
 #include <algorithm>
 #include <exception>
+#include <type_traits>
 #include <vector>
 
 #include "blocks8.h"
@@ -56,26 +57,29 @@ __device__ __forceinline__ void over_chunks(const ClipArgs& a, int c0, int c1, b
   }
 }
 
-// f(values, of which so many are the tensor's, place) of a thread's eights of a chunk: of a whole one all loads are on their way at once
+// f(values, of which so many are the tensor's, place) of a thread's 16 bytes at a time: of a whole chunk all loads are on their way at once,
+// and neighbouring lanes have neighbouring bytes (with 32 of them a lane a store writes half lines: 61 M float32 values 95 -> 73 us)
 template <typename T, typename F>
-__device__ __forceinline__ void over_eights(const T* in, long n, F f) {
-  constexpr int kEights = kClipChunk / 2048;
-  const int at = 8 * threadIdx.x;
+__device__ __forceinline__ void over_vectors(const T* in, long n, F f) {
+  constexpr int V = 16 / sizeof(T), kStep = 256 * V, kVectors = kClipChunk / kStep;
+  const int at = V * threadIdx.x;
   if (n == kClipChunk) {
-    Eight<T> raw[kEights];
+    typename Pack<T, V>::Raw raw[kVectors];
 #pragma unroll
-    for (int k = 0; k < kEights; ++k) raw[k].r = Pack<T, 8>::load(in + at + 2048 * k);
+    for (int k = 0; k < kVectors; ++k) raw[k] = Pack<T, V>::load(in + at + kStep * k);
 #pragma unroll
-    for (int k = 0; k < kEights; ++k) {
-      float v[8];
-      raw[k].widen(v);
-      f(v, 8, at + 2048 * k);
+    for (int k = 0; k < kVectors; ++k) {
+      float v[V];
+      Pack<T, V>::widen(raw[k], v);
+      f(v, std::integral_constant<int, V>(), V, at + kStep * k);
     }
   } else {
-    for (int i = at; i < n; i += 2048) {
-      float v[8];
-      load8(in + i, n - i, v);
-      f(v, (int)min(n - i, 8L), i);
+    for (int i = at; i < n; i += kStep) {
+      const int has = (int)min(n - i, (long)V);
+      float v[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = e < has ? (float)in[i + e] : 0.f;
+      f(v, std::integral_constant<int, V>(), has, i);
     }
   }
 }
@@ -98,9 +102,9 @@ __global__ void __launch_bounds__(256) clip_squares_kernel(ClipArgs a) {
   const int c0 = (long)a.chunks * blockIdx.x / gridDim.x, c1 = (long)a.chunks * (blockIdx.x + 1) / gridDim.x;
   double sum = 0.0;
   over_chunks(a, c0, c1, false, [&](const auto* in, auto*, long n) {
-    over_eights(in, n, [&](const float* v, int, int) {
+    over_vectors(in, n, [&](const float* v, auto vector, int, int) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)v[e], (double)v[e], sum);
+      for (int e = 0; e < decltype(vector)::value; ++e) sum = __builtin_fma((double)v[e], (double)v[e], sum);
     });
   });
   sum = add_threads(sum, cross);
@@ -120,19 +124,23 @@ __global__ void __launch_bounds__(256) clip_norm_kernel(ClipArgs a) {
   if (threadIdx.x == 0) *a.norm = (float)norm;
 }
 
-// A result that goes elsewhere passes the cache by, which keeps what of the gradients is in it (61 M float32 values: 146 -> 138 us).
-template <typename T>
-__device__ __forceinline__ void store_eight(const T* in, T* out, int has, const float* v) {
-  typedef typename Pack<T, 8>::Raw Raw;
+// A result that goes elsewhere passes the cache by, which keeps what of the gradients is in it (61 M float32 values: 102 -> 73 us).
+template <int V, typename T>
+__device__ __forceinline__ void store_vector(const T* in, T* out, int has, const float* v) {
+  typedef typename Pack<T, V>::Raw Raw;
   typedef Raw Anywhere __attribute__((aligned(sizeof(T))));
-  if (in == out || has < 8) {
-    store8(out, has, v);
-    return;
-  }
-  Raw r;
+  if (has < V) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (T)v[e];  // nearest even
-  __builtin_nontemporal_store(r, reinterpret_cast<Anywhere*>(out));
+    for (int e = 0; e < V; ++e)
+      if (e < has) out[e] = (T)v[e];
+  } else if (in == out) {
+    Pack<T, V>::store(out, v);
+  } else {
+    Raw r;
+#pragma unroll
+    for (int e = 0; e < V; ++e) r[e] = (T)v[e];  // nearest even
+    __builtin_nontemporal_store(r, reinterpret_cast<Anywhere*>(out));
+  }
 }
 
 __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a) {
@@ -145,10 +153,10 @@ __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a) {
   const int b = gridDim.x - 1 - blockIdx.x;
   const int c0 = (long)a.chunks * b / gridDim.x, c1 = (long)a.chunks * (b + 1) / gridDim.x;
   over_chunks(a, c0, c1, true, [&](const auto* in, auto* out, long n) {
-    over_eights(in, n, [&](float* v, int has, int i) {
+    over_vectors(in, n, [&](float* v, auto vector, int has, int i) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (float)((double)v[e] * factor);
-      store_eight(in + i, out + i, has, v);
+      for (int e = 0; e < decltype(vector)::value; ++e) v[e] = (float)((double)v[e] * factor);
+      store_vector<decltype(vector)::value>(in + i, out + i, has, v);
     });
   });
 }
