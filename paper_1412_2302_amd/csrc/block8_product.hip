@@ -71,6 +71,12 @@ __device__ __forceinline__ void store_results(const ProductArgs& p, int slice, l
     put((_Float16*)p.y + row * p.ld);
 }
 
+// The tile of a workgroup: neighbouring ones go to one of the eight dies
+__device__ __forceinline__ int die_tile() {
+  const uint32_t total = gridDim.x, L = blockIdx.x, q8 = total >> 3, r8 = total & 7, xcd = L & 7;
+  return (int)(xcd * q8 + min(xcd, r8) + (L >> 3));
+}
+
 // Eight codes of a lane as bf16, with their scale.  FMT: 0 E4M3, 1 E5M2, as the 8-bit instruction numbers them.
 template <int FMT>
 __device__ __forceinline__ v8bf widen8(int lo, int hi, float scale) {
@@ -143,9 +149,7 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu
   __shared__ __attribute__((aligned(16))) Word4 stage3[STAGES > 2 ? 2 * SIDE * 8 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int wm = wave & 1, wn = wave >> 1;
-  // neighbouring tiles to one of the eight dies
-  const uint32_t total = gridDim.x, L = blockIdx.x, q8 = total >> 3, r8 = total & 7, xcd = L & 7;
-  const int tile = (int)(xcd * q8 + min(xcd, r8) + (L >> 3));
+  const int tile = die_tile();
   const int slice = uniform(tile / (p.tiles_m * p.tiles_n)), in_slice = tile - slice * (p.tiles_m * p.tiles_n);
   // eight rows of tiles go across together: what the compute units of a die work on at a time shares most of its operands
   const int band = uniform(in_slice / (8 * p.tiles_n)), high = min(8, p.tiles_m - 8 * band), in_band = in_slice - band * 8 * p.tiles_n;
@@ -343,62 +347,101 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu
 }
 
 // ---- few rows ---------------------------------------------------------------------
-// Few rows, or few products: what counts is to have many waves and no way through LDS.  A workgroup has 16 of b's rows and 16 MT of a's,
-// its eight waves the blocks of the sum in turn, both operands straight to registers; the waves' sums meet in LDS.  As in the
-// tiles a lane's 32 codes are two units 64 bytes apart, so that a load's lanes cover whole half lines.  Four blocks sent for at a time
-// instead of one: 1 x 9216 x 4096 7.6 -> 9.6 us, 64 x 4096 x 4096 12.2 -> 12.4.
+// Few rows, or few products: what counts is to have many waves and few meetings.  A workgroup has 16 of b's rows and 16 MT of a's, its
+// eight waves an eighth of the sum each, in LDS of their own; the waves' sums meet there.  Eight lanes load a row's block, and what they
+// hold goes through LDS to be the instruction's operand, whose neighbouring lanes are of different rows: loaded that way straight to its
+// registers a load takes a clock a lane for its addresses, four times as long (64 x 4096 x 4096 12.7 -> 7.1 us, 16 x 9216 x 4096 13.3 -> 8.7).
+// A wave's blocks lie next to each other in memory (dealt out in turn 1 x 16384 x 16384 51 us instead of 38, which are 7.1 TB/s).  One
+// block at a time: the other waves' loads fill the wait, and with the next block's on their way too 128 x 1000 x 4096 takes 7.2 instead of 6.8.
+// Row r of a goes to tile r % MT, so that a lane has the scales of its tiles next to each other.
 constexpr int kRowWaves = 8;
 template <int FA, int FB, bool WIDE, int MT>
 __global__ void __launch_bounds__(64 * kRowWaves) block8_rows_kernel(ProductArgs p) {
-  __shared__ v4f sums[kRowWaves][MT][64];
+  constexpr int kUnits = 128 * (MT + 1);  // of a wave: a row of 128 bytes is eight, unit (row, slot) holding slot ^ (row & 7)
+  __shared__ __attribute__((aligned(16))) Word4 units[kRowWaves][kUnits];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int tn = blockIdx.x / p.tiles_m, tm = blockIdx.x - tn * p.tiles_m;
+  const int tile = die_tile(), tn = tile / p.tiles_m, tm = tile - tn * p.tiles_m;
   const long m0 = (long)tm * 16 * MT, n0 = (long)tn * 16;
   const int row = lane & 15, part = lane >> 4;
-  const long b_row = min(n0 + row, p.n - 1);
-  const uint8_t* const b = p.b + b_row * p.pitch + 16 * part;
-  const uint8_t* const sb = p.sb + (p.b_square ? b_row / kBlock8 : b_row);
-  const uint8_t *a[MT], *sa[MT];
+  // rows past the end repeat the last one
+  const int of8 = lane >> 3;
+  const uint8_t *a[2 * MT], *b[2];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const long r = min(m0 + 16 * i + row, p.m - 1);
-    a[i] = p.a + r * p.pitch + 16 * part;
-    sa[i] = p.sa + (p.a_square ? r / kBlock8 : r);
+  for (int h = 0; h < 2; ++h) {
+    b[h] = p.b + min(n0 + 8 * h + of8, p.n - 1) * p.pitch + 16 * (lane & 7);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) a[2 * i + h] = p.a + min(m0 + MT * (8 * h + of8) + i, p.m - 1) * p.pitch + 16 * (lane & 7);
   }
+  const long b_row = min(n0 + row, p.n - 1), a_row = min(m0 + MT * row, (p.m - 1) / MT * MT);
+  const uint8_t* const sb = p.sb + (p.b_square ? b_row / kBlock8 : b_row);
+  const uint8_t* const sa = p.sa + (p.a_square ? a_row / kBlock8 : a_row);
+  struct Block {
+    Word4 a[2 * MT], b[2];
+    uint32_t sa, sb;
+  };
+  auto load = [&](Block& q, int kb) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) q.b[h] = *reinterpret_cast<const Word4*>(b[h] + (long)kb * kBlock8);
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) q.a[i] = *reinterpret_cast<const Word4*>(a[i] + (long)kb * kBlock8);
+    q.sb = sb[kb * p.spb];
+    const uint8_t* const s = sa + kb * p.spa;
+    if (MT == 1 || p.a_square)
+      q.sa = *s * 0x01010101u;
+    else if (MT == 2)
+      q.sa = *reinterpret_cast<const uint16_t*>(s);
+    else
+      q.sa = *reinterpret_cast<const uint32_t*>(s);
+  };
   v4f acc[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = v4f{0.f, 0.f, 0.f, 0.f};
-  auto fragment = [](const uint8_t* q) {
-    const Word4 lo = *reinterpret_cast<const Word4*>(q), hi = *reinterpret_cast<const Word4*>(q + 64);
-    return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  Word4* const own = units[wave];
+  const int to = of8 * 8 + ((lane & 7) ^ of8), lo = row * 8 + (part ^ (row & 7)), hi = row * 8 + (part ^ 4 ^ (row & 7));
+  // nothing is reordered across this for the compiler; a wave's accesses to LDS are done in order
+  auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); };
+  auto fragment = [&](int tile) {
+    const Word4 l = own[tile * 128 + lo], h = own[tile * 128 + hi];
+    return v8i{(int)l[0], (int)l[1], (int)l[2], (int)l[3], (int)h[0], (int)h[1], (int)h[2], (int)h[3]};
   };
-  for (long kb = wave; kb < p.nb; kb += kRowWaves) {
-    const v8i fb = fragment(b + kb * kBlock8);
-    const int t = sb[kb * p.spb];
+  const int each = (p.nb + kRowWaves - 1) / kRowWaves, last = min(p.nb, (wave + 1) * each);
+  for (int kb = wave * each; kb < last; ++kb) {
+    Block now;
+    load(now, kb);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const v8i fa = fragment(a[i] + kb * kBlock8);
-      const int s = sa[i][kb * p.spa];
+    for (int h = 0; h < 2; ++h) {
+      own[MT * 128 + 64 * h + to] = now.b[h];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) own[i * 128 + 64 * h + to] = now.a[2 * i + h];
+    }
+    in_order();
+    const v8i fb = fragment(MT);
+    const int t = (int)now.sb;
+    for_each_index([&](auto index) {
+      constexpr int i = decltype(index)::value;
+      const v8i fa = fragment(i);
       if constexpr (WIDE) {
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FA>(fa[2 * q], fa[2 * q + 1], code_scale(s)),
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FA>(fa[2 * q], fa[2 * q + 1], code_scale(now.sa >> 8 * i & 255)),
                                                           widen8<FB>(fb[2 * q], fb[2 * q + 1], code_scale(t)), acc[i], 0, 0, 0);
       } else {
-        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[i], FA, FB, 0, s, 0, t);
+        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[i], FA, FB, i, (int)now.sa, 0, t);
       }
-    }
+    }, std::make_integer_sequence<int, MT>());
+    in_order();
   }
+  auto sums = [&](int w, int i) -> v4f* { return reinterpret_cast<v4f*>(units[w]) + i * 64 + lane; };
 #pragma unroll
-  for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+  for (int i = 0; i < MT; ++i) *sums(wave, i) = acc[i];
   __syncthreads();
   if (wave >= MT) return;
-  v4f v = sums[0][wave][lane];
+  v4f v = *sums(0, wave);
 #pragma unroll
-  for (int w = 1; w < kRowWaves; ++w) v += sums[w][wave][lane];
+  for (int w = 1; w < kRowWaves; ++w) v += *sums(w, wave);
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const long y = m0 + 16 * wave + 4 * part + r;
+    const long y = m0 + MT * (4 * part + r) + wave;
     const float f[1] = {v[r]};
     if (y < p.m) store_results<1>(p, 0, y, n0 + row, f);
   }

@@ -21,8 +21,9 @@ constexpr int kProductSlices = 64;
 constexpr long kProductGrid = 1L << 22;  // workgroups of a launch, of 512 threads at most; 2^32 results are at most 2^21 128-tiles and a few
 
 // What a model of the measured times makes cheapest, in microseconds.
-//   Rows: eight blocks take a compute unit by the rows that they read, not by their products; 64 x 4096 x 4096 12.2 (128-tiles in four slices 13.2), 129 x 1001 x 515 7.2 (14.0),
-//   128 x 4096 x 4096 21.4 (15.2 in two slices).
+//   Rows: a round of workgroups, and in it eight blocks, or the memory they come from.  With few workgroups fewer rows each give more of
+//   them: 64 x 512 x 4096 4.2 by sixteens, 6.4 by 64.  64 x 4096 x 4096 7.1 (128-tiles in four slices 13.2), 128 x 4096 x 4096 10.3 (15.8),
+//   256 x 4096 x 4096 20.2 (20.8), 512 x 4096 x 1024 15.4 (10.3).
 //   128-tiles: a step of a workgroup that has a compute unit to itself, and of two that share one; 2048 x 4096 x 4096 37 (256-tiles 50),
 //   43264 x 384 x 384 19 (26), 256 x 9216 x 4096 in four slices 24 (one 51, eight 25); with four stages, where a workgroup is alone,
 //   22, 256 x 4096 x 9216 26 -> 21, but 2048 x 4096 x 4096 37 -> 46.
@@ -36,7 +37,7 @@ inline ProductPlan product_plan(long m, long n, long k, bool wide) {
   double least = 1e300;
   auto consider = [&](int kind, int mt, long tm, long tn, long slices, bool deep, double us) {
     if (tm > kProductGrid || tn > kProductGrid || tm * tn * slices > kProductGrid) return;
-    if (slices > 1) us += 4 + slices * (0.3 + 4.0 * m * n / 4e6);
+    if (slices > 1) us += 3.5 + slices * ((slices > 8 && m * n < 1 << 18 ? 0.02 : 0.15) + 4.0 * m * n / 4e6);
     if (us >= least) return;
     least = us;
     best.kind = kind;
@@ -47,10 +48,11 @@ inline ProductPlan product_plan(long m, long n, long k, bool wide) {
     best.slices = (int)slices;
     best.steps = (int)tiles(nb, slices);
   };
-  {
-    const int mt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-    const double busy = std::max(1.0, (double)tiles(m, 16 * mt) * tiles(n, 16) / 256), block = mt == 1 ? 0.33 : mt == 2 ? 0.85 : 2.05;
-    consider(PRODUCT_ROWS, mt, tiles(m, 16 * mt), tiles(n, 16), 1, false, 5 + tiles(nb, 8) * block * busy);
+  const double turns = nb < 8 ? nb / 8.0 : (double)tiles(nb, 8), memory = (8.0 * m + n) * nb * 128 / 5e6;  // a is fetched by each die
+  for (int mt = 1; mt <= (m > 32 ? 4 : m > 16 ? 2 : 1); mt *= 2) {
+    const double rounds = (double)tiles(tiles(m, 16 * mt) * tiles(n, 16), 256);
+    const double block = mt == 1 ? (wide ? 0.36 : 0.29) : mt == 2 ? (wide ? 0.6 : 0.45) : wide ? 1.2 : 0.95;
+    consider(PRODUCT_ROWS, mt, tiles(m, 16 * mt), tiles(n, 16), 1, false, 2.3 + std::max(memory, rounds * (0.6 + turns * block)));
   }
   for (long want = 1; want <= std::min<long>(nb, kProductSlices); want += 1 + want / 8) {
     const long steps = tiles(nb, want), slices = tiles(nb, steps);

@@ -10,10 +10,11 @@ BLOCK = 128
 PRODUCT_SIZES = [
     (1, 1, 1), (1, 16, 128), (1, 1000, 2304), (2, 17, 129), (15, 3, 64), (16, 130, 1152), (17, 33, 1025), (32, 48, 256), (33, 100, 1280),
     (63, 65, 127), (64, 16, 4096), (65, 7, 1000), (129, 515, 1001), (128, 128, 128), (200, 130, 5000), (300, 1000, 260), (1000, 65, 640),
-    (65, 4096, 130), (148, 362, 4354), (591, 897, 900), (584, 498, 1037), (482, 673, 1166), (775, 452, 1293), (65, 62, 8306), (64, 65, 16441),
-    (63, 64, 19354), (16390, 1030, 129), (4000, 4090, 257), (3900, 4096, 1100), (1700, 2340, 5300)]
+    (65, 4096, 130), (257, 4149, 131), (259, 4129, 67), (770, 1250, 1188), (1485, 41, 3733), (41, 41, 37486), (4399, 40, 951), (4204, 40, 1039),
+    (4026, 40, 1188), (3935, 40, 1282), (40, 41, 42430), (41, 41, 41627), (642, 776, 4320), (609, 618, 7298), (656, 516, 10255), (16390, 1030, 129),
+    (4000, 4090, 257), (3900, 4096, 1100), (1700, 2340, 5300)]
 # and those for every pair of codes and kinds of blocks
-PRODUCT_KINDS = [(5, 40, 700), (20, 40, 300), (100, 300, 1300), (581, 2154, 184), (591, 897, 900), (200, 130, 5000), (4000, 4090, 200)]
+PRODUCT_KINDS = [(5, 40, 700), (20, 40, 300), (129, 515, 300), (300, 1000, 260), (257, 4149, 131), (4204, 40, 1039), (40, 41, 42430), (4000, 4090, 200)]
 TOP = {torch.float8_e4m3fn: 448.0, torch.float8_e5m2: 57344.0}
 HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 # half the distance of neighbours among the smallest numbers

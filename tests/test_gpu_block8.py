@@ -141,7 +141,7 @@ def test_product_of_all_kinds(lib, m, n, k, ca, cb, sa, sb):
         close(lib.block8_product(a, b, dtype), va, vb, dtype)
 
 
-@pytest.mark.parametrize("m,n", [(3, 21), (50, 21), (581, 2154), (4000, 4090)])
+@pytest.mark.parametrize("m,n", [(3, 21), (129, 515), (300, 1000), (581, 2154), (4000, 4090)])
 def test_every_code_under_many_scales(lib, m, n):
     """Operands of any bytes, not of packing alone."""
     k = 384
@@ -159,7 +159,7 @@ def test_every_code_under_many_scales(lib, m, n):
         assert np.array_equal(f64(lib.block8_unpack(a)), va.astype(np.float32).astype(np.float64))
 
 
-@pytest.mark.parametrize("m,n,k", [(9, 20, 300), (130, 70, 30000), (581, 2154, 184), (591, 897, 900), (4000, 4090, 128)])
+@pytest.mark.parametrize("m,n,k", [(9, 20, 300), (129, 515, 1001), (300, 1000, 260), (257, 4149, 131), (4204, 40, 1039), (642, 776, 4320), (4000, 4090, 128)])
 def test_product_writes_its_result_and_nothing_else(lib, m, n, k):
     a, b, va, vb = product_case(lib, m, n, k, torch.bfloat16, E4M3, E4M3, False, True)
     room = torch.full((m + 2, n + 11), 7.0, dtype=torch.bfloat16, device="cuda")
@@ -201,7 +201,7 @@ def test_a_layer_and_its_gradients(lib):
 
 def test_captured_and_replayed(lib):
     """Packing and products of every kind in one graph over static buffers, replayed with other inputs, eager work between."""
-    sizes = [(3, 200, 300), (130, 140, 26000), (4000, 4090, 130)]
+    sizes = [(3, 200, 300), (642, 776, 4320), (4000, 4090, 130)]
     xs = [matrix(m, k).cuda() for m, n, k in sizes]
     ws = [matrix(n, k).cuda() for m, n, k in sizes]
 
