@@ -4,9 +4,10 @@
 // + 7: a row's block is sixteen neighbouring lanes and a column's the same lanes of all waves, so both kinds of scales and of
 // codes come from one read.  Of the transpose a thread has eight codes of each of its columns as two words (the conversion takes
 // two values to a word, which here are two rows); they go through LDS to be stored as whole lines.
-// 4096 x 9216 float32 to square blocks both ways 50 us (4.5 TB/s), 43264 x 384 bf16 both ways 16 (4.1 TB/s), 256 x 9216 bf16 both ways, which is
-// 144 workgroups, 9: the eight loads of a thread on their way together, before that 13.
+// 4096 x 9216 float32 to square blocks both ways 50 us (4.5 TB/s), 43264 x 384 bf16 both ways 13.5 (4.9 TB/s), 256 x 9216 bf16, which is
+// 144 workgroups, 5.1: the eight loads of a thread are on their way together.
 #include <algorithm>
+#include <type_traits>
 
 #include "blocks8.h"
 #include "kernels.h"
@@ -22,9 +23,126 @@ struct Pack8Args {
   long pitch, spitch, pitch_t, spitch_t;
 };
 
+// A thread's 8 x 8 of a matrix: what its blocks' scales and codes are made of
+template <typename T>
+struct Patch {
+  float v[8][8];
+  __device__ __forceinline__ void take(int i, const Eight<T>& raw, bool on) {
+    raw.widen(v[i]);
+    if (!on)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+  }
+  // the largest magnitudes, as the bits of a float32: of rows over their block's sixteen lanes, of columns over all of the workgroup
+  __device__ __forceinline__ void rows_most(uint32_t* of_row) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = max(m, magnitude_bits(v[i][j]));
+      of_row[i] = max_of_16(m);
+    }
+  }
+  __device__ __forceinline__ void columns_most(uint32_t* of_col, uint32_t (*most)[128]) const {
+    const int t = threadIdx.x, tc = t & 15;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, magnitude_bits(v[i][j]));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+      of_col[j] = max(m, (uint32_t)__shfl_xor((int)m, 32));
+    }
+    if ((t & 48) == 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most[t >> 6][8 * tc + j] = of_col[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int c = 8 * tc + j;
+      of_col[j] = max(max(most[0][c], most[1][c]), max(most[2][c], most[3][c]));
+    }
+  }
+  template <int CODE>
+  __device__ __forceinline__ Word2 row(int i, uint32_t s) const {
+    return floats_to_codes<CODE, 8>(v[i], s);
+  }
+  template <int CODE>
+  __device__ __forceinline__ Word2 column(int j, uint32_t s) const {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = v[i][j];
+    return floats_to_codes<CODE, 8>(f, s);
+  }
+};
+// 16 bits: two values to a word throughout, which is half the work and half the registers (43264 x 384 both ways 16.2 -> 13.5 us,
+// 256 x 9216 6.2 -> 5.1)
+template <typename T>
+struct Patch16 {
+  uint32_t v[8][4];
+  __device__ __forceinline__ void take(int i, const Eight<T>& raw, bool on) {
+    const Word4 w = __builtin_bit_cast(Word4, raw.r);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[i][j] = w[j];
+    if (!on)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i][j] = 0;
+  }
+  static __device__ __forceinline__ uint32_t bits(uint32_t magnitude) { return __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(T, (unsigned short)magnitude)); }
+  __device__ __forceinline__ void rows_most(uint32_t* of_row) const {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      uint32_t m[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        m[k] = max_halves(max_halves(v[i + k][0] & 0x7fff7fffu, v[i + k][1] & 0x7fff7fffu), max_halves(v[i + k][2] & 0x7fff7fffu, v[i + k][3] & 0x7fff7fffu));
+      const uint32_t both = max_halves_of_16(max_halves(__builtin_amdgcn_perm(m[1], m[0], 0x05040100u), __builtin_amdgcn_perm(m[1], m[0], 0x07060302u)));
+      of_row[i] = bits(both & 0xffffu);
+      of_row[i + 1] = bits(both >> 16);
+    }
+  }
+  __device__ __forceinline__ void columns_most(uint32_t* of_col, uint32_t (*most)[128]) const {
+    const int t = threadIdx.x, tc = t & 15;
+    uint32_t m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[j] = max_halves(m[j], v[i][j] & 0x7fff7fffu);
+      m[j] = max_halves(m[j], (uint32_t)__shfl_xor((int)m[j], 16));
+      m[j] = max_halves(m[j], (uint32_t)__shfl_xor((int)m[j], 32));
+    }
+    if ((t & 48) == 0) *reinterpret_cast<Word4*>(&most[t >> 6][4 * tc]) = Word4{m[0], m[1], m[2], m[3]};
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const Word4 o = *reinterpret_cast<const Word4*>(&most[w][4 * tc]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m[j] = max_halves(m[j], o[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      of_col[2 * j] = bits(m[j] & 0xffffu);
+      of_col[2 * j + 1] = bits(m[j] >> 16);
+    }
+  }
+  template <int CODE>
+  __device__ __forceinline__ Word2 row(int i, uint32_t s) const {
+    return eight_codes<CODE, T>(v[i], s);
+  }
+  template <int CODE>
+  __device__ __forceinline__ Word2 column(int j, uint32_t s) const {
+    uint32_t f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+    return eight_codes<CODE, T>(f, s);
+  }
+};
+
 template <typename T, int CODE, bool SQUARE, bool ROWS, bool COLS>
 __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
-  __shared__ uint32_t most[4][128];  // of the columns, wave by wave
+  __shared__ __attribute__((aligned(16))) uint32_t most[4][128];  // of the columns, wave by wave
   __shared__ Word4 turned[COLS ? 1024 : 1];
   const int t = threadIdx.x, tr = t >> 4, tc = t & 15, wave = t >> 6;
   const long rb = blockIdx.x / a.across, cb = blockIdx.x - rb * a.across;
@@ -38,31 +156,16 @@ __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) raw[i].load((const T*)a.x + min(row0 + i, a.rows - 1) * a.ld + col0, a.cols - col0);
   }
-  float v[8][8];
+  typename std::conditional<sizeof(T) == 2, Patch16<T>, Patch<T>>::type patch;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    raw[i].widen(v[i]);
-    if (row0 + i >= a.rows)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-  }
+  for (int i = 0; i < 8; ++i) patch.take(i, raw[i], row0 + i < a.rows);
 
   uint32_t of_row[8], of_col[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) of_row[i] = of_col[i] = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t m = magnitude_bits(v[i][j]);
-      if (ROWS || SQUARE) of_row[i] = max(of_row[i], m);
-      if (COLS && !SQUARE) of_col[j] = max(of_col[j], m);
-    }
+  if constexpr (ROWS || SQUARE) patch.rows_most(of_row);
   if constexpr (SQUARE) {
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, of_row[i]);
-    m = max_of_16(m);
     m = max(m, (uint32_t)__shfl_xor((int)m, 16));
     m = max(m, (uint32_t)__shfl_xor((int)m, 32));
     if ((t & 63) == 0) most[wave][0] = m;
@@ -78,7 +181,7 @@ __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
   } else {
     if constexpr (ROWS) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) of_row[i] = row0 + i < a.rows ? scale_code<CODE>(max_of_16(of_row[i])) : 0;
+      for (int i = 0; i < 8; ++i) of_row[i] = row0 + i < a.rows ? scale_code<CODE>(of_row[i]) : 0;
       if (tc == 0) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -88,22 +191,9 @@ __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
       }
     }
     if constexpr (COLS) {
+      patch.columns_most(of_col, most);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        uint32_t m = of_col[j];
-        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-        of_col[j] = max(m, (uint32_t)__shfl_xor((int)m, 32));
-      }
-      if ((t & 48) == 0) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) most[wave][8 * tc + j] = of_col[j];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = 8 * tc + j;
-        of_col[j] = col0 + j < a.cols ? scale_code<CODE>(max(max(most[0][c], most[1][c]), max(most[2][c], most[3][c]))) : 0;
-      }
+      for (int j = 0; j < 8; ++j) of_col[j] = col0 + j < a.cols ? scale_code<CODE>(of_col[j]) : 0;
       if (tr == 0) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -116,19 +206,14 @@ __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
   if constexpr (ROWS) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (row0 + i < a.rows) *reinterpret_cast<Word2*>(a.codes + (row0 + i) * a.pitch + col0) = floats_to_codes<CODE, 8>(v[i], of_row[i]);
+      if (row0 + i < a.rows) *reinterpret_cast<Word2*>(a.codes + (row0 + i) * a.pitch + col0) = patch.template row<CODE>(i, of_row[i]);
   }
   if constexpr (COLS) {
     // column 8 tc + j: 128 bytes, of which this thread has unit tr of eight; units are shifted about by tc so that the lanes of a
     // store and those of a load spread over all banks
     Word2* const unit = reinterpret_cast<Word2*>(turned);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float f[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = v[i][j];
-      unit[(8 * tc + j) * 16 + (tr ^ tc)] = floats_to_codes<CODE, 8>(f, of_col[j]);
-    }
+    for (int j = 0; j < 8; ++j) unit[(8 * tc + j) * 16 + (tr ^ tc)] = patch.template column<CODE>(j, of_col[j]);
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 4; ++k) {

@@ -6,6 +6,8 @@
 // has a tail along its sum.  Scales lie block by block along the rows of the matrix, so that a lane that works on four
 // neighbouring rows gets theirs as one word, which the instruction picks its byte from.
 #pragma once
+#include <type_traits>
+
 #include "codes8.h"
 
 namespace ax {
@@ -75,5 +77,49 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t m) {
   m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x141, 0xf, 0xf, false));  // the other four of eight
   return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x140, 0xf, 0xf, false));  // the other eight
 }
+// The same of two 16-bit values in a word each
+typedef unsigned short Halves __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(Halves, a), __builtin_bit_cast(Halves, b)));
+}
+__device__ __forceinline__ uint32_t max_halves_of_16(uint32_t m) {
+  m = max_halves(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xf, 0xf, false));
+  m = max_halves(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xf, 0xf, false));
+  m = max_halves(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x141, 0xf, 0xf, false));
+  return max_halves(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x140, 0xf, 0xf, false));
+}
 __device__ __forceinline__ uint32_t magnitude_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+
+// Eight codes of words with two values of type T each, under a scale code that scale_code() gave: the instruction divides by the power of
+// two, exactly, and rounds to nearest even, as floats_to_codes() does.
+typedef short Short2 __attribute__((ext_vector_type(2)));
+template <int CODE, bool HIGH, typename T>
+__device__ __forceinline__ Short2 two_codes(Short2 w, uint32_t both, float scale) {
+  typedef T Two __attribute__((ext_vector_type(2)));
+  const Two v = __builtin_bit_cast(Two, both);
+  if constexpr (std::is_same<T, __bf16>::value) {
+    if constexpr (CODE == ALEXNET_CODE_E4M3)
+      return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, v, scale, HIGH);
+    else
+      return __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(w, v, scale, HIGH);
+  } else {
+    if constexpr (CODE == ALEXNET_CODE_E4M3)
+      return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, v, scale, HIGH);
+    else
+      return __builtin_amdgcn_cvt_scalef32_pk_bf8_f16(w, v, scale, HIGH);
+  }
+}
+template <int CODE, typename T>
+__device__ __forceinline__ Word2 eight_codes(const uint32_t* v, uint32_t s) {
+  const float scale = code_scale(s);
+  Word2 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    Short2 w = {0, 0};
+    w = two_codes<CODE, false, T>(w, v[2 * h], scale);
+    w = two_codes<CODE, true, T>(w, v[2 * h + 1], scale);
+    r[h] = s == 255 ? 0u : __builtin_bit_cast(uint32_t, w);
+  }
+  return r;
+}
 }  // namespace ax

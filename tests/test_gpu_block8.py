@@ -83,6 +83,22 @@ def test_infinities_and_nans_mark_their_block(lib, bad, square):
     assert torch.equal(y, want.any(1)[:, None].expand(260, 70))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("code", CODES, ids=str)
+@pytest.mark.parametrize("square", [False, True], ids=["rows", "square"])
+def test_every_16_bit_number_packs_as_its_float32_does(lib, dtype, code, square):
+    """Sorted, so that blocks are of neighbours, and shuffled with the largest ones left out of most blocks."""
+    numbers = torch.arange(-2**15, 2**15, dtype=torch.int32).to(torch.int16)
+    order = torch.randperm(2**16, generator=torch.Generator().manual_seed(5))
+    for x in (numbers, numbers[order], numbers[torch.argsort(numbers.view(dtype).float().abs() // 1 + order % 7)]):
+        x = x.view(dtype).view(512, 128)
+        for got, want in zip(lib.block8_pack(x.cuda(), code, square, "both"), lib.block8_pack(x.cuda().float(), code, square, "both")):
+            assert torch.equal(got.codes.view(torch.uint8), want.codes.view(torch.uint8)) and torch.equal(got.scales, want.scales)
+    # and the float32's are the definition's
+    by_rows, by_columns = lib.block8_pack(x.cuda().float(), code, square, "both")
+    assert same(by_rows, R.pack(f64(x), code, square)) and same(by_columns, R.pack(f64(x).T, code, square))
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_strided_and_unaligned(lib, dtype):
     wide = matrix(70, 333, dtype, spread=4).cuda()
