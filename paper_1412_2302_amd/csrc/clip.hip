@@ -29,7 +29,7 @@ struct ClipArgs {
   float* norm;
   int count, chunks, first_part, parts;  // parts: of all launches
   float max_norm;
-  int in_place;
+  int in_place, pass_by;
 };
 static_assert(sizeof(ClipArgs) <= 4096, "kernel arguments");
 
@@ -58,7 +58,7 @@ __device__ __forceinline__ void over_chunks(const ClipArgs& a, int c0, int c1, b
 }
 
 // f(values, of which so many are the tensor's, place) of a thread's 16 bytes at a time: of a whole chunk all loads are on their way at once,
-// and neighbouring lanes have neighbouring bytes (with 32 of them a lane a store writes half lines: 61 M float32 values 95 -> 73 us)
+// and neighbouring lanes have neighbouring bytes (with 32 of them a lane a store writes half lines, which past the cache costs: 61 M float32 values 95 -> 73 us)
 template <typename T, typename F>
 __device__ __forceinline__ void over_vectors(const T* in, long n, F f) {
   constexpr int V = 16 / sizeof(T), kStep = 256 * V, kVectors = kClipChunk / kStep;
@@ -124,16 +124,19 @@ __global__ void __launch_bounds__(256) clip_norm_kernel(ClipArgs a) {
   if (threadIdx.x == 0) *a.norm = (float)norm;
 }
 
-// A result that goes elsewhere passes the cache by, which keeps what of the gradients is in it (61 M float32 values: 102 -> 73 us).
+// Results that go elsewhere pass the last-level cache by where the gradients alone fill a good part of it: these are then still there for
+// this pass.  61 M float32 values 140 -> 112 us, with a pass over the results behind it 271 -> 259; 120 M bf16 142 -> 115 and 270 -> 256.  Of
+// fewer values the results are found there afterwards: 20 M float32 with such a pass 75 us, 77 past the cache, 40 M 181 and 172.
+constexpr double kPassBy = 100e6;  // bytes of gradients
 template <int V, typename T>
-__device__ __forceinline__ void store_vector(const T* in, T* out, int has, const float* v) {
+__device__ __forceinline__ void store_vector(const T* in, T* out, int has, const float* v, bool pass_by) {
   typedef typename Pack<T, V>::Raw Raw;
   typedef Raw Anywhere __attribute__((aligned(sizeof(T))));
   if (has < V) {
 #pragma unroll
     for (int e = 0; e < V; ++e)
       if (e < has) out[e] = (T)v[e];
-  } else if (in == out) {
+  } else if (in == out || !pass_by) {
     Pack<T, V>::store(out, v);
   } else {
     Raw r;
@@ -156,7 +159,7 @@ __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a) {
     over_vectors(in, n, [&](float* v, auto vector, int has, int i) {
 #pragma unroll
       for (int e = 0; e < decltype(vector)::value; ++e) v[e] = (float)((double)v[e] * factor);
-      store_vector<decltype(vector)::value>(in + i, out + i, has, v);
+      store_vector<decltype(vector)::value>(in + i, out + i, has, v, a.pass_by);
     });
   });
 }
@@ -234,6 +237,7 @@ static int clip_call(const char* who, int count, const void* const* grads, void*
   a.in_place = !outs;
   double bytes = 0;
   for (int i = 0; i < count; ++i) bytes += (double)sizes[i] * type_size(types[i]);
+  a.pass_by = bytes > kPassBy;
   {
     KernelScope ks("clip_squares", 2.0 * p.values, bytes, st);
     AX_TRY(clip_launches(count, grads, outs, sizes, types, p, a, [&](dim3 grid) {

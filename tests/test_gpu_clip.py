@@ -55,6 +55,21 @@ def test_norm_and_clipping(lib, sizes, seed):
         assert all(torch.equal(a, b) for a, b in zip(mixed, out))
 
 
+def test_many_values_at_any_alignment(lib):
+    """Results past the cache, not aligned to more than their elements, with neighbours that stay as they are."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    whole = [torch.randn(n, generator=gen, device="cuda").to(t) for n, t in ((30000001, torch.float32), (9000013, torch.bfloat16), (8195, torch.float16))]
+    grads = [w[1 + k:-1] for k, w in enumerate(whole)]
+    rooms = [torch.full_like(w, 7.0) for w in whole]
+    out = [r[3 - k:][:len(g)] for k, (r, g) in enumerate(zip(rooms, grads))]
+    grads = [g[:len(o)] for g, o in zip(grads, out)]
+    want = norm64(grads)
+    assert abs(lib.clip_gradients(grads, float(want) / 3, out=out).item() - want) <= 1.01 * EPS32 * want
+    check(out, grads, float(np.float32(want / 3)) / want)
+    for k, (r, o) in enumerate(zip(rooms, out)):
+        assert (r[:3 - k] == 7).all() and (r[3 - k + len(o):] == 7).all()
+
+
 def test_far_from_one(lib):
     """Squares past float32's range, on either side."""
     for size in (1e30, 1e-30, 1e-44):
