@@ -316,9 +316,9 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu
     load(stage(i), decltype(i)::value);
     s[decltype(i)::value] = scales();
   }, std::make_integer_sequence<int, STAGES - 1>());
+  load(stage(std::integral_constant<int, STAGES - 1>()), STAGES - 1);
   arrived(s[0]);
   meet();
-  load(stage(std::integral_constant<int, STAGES - 1>()), STAGES - 1);
   a[0] = fragment_a(stage0, 0);
   a[1] = fragment_a(stage0, 1);
 #pragma unroll
