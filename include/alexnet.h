@@ -503,9 +503,10 @@ int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* 
  * y goes to d_y, rounded once to TYPE, or to `blocks` (not square) as an operand of a
  * product; the other of the two is null.  d_gamma [cols] may be null (1), as may d_rstd [rows], which
  * receives r.  ld_* are row strides in elements (>= cols).  y and sum may each take the place of x or
- * residual (same pointer and stride).  Sums are float32: r is 0, and y with it, where the squares of a row add up past
- * 3.4 * 10^38.  A row with an infinity or a NaN has NaN somewhere in y, and as blocks no finite value in
- * the blocks that it has them in.  At most 2^24 rows and 2^20 columns; rows may be 0. */
+ * residual (same pointer and stride).  Sums are float32, and where a row's squares add up past its
+ * range they are taken again of smaller numbers.  A row with an infinity or a NaN has NaN somewhere in y,
+ * and as blocks no finite value in the blocks that it has them in.  At most 2^24 rows and 2^20 columns;
+ * rows may be 0. */
 int alexnet_rms_norm_forward(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, int32_t type,
                              int64_t rows, int64_t cols, float eps, const float* d_gamma, void* d_sum, int64_t ld_sum,
                              void* d_y, int64_t ld_y, const alexnet_blocks8_t* blocks, float* d_rstd, void* stream);

@@ -60,10 +60,20 @@ __device__ __forceinline__ void get_s(const RmsArgs& a, long row, int col, float
   }
 }
 
+// 1 / sqrt(mean(s^2) + eps) of the team's row from each lane's squares.  Where they add up past float32's range, again(f) gives those of f s;
+// eps is nothing beside them then.  An infinity among s stays one, and makes NaN of its y.
+template <int TEAM, typename F>
+__device__ __forceinline__ float row_rstd(const RmsArgs& a, float squares, float (*cross)[16], F again) {
+  const float total = team_sum<TEAM>(squares, cross[0]);
+  if (total < __builtin_inff()) return 1.f / sqrtf(total / (float)a.cols + a.eps);
+  const float less = team_sum<TEAM>(again(0x1p-100f), cross[1]);
+  return 0x1p-100f / sqrtf(less / (float)a.cols);
+}
+
 template <typename T, int CODE, int TEAM, int NV>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256) rms_norm_kernel(RmsArgs a) {
   constexpr int kTeams = TEAM > 256 ? 1 : 256 / TEAM;
-  __shared__ float cross[16];
+  __shared__ float cross[2][16];
   const int t = threadIdx.x % TEAM;
   const long row = group_of_rows() * kTeams + threadIdx.x / TEAM;
   if (row >= a.rows) return;  // a whole team
@@ -81,7 +91,14 @@ __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256) rms_norm_kernel(RmsAr
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(s[i][e], s[i][e], squares);
-    const float rstd = 1.f / sqrtf(team_sum<TEAM>(squares, cross) / (float)a.cols + a.eps);
+    const float rstd = row_rstd<TEAM>(a, squares, cross, [&](float f) {
+      float less = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) less = __builtin_fmaf(s[i][e] * f, s[i][e] * f, less);
+      return less;
+    });
     if (t == 0 && a.rstd_out) a.rstd_out[row] = rstd;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -98,10 +115,20 @@ __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256) rms_norm_kernel(RmsAr
       for (int e = 0; e < 8; ++e) one = __builtin_fmaf(s[e], s[e], one);
       squares += one;
     }
-    const float rstd = 1.f / sqrtf(team_sum<TEAM>(squares, cross) / (float)a.cols + a.eps);
-    if (t == 0 && a.rstd_out) a.rstd_out[row] = rstd;
     // each lane reads back what it has written itself
     const T* const from = a.residual ? (const T*)a.sum + row * a.ld_sum : (const T*)a.x + row * a.ld_x;
+    const float rstd = row_rstd<TEAM>(a, squares, cross, [&](float f) {
+      float less = 0.f;
+      for (int v = t; 8 * v < a.cols; v += TEAM) {
+        float s[8], one = 0.f;
+        load8(from + 8 * v, a.cols - 8 * v, s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) one = __builtin_fmaf(s[e] * f, s[e] * f, one);
+        less += one;
+      }
+      return less;
+    });
+    if (t == 0 && a.rstd_out) a.rstd_out[row] = rstd;
     for (int v = t; v < (a.vecs + 15) / 16 * 16; v += TEAM) {
       float s[8];
       load8(from + 8 * v, a.cols - 8 * v, s);

@@ -225,3 +225,18 @@ def test_on_another_stream(lib):
     here = lib.rms_norm_forward(x, gamma, residual, EPS)
     assert all(torch.equal(p, q) for p, q in zip((y, s, rstd), here))
     assert all(torch.equal(p, q) for p, q in zip((dx, dgamma), lib.rms_norm_backward(s, dy, rstd, gamma, dsum)))
+
+
+@pytest.mark.parametrize("cols", [1, 8, 129, 384, 777, 1024, 2049, 8192, 20000, 65536, 70001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_squares_past_float32(lib, cols, dtype):
+    """Rows of numbers from 2^55 to just under 2^128, among ordinary ones."""
+    gen = torch.Generator().manual_seed(cols)
+    x = (torch.rand((37, cols), generator=gen) + 0.5) * torch.where(torch.rand((37, cols), generator=gen) < 0.5, -1.0, 1.0)
+    x = (x * torch.exp2(torch.tensor([0.0, 55, 60, 63, 64, 65, 100, 126, 127] * 5)[:37, None] * 0.999)).to(dtype)
+    assert x.isfinite().all()
+    gamma = torch.rand(cols, generator=gen) + 0.5
+    want, _, _ = check_forward(lib.rms_norm_forward(x.cuda(), gamma.cuda(), None, EPS), x, None, gamma, dtype)
+    y = lib.block8_unpack(lib.rms_norm_forward(x.cuda(), gamma.cuda(), None, EPS, blocks=torch.float8_e4m3fn)[0])
+    # eight steps of a code to each power of two
+    within(y, want, np.abs(want) * 2.0 ** -4 + R.norm_tolerance(want, cols) * 2 + np.abs(want).max(1, keepdims=True) * 2.0 ** -17)
