@@ -489,9 +489,11 @@ int alexnet_block8_unpack(const alexnet_blocks8_t* in, int64_t rows, int64_t col
  * makes of some just under it, count as infinities).  For BF16 and FP16 eight products at
  * a time are added with 13 bits under the largest of them, those sums in float32:
  * off by at most 7 * 2^-13 of what each eight's largest add up to, 1.5e-5 of a result of
- * normal numbers.  Results repeat bit for bit.  k = 0 gives
+ * normal numbers, more of one that large products cancel in; ALEXNET_TYPE_BF16 + ALEXNET_SUMS_FP32 and
+ * ALEXNET_TYPE_FP16 + ALEXNET_SUMS_FP32 ask for sums as FP32 has them, at half the rate.  Results repeat bit for bit.  k = 0 gives
  * zeros.  Codes and scales may be any bytes.  At most 2^28 rows of either, 2^22
  * columns and 2^32 results. */
+#define ALEXNET_SUMS_FP32 16 /* added to the type of a product's result */
 int alexnet_block8_product_query(int64_t m, int64_t n, int64_t k, int32_t type, size_t* workspace_bytes);
 int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* b, int64_t m, int64_t n, int64_t k,
                            void* d_y, int64_t ld_y, int32_t type, void* d_workspace, size_t workspace_bytes,

@@ -994,11 +994,16 @@ def _block8_product_ws(m: int, n: int, k: int, kind: int) -> int:
     return ws.value
 
 
+_SUMS_FP32 = 16
+
+
 def block8_product(a: Blocks8, b: Blocks8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
-                   stream=None) -> torch.Tensor:
+                   stream=None, full_sums: bool = False) -> torch.Tensor:
     """y [m][n] = a b^T of a [m][k] and b [n][k] in float32, bfloat16 or float16.  With w [out][in] a dense layer's forward pass is
     block8_product(x, w), the gradient of x block8_product(dy, w along columns), that of w block8_product(dy along columns, x
-    along columns).  out: where y goes."""
+    along columns).  out: where y goes.  full_sums: a 16-bit result's sums are float32 throughout, as a float32 result's always are,
+    at half the rate; otherwise products are added by eights with 13 bits under the largest of the eight, 1.5e-5 of a result unless
+    large products cancel."""
     Blocks8._need(a, "block8_product: a")
     Blocks8._need(b, "block8_product: b")
     codes = a.codes
@@ -1008,8 +1013,8 @@ def block8_product(a: Blocks8, b: Blocks8, dtype: torch.dtype = torch.bfloat16, 
     if dtype not in _TYPES:
         raise ValueError(f"block8_product: expected float32, bfloat16 or float16, got {dtype}")
     if not _here(codes, stream):
-        return _there(codes, stream, (a, b, out), lambda: block8_product(a, b, dtype, out))
-    m, n, k, kind, device = codes.shape[0], b.codes.shape[0], a.cols, _TYPES[dtype], codes.device
+        return _there(codes, stream, (a, b, out), lambda: block8_product(a, b, dtype, out, full_sums=full_sums))
+    m, n, k, kind, device = codes.shape[0], b.codes.shape[0], a.cols, _TYPES[dtype] + (_SUMS_FP32 if full_sums else 0), codes.device
     y, ld = _make(out, torch.Size((m, n)), dtype, codes, "block8_product: out")
     ws_bytes = _block8_product_ws(m, n, k, kind)
     ws = _scratch_for(ws_bytes, codes)

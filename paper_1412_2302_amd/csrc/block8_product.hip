@@ -1,12 +1,13 @@
 // y [m][n] = a b^T of two operands in 8-bit floating point with power-of-two scales per block of 128 (blocks8.h):
 //   y[i][j] = sum over blocks B of 2^(sa[B][i] + sb[B][j] - 254) * sum over k in B of code_a[i][k] * code_b[j][k]
 //
-// Two kinds of arithmetic, by the type of y.
+// Two kinds of arithmetic, by the type of y and what the caller asks for.
 //   16 bits: the 8-bit matrix instruction, which takes 128 of the sum, a lane's 32 with a scale byte of their own, so that
 //     scales cost the load of a word per block.  It adds eight products at a time with 13 bits under the largest of the
 //     eight (measured; the sums of those eights go on in float32), 1.5e-5 of a result of normal numbers and a hundredth of what
-//     rounding it to bf16 costs, a twentieth to fp16: a choice for twice the rate.
-//   32 bits: codes are widened to bf16 with their scales, which is exact, and go through the bf16 instruction, whose sums are
+//     rounding it to bf16 costs, a twentieth to fp16: a choice for twice the rate (16384 x 4096 x 4096 209 us, 460 the other way).  What is
+//     lost is of the largest product, so that where large products cancel it is more of the result: a caller may ask for the other kind.
+//   32 bits, and 16 with ALEXNET_SUMS_FP32: codes are widened to bf16 with their scales, which is exact, and go through the bf16 instruction, whose sums are
 //     float32 throughout: 6e-8 of a result.
 //
 // Tiles.  Operands go from memory to LDS directly (buffer_load ... lds), a block of 128 at a time: a row of a stage is the 128 bytes
@@ -514,8 +515,8 @@ static int product_launch(const ProductArgs& a, const ProductPlan& p, hipStream_
   return ALEXNET_OK;
 }
 template <int FA, int FB>
-static int product_launch_type(const ProductArgs& a, const ProductPlan& p, hipStream_t st) {
-  return a.type == ALEXNET_TYPE_FP32 ? product_launch<FA, FB, true>(a, p, st) : product_launch<FA, FB, false>(a, p, st);
+static int product_launch_sums(const ProductArgs& a, const ProductPlan& p, bool wide, hipStream_t st) {
+  return wide ? product_launch<FA, FB, true>(a, p, st) : product_launch<FA, FB, false>(a, p, st);
 }
 template <typename T, int TEAM>
 static int product_sum_team(const ProductArgs& a, hipStream_t st) {
@@ -536,8 +537,11 @@ static int product_zero(void* y, long m, long n, long ld, hipStream_t st) {
   return ALEXNET_OK;
 }
 
+// what `type` says of a result, and whether its sums are to be float32 throughout
+static int type_of(int type) { return type & ~ALEXNET_SUMS_FP32; }
+static bool wide_of(int type) { return type_of(type) == ALEXNET_TYPE_FP32 || (type & ALEXNET_SUMS_FP32); }
 static int check_product(const char* who, long m, long n, long k, int type) {
-  AX_REQUIRE(type_ok(type), ALEXNET_EINVAL, "%s: unknown type %d", who, type);
+  AX_REQUIRE(type_ok(type_of(type)), ALEXNET_EINVAL, "%s: unknown type %d", who, type);
   AX_REQUIRE(m >= 0 && m <= 1L << 28 && n >= 0 && n <= 1L << 28 && k >= 0 && k <= 1L << 22 && m * n <= 1L << 32 &&
                  blocks_sizes_ok(m, k) && blocks_sizes_ok(n, k),
              ALEXNET_ESHAPE, "%s: bad sizes, %ld by %ld over %ld (at most 2^28 rows of an operand, 2^22 columns, 2^32 results)", who, m, n, k);
@@ -553,7 +557,7 @@ extern "C" {
 int alexnet_block8_product_query(int64_t m, int64_t n, int64_t k, int32_t type, size_t* workspace_bytes) {
   AX_TRY(check_product("alexnet_block8_product_query", m, n, k, type));
   AX_REQUIRE(workspace_bytes, ALEXNET_EINVAL, "alexnet_block8_product_query: null argument");
-  *workspace_bytes = m && n ? product_plan(m, n, k, type == ALEXNET_TYPE_FP32).ws : 0;
+  *workspace_bytes = m && n ? product_plan(m, n, k, wide_of(type)).ws : 0;
   return ALEXNET_OK;
 }
 
@@ -562,6 +566,8 @@ int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* 
   const char* who = "alexnet_block8_product";
   AX_TRY(check_product(who, m, n, k, type));
   if (m == 0 || n == 0) return ALEXNET_OK;
+  const bool wide = wide_of(type);
+  type = type_of(type);
   AX_REQUIRE(d_y, ALEXNET_EINVAL, "%s: null argument", who);
   AX_REQUIRE(ld_y >= n && ld_y <= 1L << 40, ALEXNET_ESHAPE, "%s: row stride %ld of %ld columns", who, (long)ld_y, (long)n);
   AX_REQUIRE((uintptr_t)d_y % type_size(type) == 0, ALEXNET_EALIGN, "%s: a pointer is not aligned to its elements", who);
@@ -572,7 +578,7 @@ int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* 
                                        : product_zero<_Float16>(d_y, m, n, ld_y, st);
   AX_TRY(check_blocks(a, "a", who));
   AX_TRY(check_blocks(b, "b", who));
-  const ProductPlan p = product_plan(m, n, k, type == ALEXNET_TYPE_FP32);
+  const ProductPlan p = product_plan(m, n, k, wide);
   AX_TRY(check_scratch(who, d_workspace, workspace_bytes, p.ws));
   const long size = (long)type_size(type);
   AX_TRY(check_apart(who,
@@ -606,8 +612,8 @@ int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* 
   {
     KernelScope ks("block8_product", 2.0 * m * n * k, (double)(m + n) * k + (double)m * n * size, st);
     const bool b4 = b->code == ALEXNET_CODE_E4M3;
-    AX_TRY(a->code == ALEXNET_CODE_E4M3 ? (b4 ? product_launch_type<0, 0>(g, p, st) : product_launch_type<0, 1>(g, p, st))
-                                        : (b4 ? product_launch_type<1, 0>(g, p, st) : product_launch_type<1, 1>(g, p, st)));
+    AX_TRY(a->code == ALEXNET_CODE_E4M3 ? (b4 ? product_launch_sums<0, 0>(g, p, wide, st) : product_launch_sums<0, 1>(g, p, wide, st))
+                                        : (b4 ? product_launch_sums<1, 0>(g, p, wide, st) : product_launch_sums<1, 1>(g, p, wide, st)));
   }
   if (p.slices == 1) return ALEXNET_OK;
   return type == ALEXNET_TYPE_FP32   ? product_sum<float>(g, st)
