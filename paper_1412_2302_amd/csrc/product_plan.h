@@ -48,12 +48,6 @@ inline ProductPlan product_plan(long m, long n, long k, bool wide) {
     best.slices = (int)slices;
     best.steps = (int)tiles(nb, slices);
   };
-  const double turns = nb < 8 ? nb / 8.0 : (double)tiles(nb, 8), memory = (8.0 * m + n) * nb * 128 / 5e6;  // a is fetched by each die
-  for (int mt = 1; mt <= (m > 32 ? 4 : m > 16 ? 2 : 1); mt *= 2) {
-    const double rounds = (double)tiles(tiles(m, 16 * mt) * tiles(n, 16), 256);
-    const double block = mt == 1 ? (wide ? 0.36 : 0.29) : mt == 2 ? (wide ? 0.6 : 0.45) : wide ? 1.2 : 0.95;
-    consider(PRODUCT_ROWS, mt, tiles(m, 16 * mt), tiles(n, 16), 1, false, 2.3 + std::max(memory, rounds * (0.6 + turns * block)));
-  }
   for (long want = 1; want <= std::min<long>(nb, kProductSlices); want += 1 + want / 8) {
     const long steps = tiles(nb, want), slices = tiles(nb, steps);
     {
@@ -66,6 +60,20 @@ inline ProductPlan product_plan(long m, long n, long k, bool wide) {
       const double work = (double)tiles(m, 256) * tiles(n, 256) * slices, rounds = (double)(long)((work + 255) / 256);
       consider(PRODUCT_256, 0, tiles(m, 256), tiles(n, 256), slices, false, 3 + rounds * (steps * 1.35 + 10));
     }
+  }
+  // Where sixteen rows or fewer meet as many as fill the chip, memory is what counts, and rows reach its rate. Of operands that no cache holds:
+  // 1 x 16384 x 16384 51 us by rows, 55 to 69 by tiles; 1 x 4096 x 16384 17 and 19 to 26; 16 x 16384 x 16384 58 and 60 to 70;
+  // 4096 x 4096 x 16 6 and 12; 1 x 20000 x 5000 25 and 30 to 36.  Of longer sums an uneven number of workgroups to a compute unit
+  // counts for more, which their costs do not know: 2 x 32768 x 9216 84 and 69, 16 x 30000 x 4200 46 and 33.
+  const bool few = std::min(m, n) <= 16 && tiles(m, 16) * tiles(n, 16) >= 256 && nb <= 192;
+  const double codes = (m + n) * nb * 128 / 5.5e6;
+  if (few) least = std::max(least, codes + (best.slices > 1 ? 6.5 : 3));
+  const double turns = nb < 8 ? nb / 8.0 : (double)tiles(nb, 8);
+  for (int mt = 1; mt <= (m > 32 ? 4 : m > 16 ? 2 : 1); mt *= 2) {
+    const double rounds = (double)tiles(tiles(m, 16 * mt) * tiles(n, 16), 256);
+    const double memory = few ? codes : (8.0 * m + n) * nb * 128 / 5e6;  // a is fetched by each die
+    const double block = mt == 1 ? (wide ? 0.36 : 0.29) : mt == 2 ? (wide ? 0.6 : 0.45) : wide ? 1.2 : 0.95;
+    consider(PRODUCT_ROWS, mt, tiles(m, 16 * mt), tiles(n, 16), 1, false, 2.3 + std::max(memory, rounds * (0.6 + turns * block)));
   }
   best.slab = ((size_t)m * n + 63) & ~(size_t)63;
   best.ws = best.slices > 1 ? best.slices * best.slab * sizeof(float) : 0;
