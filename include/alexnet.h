@@ -487,7 +487,7 @@ int alexnet_block8_unpack(const alexnet_blocks8_t* in, int64_t rows, int64_t col
 /* y [m][n] = a b^T of a [m][k] and b [n][k], rounded once to `type`.  In FP32
  * products are exact and sums float32 (values past float32's range, which packing
  * makes of some just under it, count as infinities).  For BF16 and FP16 eight products at
- * a time are added with 13 bits under the largest of them, those sums in float32:
+ * a time may be added with 13 bits under the largest of them, those sums in float32:
  * off by at most 7 * 2^-13 of what each eight's largest add up to, 1.5e-5 of a result of
  * normal numbers, more of one that large products cancel in; ALEXNET_TYPE_BF16 + ALEXNET_SUMS_FP32 and
  * ALEXNET_TYPE_FP16 + ALEXNET_SUMS_FP32 ask for sums as FP32 has them, at half the rate.  Results repeat bit for bit.  k = 0 gives

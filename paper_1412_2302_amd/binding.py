@@ -1002,7 +1002,7 @@ def block8_product(a: Blocks8, b: Blocks8, dtype: torch.dtype = torch.bfloat16, 
     """y [m][n] = a b^T of a [m][k] and b [n][k] in float32, bfloat16 or float16.  With w [out][in] a dense layer's forward pass is
     block8_product(x, w), the gradient of x block8_product(dy, w along columns), that of w block8_product(dy along columns, x
     along columns).  out: where y goes.  full_sums: a 16-bit result's sums are float32 throughout, as a float32 result's always are,
-    at half the rate; otherwise products are added by eights with 13 bits under the largest of the eight, 1.5e-5 of a result unless
+    at half the rate; otherwise products may be added by eights with 13 bits under the largest of the eight, 1.5e-5 of a result unless
     large products cancel."""
     Blocks8._need(a, "block8_product: a")
     Blocks8._need(b, "block8_product: b")

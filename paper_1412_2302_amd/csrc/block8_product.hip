@@ -355,6 +355,8 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu
 // A wave's blocks lie next to each other in memory (dealt out in turn 1 x 16384 x 16384 51 us instead of 38, which are 7.1 TB/s).  One
 // block at a time: the other waves' loads fill the wait, and with the next block's on their way too 128 x 1000 x 4096 takes 7.2 instead of 6.8.
 // Row r of a goes to tile r % MT, so that a lane has the scales of its tiles next to each other.
+// Of sixteen rows the sums are always float32: memory bounds them either way (16 x 16384 x 16384 57 us by the 8-bit instruction and 58,
+// 1 x 16384 x 16384 51 and 51).  Of 32 and 64 the 8-bit instruction is worth a tenth (64 x 4096 x 4096 9.0 and 10.0).
 constexpr int kRowWaves = 8;
 template <int FA, int FB, bool WIDE, int MT>
 __global__ void __launch_bounds__(64 * kRowWaves) block8_rows_kernel(ProductArgs p) {
@@ -506,7 +508,7 @@ static int product_launch(const ProductArgs& a, const ProductPlan& p, hipStream_
   if (p.kind == PRODUCT_128)
     hipLaunchKernelGGL((block8_tile_kernel<FA, FB, WIDE, 128, 2>), grid, dim3(256), 0, st, a);
   else if (p.mt == 1)
-    hipLaunchKernelGGL((block8_rows_kernel<FA, FB, WIDE, 1>), grid, dim3(64 * kRowWaves), 0, st, a);
+    hipLaunchKernelGGL((block8_rows_kernel<FA, FB, true, 1>), grid, dim3(64 * kRowWaves), 0, st, a);
   else if (p.mt == 2)
     hipLaunchKernelGGL((block8_rows_kernel<FA, FB, WIDE, 2>), grid, dim3(64 * kRowWaves), 0, st, a);
   else

@@ -77,3 +77,12 @@ def test_strides_streams_and_replays(lib):
 def test_nothing_to_add(lib):
     a, b = lib.block8_pack(torch.zeros((0, 70), device="cuda"), along="columns"), lib.block8_pack(torch.zeros((0, 9), device="cuda"), along="columns")
     assert torch.equal(lib.block8_product(a, b, full_sums=True), torch.zeros((70, 9), dtype=torch.bfloat16, device="cuda"))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 16, 128), (1, 1000, 960), (2, 17, 129), (9, 20, 300), (16, 130, 1000), (5, 5000, 512), (16, 4200, 700)])
+@pytest.mark.parametrize("dtype", SIXTEEN, ids=str)
+def test_few_rows_have_full_sums_anyway(lib, m, n, k, dtype):
+    """Where memory is what counts nothing is won by fewer bits."""
+    x, w, y = pairs(m, n, k)
+    a, b = lib.block8_pack(x.cuda(), E5M2), lib.block8_pack(w.cuda(), E4M3, True)
+    assert torch.equal(lib.block8_product(a, b, dtype).cpu(), y.to(dtype))
