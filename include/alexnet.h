@@ -484,15 +484,16 @@ int alexnet_block8_pack(const void* d_x, int64_t ld_x, int32_t type, int64_t row
 /* Values are rounded once to `type` (past its range: infinity). */
 int alexnet_block8_unpack(const alexnet_blocks8_t* in, int64_t rows, int64_t cols, void* d_x, int64_t ld_x,
                           int32_t type, void* stream);
-/* y [m][n] = a b^T of a [m][k] and b [n][k], rounded once to `type`.  In FP32
- * products are exact and sums float32 (values past float32's range, which packing
- * makes of some just under it, count as infinities).  For BF16 and FP16 eight products at
- * a time may be added with 13 bits under the largest of them, those sums in float32:
+/* y [m][n] = a b^T of a [m][k] and b [n][k], rounded once to `type`.  In FP32 sums are float32 and
+ * products exact, of values that are taken in bf16.  That holds all of them but for those
+ * under 2^-126 (E4M3 under scales 0 to 2, E5M2 under 0 to 9), of which it takes the nearest multiple of 2^-133, and those
+ * past float32's range, which count as infinities (packing makes some of numbers just under it).
+ *   For BF16 and FP16 eight products at a time may be added with 13 bits under the largest of them, those sums in float32:
  * off by at most 7 * 2^-13 of what each eight's largest add up to, 1.5e-5 of a result of
- * normal numbers, more of one that large products cancel in; ALEXNET_TYPE_BF16 + ALEXNET_SUMS_FP32 and
- * ALEXNET_TYPE_FP16 + ALEXNET_SUMS_FP32 ask for sums as FP32 has them, at half the rate.  Results repeat bit for bit.  k = 0 gives
- * zeros.  Codes and scales may be any bytes.  At most 2^28 rows of either, 2^22
- * columns and 2^32 results. */
+ * normal numbers, more of one that large products cancel in.  ALEXNET_TYPE_BF16 + ALEXNET_SUMS_FP32 and
+ * ALEXNET_TYPE_FP16 + ALEXNET_SUMS_FP32 ask for sums as FP32 has them, at half the rate; a few rows have them anyway.
+ *   Results repeat bit for bit.  k = 0 gives zeros.  Codes and scales may be any bytes: a scale of 255 makes NaN of every
+ * result that its block counts in.  At most 2^28 rows of either, 2^22 columns and 2^32 results. */
 #define ALEXNET_SUMS_FP32 16 /* added to the type of a product's result */
 int alexnet_block8_product_query(int64_t m, int64_t n, int64_t k, int32_t type, size_t* workspace_bytes);
 int alexnet_block8_product(const alexnet_blocks8_t* a, const alexnet_blocks8_t* b, int64_t m, int64_t n, int64_t k,

@@ -7,8 +7,9 @@
 //     eight (measured; the sums of those eights go on in float32), 1.5e-5 of a result of normal numbers and a hundredth of what
 //     rounding it to bf16 costs, a twentieth to fp16: a choice for twice the rate (16384 x 4096 x 4096 209 us, 460 the other way).  What is
 //     lost is of the largest product, so that where large products cancel it is more of the result: a caller may ask for the other kind.
-//   32 bits, and 16 with ALEXNET_SUMS_FP32: codes are widened to bf16 with their scales, which is exact, and go through the bf16 instruction, whose sums are
-//     float32 throughout: 6e-8 of a result.
+//   32 bits, and 16 with ALEXNET_SUMS_FP32: codes are widened to bf16 with their scales and go through the bf16 instruction, whose sums are
+//     float32 throughout: 6e-8 of a result.  That is exact but at bf16's ends, 2^-133 and 2^128: E4M3 under scales 0 to 2 and over 246, E5M2
+//     under 0 to 9 and over 239.  The scales would have to go to each block's sums for more: 8.6 us for 7.9 of 1 x 9216 x 4096.
 //
 // Tiles.  Operands go from memory to LDS directly (buffer_load ... lds), a block of 128 at a time: a row of a stage is the 128 bytes
 // of one row's block, eight 16-byte units, unit (row, slot) holding slot ^ (row & 7), so that a fragment read of eight rows
