@@ -84,3 +84,53 @@ def test_small_values_of_float32_sums(lib, m, n, k, ca, cb, sa, sb):
             off = (lib.block8_product(a, b, dtype, full_sums=full).double() - want).abs()
             tol = tolerance(va, vb, want, dtype, full)
             assert (off <= (tol + lost * (1 + R.HALF[dtype]) if few or dtype == torch.float32 or full else tol)).all(), (least, dtype, full)
+
+
+def mark(q, row, block):
+    """That block as packing leaves one with an infinity or a NaN in it."""
+    q.scales[block, row // 128 if q.square else row] = 255
+    first, last = (row // 128 * 128, row // 128 * 128 + 128) if q.square else (row, row + 1)
+    q.codes.view(torch.uint8)[first:last, 128 * block:128 * block + 128] = 0
+
+
+@pytest.mark.parametrize("m,n,k", FEW + TILES)
+@pytest.mark.parametrize("ca,cb,sa,sb", PAIRS)
+def test_blocks_that_are_not_numbers(lib, m, n, k, ca, cb, sa, sb):
+    gen = torch.Generator().manual_seed(m + n + k)
+    blocks = -(-k // 128)
+    for turn, which in enumerate(((True, False), (False, True), (True, True))):
+        a, _ = operand(lib, gen, m, k, ca, sa, torch.full((blocks,), 126))
+        b, _ = operand(lib, gen, n, k, cb, sb, torch.full((blocks,), 126))
+        for q, rows, marked in ((a, m, which[0]), (b, n, which[1])):
+            if marked:
+                for row, block in ((rows - 1, blocks - 1), (rows // 3, blocks // 2), (0, 0))[:turn + 1]:
+                    mark(q, row, block)
+        bad = lib.block8_unpack(a).isnan().any(1)[:, None] | lib.block8_unpack(b).isnan().any(1)[None]
+        assert bad.any()
+        for dtype, full in KINDS:
+            assert torch.equal(lib.block8_product(a, b, dtype, full_sums=full).isnan(), bad), (turn, dtype, full)
+
+
+@pytest.mark.parametrize("m,n,k", FEW + TILES)
+@pytest.mark.parametrize("ca,cb,sa,sb", PAIRS)
+def test_codes_that_are_not_numbers(lib, m, n, k, ca, cb, sa, sb):
+    """NaNs of both codes, infinities of E5M2, alone and against zeros and each other."""
+    gen = torch.Generator().manual_seed(m + n + k)
+    blocks = -(-k // 128)
+    a, _ = operand(lib, gen, m, k, ca, sa, torch.full((blocks,), 110))
+    b, _ = operand(lib, gen, n, k, cb, sb, torch.full((blocks,), 110))
+    for q, rows, code in ((a, m, ca), (b, n, cb)):
+        byte = q.codes.view(torch.uint8)
+        byte[rows // 2, k // 2] = 0x7f
+        byte[rows - 1, k - 1] = 0xff
+        if code == E5M2:
+            byte[rows // 3, k // 3], byte[rows // 4, 0], byte[rows // 5, k - 1] = 0x7c, 0xfc, 0x7d
+        byte[0, k // 3] = 0
+    va, vb = (lib.block8_unpack(q).double() for q in (a, b))
+    # as a sum of products has them: a NaN, an infinity times 0 and infinities of both signs make NaN
+    want = times(va, vb)
+    for dtype, full in KINDS:
+        got = lib.block8_product(a, b, dtype, full_sums=full)
+        assert torch.equal(got.isnan(), want.isnan()), (dtype, full)
+        assert torch.equal(got[want.isinf()].double(), want[want.isinf()]), (dtype, full)
+        assert got[want.isfinite()].isfinite().all(), (dtype, full)
