@@ -531,8 +531,9 @@ int alexnet_rms_norm_backward(const void* d_sum, int64_t ld_sum, const void* d_d
  * The tables are HOST arrays, read before the call returns; tensor i has sizes[i]
  * contiguous values of types[i] at grads[i] (anything where sizes[i] = 0).  outs null: in place.
  * Sums are float64, in a fixed order, so that no finite float32 gradient is too large or small for them.  d_norm
- * (float32, may be null in clip_gradients) receives the norm.  Where the norm is
- * an infinity or a NaN, or not over max_norm, gradients stay as they are.
+ * (float32, may be null in clip_gradients) receives the norm.  Where a gradient is
+ * an infinity or a NaN, or the norm not over max_norm, gradients stay as they are.  A norm of finite
+ * gradients past float32's range is handed out as an infinity, and they are scaled by the norm itself.
  * At most 2^20 tensors and 2^40 values. */
 int alexnet_clip_query(int32_t count, const int64_t* sizes, size_t* workspace_bytes);
 int alexnet_gradient_norm(int32_t count, const void* const* grads, const int64_t* sizes, const int32_t* types,

@@ -1146,8 +1146,9 @@ def gradient_norm(grads, stream=None) -> torch.Tensor:
 
 def clip_gradients(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
     """Scales all tensors by max_norm / norm if their gradient_norm is over max_norm, and returns that norm.  out: tensors of the same
-    sizes and types that receive the result (each may be its own gradient); otherwise that happens in place.  Where the norm is an
-    infinity or a NaN nothing is scaled."""
+    sizes and types that receive the result (each may be its own gradient); otherwise that happens in place.  Where a gradient is an
+    infinity or a NaN nothing is scaled.  A norm of finite gradients past float32's range is returned as an infinity, and they are
+    scaled by the norm itself."""
     what = "clip_gradients"
     grads, index, pointers, sizes, types = _gradients(grads, what)
     results = None
