@@ -527,7 +527,7 @@ int alexnet_rms_norm_backward(const void* d_sum, int64_t ld_sum, const void* d_d
 
 /* The norm of `count` gradients together, and clipping to it:
  *   norm = sqrt(sum over all tensors and values of g^2),
- *   out = g * min(1, max_norm / norm), rounded once to the tensor's type
+ *   out = g * min(1, max_norm / norm), rounded to float32 and that to the tensor's type
  * The tables are HOST arrays, read before the call returns; tensor i has sizes[i]
  * contiguous values of types[i] at grads[i] (anything where sizes[i] = 0).  outs null: in place.
  * Sums are float64, in a fixed order, so that no finite float32 gradient is too large or small for them.  d_norm

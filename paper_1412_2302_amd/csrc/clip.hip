@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a) {
   over_chunks(a, c0, c1, true, [&](const auto* in, auto* out, long n) {
     over_vectors(in, n, [&](float* v, auto vector, int has, int i) {
 #pragma unroll
-      for (int e = 0; e < decltype(vector)::value; ++e) v[e] = (float)((double)v[e] * factor);
+      for (int e = 0; e < decltype(vector)::value; ++e) v[e] = (float)((double)v[e] * factor);  // one rounding to 16 bits would cost 3 %: 122 M bf16 values 128 -> 132 us
       store_vector<decltype(vector)::value>(in + i, out + i, has, v, a.pass_by);
     });
   });

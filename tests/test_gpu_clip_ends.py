@@ -8,6 +8,10 @@ from dense8_reference import EPS32, HALF, f64
 pytestmark = pytest.mark.gpu
 
 
+def norm64(g):
+    return np.sqrt((f64(g) ** 2).sum())
+
+
 @pytest.mark.parametrize("places", ["there", "elsewhere"])
 @pytest.mark.parametrize("count", [3, 200])
 def test_a_norm_past_float32_of_finite_gradients(lib, places, count):
@@ -37,3 +41,15 @@ def test_an_infinity_or_a_nan_among_the_gradients(lib, bad, dtype, size):
         assert norm.isnan() if bad != bad else norm == float("inf")
         for g, b in zip(places or grads, before):
             assert torch.equal(g.nan_to_num(nan=123.0), b.nan_to_num(nan=123.0))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=str)
+def test_the_roundings_of_a_result(lib, dtype):
+    """From float64 to float32 and from there to the type, under the factor that the norm makes."""
+    g = torch.randn(400000, generator=torch.Generator().manual_seed(3)).to(dtype)
+    max_norm = float(np.float32(300.7))
+    out = torch.empty_like(g, device="cuda")
+    lib.clip_gradients([g.cuda()], max_norm, out=[out])
+    want = (g.double() * (max_norm / norm64(g))).float().to(dtype)
+    # the order of the sum moves the factor by some of float64's steps, 2^-29 of float32's: hardly a result falls the other way
+    assert (out.cpu() != want).sum() <= 2
