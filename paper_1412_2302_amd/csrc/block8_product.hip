@@ -314,9 +314,12 @@ __global__ void __launch_bounds__(SIDE == 256 ? 512 : 256) __attribute__((amdgpu
     return I == 0 ? stage0 : I == 1 ? stage1 : I == 2 ? stage2 : stage3;
   };
   Scales s[STAGES];
+  // arrived() takes a stage's scales for its codes: none may be sent before them
   for_each_index([&](auto i) {
     load(stage(i), decltype(i)::value);
+    __builtin_amdgcn_sched_barrier(0);
     s[decltype(i)::value] = scales();
+    __builtin_amdgcn_sched_barrier(0);
   }, std::make_integer_sequence<int, STAGES - 1>());
   load(stage(std::integral_constant<int, STAGES - 1>()), STAGES - 1);
   arrived(s[0]);
