@@ -4,8 +4,8 @@
 // + 7: a row's block is sixteen neighbouring lanes and a column's the same lanes of all waves, so both kinds of scales and of
 // codes come from one read.  Of the transpose a thread has eight codes of each of its columns as two words (the conversion takes
 // two values to a word, which here are two rows); they go through LDS to be stored as whole lines.
-// 4096 x 9216 float32 to square blocks both ways 50 us (4.5 TB/s), 43264 x 384 bf16 both ways 13.5 (4.9 TB/s), 256 x 9216 bf16, which is
-// 144 workgroups, 5.1: the eight loads of a thread are on their way together.
+// In a layer's pass 4096 x 9216 float32 to square blocks both ways 51 us (4.5 TB/s), 43264 x 384 bf16 both ways 16.5 (4.0 TB/s), 256 x 9216
+// bf16, which is 144 workgroups, 8.1; replayed 42, 14 and 6.1.  The eight loads of a thread are on their way together.
 #include <algorithm>
 #include <type_traits>
 
@@ -76,7 +76,7 @@ struct Patch {
     return floats_to_codes<CODE, 8>(f, s);
   }
 };
-// 16 bits: two values to a word throughout, which is half the work and half the registers (43264 x 384 both ways 16.2 -> 13.5 us,
+// 16 bits: two values to a word throughout, which is half the work and half the registers (43264 x 384 both ways, replayed, 16.2 -> 13.5 us,
 // 256 x 9216 6.2 -> 5.1)
 template <typename T>
 struct Patch16 {
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(256) block8_pack_kernel(Pack8Args a) {
   }
 }
 
-// Eight codes a thread at a time.  43264 x 384 to bf16 10 us (4.8 TB/s): what comes from the cache and memory bounds it.
+// Eight codes a thread at a time.  43264 x 384 to bf16 11 us (4.4 TB/s): what comes from the cache and memory bounds it.
 struct Unpack8Args {
   const uint8_t *codes, *scales;
   void* x;

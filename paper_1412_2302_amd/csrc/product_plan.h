@@ -21,13 +21,12 @@ constexpr int kProductSlices = 64;
 constexpr long kProductGrid = 1L << 22;  // workgroups of a launch, of 512 threads at most; 2^32 results are at most 2^21 128-tiles and a few
 
 // What a model of the measured times makes cheapest, in microseconds.
-//   Rows: a round of workgroups, and in it eight blocks, or the memory they come from.  With few workgroups fewer rows each give more of
-//   them: 64 x 512 x 4096 4.2 by sixteens, 6.4 by 64.  64 x 4096 x 4096 7.1 (128-tiles in four slices 13.2), 128 x 4096 x 4096 10.3 (15.8),
-//   256 x 4096 x 4096 20.2 (20.8), 512 x 4096 x 1024 15.4 (10.3).
-//   128-tiles: a step of a workgroup that has a compute unit to itself, and of two that share one; 2048 x 4096 x 4096 37 (256-tiles 50),
-//   43264 x 384 x 384 19 (26), 256 x 9216 x 4096 in four slices 24 (one 51, eight 25); with four stages, where a workgroup is alone,
-//   22, 256 x 4096 x 9216 26 -> 21, but 2048 x 4096 x 4096 37 -> 46.
-//   256-tiles, one to a compute unit: 16384 x 4096 x 4096 222 (128-tiles 266), 4096 x 4096 x 4096 65 (77).
+//   Rows: a round of workgroups, and in it eight blocks, or the memory they come from.  64 x 4096 x 4096 7.7 (128-tiles in four slices
+//   12.8), 128 x 4096 x 4096 11.4 (15.3), 512 x 4096 x 1024 10.6 (14.9), 256 x 4096 x 4096 19.0 (19.1).
+//   128-tiles: a step of a workgroup that has a compute unit to itself, and of two that share one; 2048 x 4096 x 4096 40 (256-tiles 50),
+//   43264 x 384 x 384 20 (26), 256 x 9216 x 4096 in four slices 25 (one 53, eight 26); with four stages, where a workgroup is alone,
+//   22, 256 x 4096 x 9216 27 -> 22, but 2048 x 4096 x 4096 40 -> 46.
+//   256-tiles, one to a compute unit: 16384 x 4096 x 4096 213 (128-tiles 270), 4096 x 4096 x 4096 57 (71).
 //   Slices are written and read once more each, in a second launch.
 // wide: the products are those of bf16, of which 256-tiles have more operands than registers.
 inline ProductPlan product_plan(long m, long n, long k, bool wide) {

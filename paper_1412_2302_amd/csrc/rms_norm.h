@@ -24,7 +24,8 @@ struct RmsArgs {
 };
 
 // What fits in registers: vectors of a row <= TEAM * NV.  The backward pass holds a row's values three times over (with gamma and its
-// gradient), so its teams are larger: 4096 x 9216 bf16 104 us by 256 lanes of eight vectors, 67 by 512 of three.
+// gradient), so its teams are larger: 4096 x 9216 bf16 104 us by 256 lanes of eight vectors, 67 by 512 of three.  Rows that
+// no team holds: 64 x 65536 bf16 13 us from registers, 64 x 70000 17 read twice.
 struct RmsPlan {
   int team, nv;  // nv 0: rows are read twice
 };

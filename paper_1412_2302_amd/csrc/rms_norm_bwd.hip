@@ -4,7 +4,8 @@
 //
 // A team walks down rows and keeps its columns' share of dgamma in registers; workgroups leave theirs as a row of the workspace and a second
 // launch adds those up in one order.
-// 16384 x 4096 bf16 with dsum 107 us (5.0 TB/s) and 5 for the parts, 93312 x 256 float32 50 (5.7 TB/s) and 4.
+// 16384 x 4096 bf16 with dsum 110 us (4.9 TB/s) and 5 for the parts, 93312 x 256 float32 50 (5.7 TB/s) and 4.
+// Rows that no registers hold are read twice: 2048 x 20000 bf16 106 us (2048 x 16384, which they hold, 65).
 #include <algorithm>
 #include <type_traits>
 
